@@ -450,6 +450,154 @@ crvq_status crvq_quantize_layer(const float* W, const float* X, int64_t M, int64
                                 const crvq_layer_outputs* out, crvq_layer_report* report,
                                 crvq_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A decode step beside the quantized matrices: a paged key/value cache in 8 bits, attention over
+ * it, and products with 4-bit weights (output heads and projections that stay outside the vector
+ * quantizer). The paper has no counterpart: it compresses weights only, and a served model reads
+ * its cache beside them in every step.
+ * ------------------------------------------------------------------------------------------ */
+
+/* Element types of activations. */
+enum { CRVQ_F32 = 0, CRVQ_BF16 = 1, CRVQ_F16 = 2 };
+
+/* Cache formats: int8 codes -127..127, or e4m3 (fp8, largest value 448). */
+enum { CRVQ_KV_INT8 = 0, CRVQ_KV_E4M3 = 1 };
+
+/* Activations of `heads` heads: element c of head h of token t is data[t * ld_tok + h * ld_head + c]
+ * (strides in elements; any, also views into a fused projection's rows), 0 <= c < head_dim. */
+typedef struct crvq_heads {
+  void* data;
+  int64_t ld_tok;
+  int64_t ld_head;
+  int32_t heads;
+  int32_t type; /* CRVQ_F32, CRVQ_BF16 or CRVQ_F16 */
+} crvq_heads;
+
+/*
+ * A paged cache of n_seq sequences. Page p of kv head h holds `page` tokens of head_dim codes:
+ *   code of token slot t: K[p * page_stride + (h * page + t) * head_dim + c]   (V the same),
+ *   its scale:            k_scale[(p * n_kv + h) * (page / 16) + t / 16],
+ * one fp32 scale per 16 tokens ("block") and head; the value is code * scale. Token i of sequence b
+ * lies in slot i % page of page pages[b * ld_pages + i / page]. Only pages that hold tokens are
+ * looked up. Entries outside [0, n_pages) and lengths outside [0, max_pages * page] are skipped and
+ * reported as CRVQ_ERR_DEVICE by crvq_sync (what is skipped counts as not cached).
+ */
+typedef struct crvq_kv_cache {
+  void* K;               /* 16-byte aligned */
+  void* V;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* pages;  /* [n_seq x max_pages], row stride ld_pages */
+  const int32_t* lens;   /* [n_seq] tokens of every sequence, those of the present step included */
+  int64_t n_pages;       /* pages in the pool */
+  int64_t page_stride;   /* bytes from page to page, >= n_kv * page * head_dim, a multiple of 16 */
+  int64_t ld_pages;
+  int32_t n_seq;
+  int32_t max_pages;
+  int32_t page;          /* tokens per page: a multiple of 16 */
+  int32_t n_kv;
+  int32_t head_dim;      /* 64, 128 or 256 */
+  int32_t format;        /* CRVQ_KV_INT8 or CRVQ_KV_E4M3 */
+} crvq_kv_cache;
+
+/* Rotary positions: channel pairs (i, i + half) or, interleaved, (2 i, 2 i + 1) for 0 <= i < half
+ * turn by the angle whose cosine and sine are cos/sin[pos * ld + i]:
+ * (a, b) -> (a cos - b sin, b cos + a sin); channels from 2 * half on stay. */
+typedef struct crvq_rotary {
+  const float* cos;
+  const float* sin;
+  const int32_t* positions; /* [n_tok] row of the tables per token, or NULL: its place in the cache */
+  int64_t n_pos;            /* rows of the tables; a position outside is reported and not rotated */
+  int64_t ld;
+  int32_t half;             /* 1 <= half <= head_dim / 2 */
+  int32_t interleaved;
+} crvq_rotary;
+
+/*
+ * Appends the keys and values of n_tok new tokens to the cache, keys rotated on the way. The new
+ * tokens of sequence b are its last ones: k and v rows new_off[b] .. new_off[b + 1) go to the places
+ * lens[b] - (new_off[b + 1] - new_off[b]) .. lens[b].
+ *   new_off  [n_seq + 1] int32, or NULL: n_tok / n_seq tokens each.
+ *   rot      NULL: no rotation.
+ *   q, q_out NULL, or the step's queries and where their rotated values go (may be the same memory).
+ * A block's scale is the largest of its new values' magnitudes times 1/127 (1/448 for e4m3), or the
+ * present scale where that is larger and the block holds earlier tokens; their codes c then become
+ * round(c * (old scale / new scale)), the new ones round(x / scale), ties to even, all in fp32. The
+ * rotation rounds each product and sum to fp32. Values that are not finite are stored as 0 and
+ * reported as CRVQ_ERR_NUMERIC by crvq_sync. Appending the same tokens again changes nothing.
+ */
+crvq_status crvq_cache_append(const crvq_kv_cache* cache, const crvq_heads* k, const crvq_heads* v,
+                              int64_t n_tok, const int32_t* new_off, const crvq_rotary* rot,
+                              const crvq_heads* q, const crvq_heads* q_out, crvq_stream_t stream);
+
+/*
+ * Values of token ranges: rows off[b] .. off[b + 1) of K_out and V_out ([n_tok x n_kv x head_dim],
+ * contiguous, of `type`, 16-byte aligned) get code * scale of the tokens start[b], start[b] + 1, ...
+ * of sequence b. Tokens that the sequence does not have read as 0 and are reported.
+ *   start [n_seq] int32, off [n_seq + 1] int32 with off[n_seq] = n_tok.
+ */
+crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, const int32_t* off,
+                            int64_t n_tok, int32_t type, void* K_out, void* V_out,
+                            crvq_stream_t stream);
+
+/*
+ * Attention of the newest tokens of every sequence over the cache:
+ *   out[t][h] = sum_j p_j V_j / sum_j p_j,  p_j = exp(scale * q[t][h] . K_j - max),
+ * K_j and V_j the cached values of kv head h / (q->heads / n_kv). The queries of sequence b are rows
+ * q_off[b] .. q_off[b + 1); the last of them stands at place lens[b] - 1, the others before it. A
+ * query at place t sees the key at place j when 0 <= j < lens[b], when j <= t (causal), and when
+ * j > t - window (window > 0). A query that sees nothing gets 0.
+ *   q_off   [n_seq + 1] int32, or NULL: n_tok / n_seq queries each.
+ *   out     [n_tok x q->heads x head_dim], the type of q.
+ *   lse     [n_tok x q->heads] fp32 or NULL: log sum_j exp(scale * q . K_j), -inf where nothing is seen.
+ * Scores, maxima and sums are fp32, products run on the tensor cores with fp32 accumulation. q is
+ * taken relative to a power of two per row in one fp16 operand (exact for 16-bit types but for
+ * elements below 2^-14 of the row's largest) or, from fp32, in two; the weights p_j are rounded to
+ * fp16 for 16-bit types and kept to 22 bits for fp32. Work is split over the cached tokens by the
+ * lengths on the device and joined in a fixed order: results are identical run to run.
+ * Requires q->heads to be a multiple of n_kv.
+ */
+crvq_status crvq_cache_attention(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok,
+                                 const int32_t* q_off, float scale, int32_t causal, int32_t window,
+                                 const crvq_heads* out, float* lse, crvq_stream_t stream);
+
+/*
+ * A matrix in 4 bits with a scale per group of inputs: W[i][j] = (code - zero) * scale, code of (i, j)
+ * the low (j even) or high (j odd) four bits of codes[i * ld_codes + j / 2], scale and zero those of
+ * group j / group of row i.
+ */
+typedef struct crvq_q4_matrix {
+  uint8_t* codes;
+  void* scales;      /* [M x ceil(N / group)] bf16, row stride ld_scales */
+  uint8_t* zeros;    /* the same shape and row stride (each 0..15), or NULL: 8 */
+  int64_t M;
+  int64_t N;
+  int64_t ld_codes;  /* bytes, >= ceil(N / 2) */
+  int64_t ld_scales; /* elements, >= ceil(N / group) */
+  int32_t group;     /* 32, 64 or 128 */
+  int32_t _pad;
+} crvq_q4_matrix;
+
+/*
+ * W (M x N of `type`, row stride ldw) to 4 bits, by rounding to the nearest level. Without zeros the
+ * scale of a group is bf16(max|w| * (1/7)), the code round(w / scale) + 8; with zeros, for lo = min(w, 0)
+ * and hi = max(w, 0), scale = bf16((hi - lo) * (1/15)), zero = round(-lo / scale), code = round(w /
+ * scale) + zero; ties to even, clamped to 0..15. A group of zeros gets scale 0.
+ *   W_hat [M x N] fp32 (contiguous) or NULL: the values that the codes stand for.
+ * Values that are not finite count as 0 and are reported as CRVQ_ERR_NUMERIC by crvq_sync.
+ */
+crvq_status crvq_q4_quantize(const void* W, int64_t ldw, int32_t type, const crvq_q4_matrix* m,
+                             float* W_hat, crvq_stream_t stream);
+
+/*
+ * Y = X W^T for b inputs (X b x N, Y b x M, both of `type`, row strides ldx and ldy). Codes minus
+ * zero points are exact operands of the tensor cores, X one operand of its own type or, from fp32,
+ * three bf16 ones (24 bits); sums are fp32 in a fixed order, each group's scaled once.
+ * Requires 1 <= b <= 32.
+ */
+crvq_status crvq_q4_matvec(const crvq_q4_matrix* m, const void* X, int64_t ldx, int64_t b,
+                           int32_t type, void* Y, int64_t ldy, crvq_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

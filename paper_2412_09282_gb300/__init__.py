@@ -16,3 +16,7 @@ from .api import (  # noqa: F401
     crvq_version, CrvqError, IMPORTANCE_WA, IMPORTANCE_W_ONLY, IMPORTANCE_RANDOM,
     IMPORTANCE_WA_INV, library_path,
 )
+from .decode import (  # noqa: F401
+    KVCache, Q4Matrix, crvq_cache_append, crvq_cache_attention, crvq_cache_read, crvq_q4_matvec,
+    crvq_q4_quantize,
+)

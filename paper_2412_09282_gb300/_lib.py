@@ -46,6 +46,30 @@ class crvq_kernel_stat(C.Structure):
                 ("units", C.c_double)]
 
 
+class crvq_heads(C.Structure):
+    _fields_ = [("data", c_vp), ("ld_tok", C.c_int64), ("ld_head", C.c_int64),
+                ("heads", C.c_int32), ("type", C.c_int32)]
+
+
+class crvq_kv_cache(C.Structure):
+    _fields_ = [("K", c_vp), ("V", c_vp), ("k_scale", c_vp), ("v_scale", c_vp), ("pages", c_vp),
+                ("lens", c_vp), ("n_pages", C.c_int64), ("page_stride", C.c_int64),
+                ("ld_pages", C.c_int64), ("n_seq", C.c_int32), ("max_pages", C.c_int32),
+                ("page", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32),
+                ("format", C.c_int32)]
+
+
+class crvq_rotary(C.Structure):
+    _fields_ = [("cos", c_vp), ("sin", c_vp), ("positions", c_vp), ("n_pos", C.c_int64),
+                ("ld", C.c_int64), ("half", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class crvq_q4_matrix(C.Structure):
+    _fields_ = [("codes", c_vp), ("scales", c_vp), ("zeros", c_vp), ("M", C.c_int64),
+                ("N", C.c_int64), ("ld_codes", C.c_int64), ("ld_scales", C.c_int64),
+                ("group", C.c_int32), ("_pad", C.c_int32)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "crvq_last_error": (C.c_char_p, []),
@@ -94,6 +118,14 @@ SIGNATURES = {
     "crvq_quantize_layer": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int64,
                                         C.POINTER(crvq_config), C.POINTER(crvq_layer_outputs),
                                         C.POINTER(crvq_layer_report), c_vp]),
+    # (the structures of these go by address, c_void_p: ctypes then converts a plain int)
+    "crvq_cache_append": (C.c_int32, [c_vp, c_vp, c_vp, C.c_int64, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "crvq_cache_read": (C.c_int32, [c_vp, c_vp, c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
+    "crvq_cache_attention": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, C.c_float, C.c_int32,
+                                         C.c_int32, c_vp, c_vp, c_vp]),
+    "crvq_q4_quantize": (C.c_int32, [c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
+    "crvq_q4_matvec": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int32, c_vp, C.c_int64,
+                                   c_vp]),
 }
 
 _lib = None

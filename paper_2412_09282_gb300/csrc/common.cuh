@@ -40,6 +40,15 @@ void clear_last_error();
     if (s_ != CRVQ_OK) return s_;         \
   } while (0)
 
+// Body of a C entry point: no C++ exception (a host allocation that fails) crosses the boundary.
+#define CRVQ_ENTRY(...)         \
+  try {                         \
+    ::crvq::clear_last_error(); \
+    __VA_ARGS__                 \
+  } catch (...) {               \
+    return CRVQ_ERR_NOMEM;      \
+  }
+
 // Launch bookkeeping: counts the launch and reports a launch-configuration failure right
 // after a <<<>>> launch.
 void count_launch();
