@@ -28,9 +28,20 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kTile = kCacheBlock * kWarps;  // tokens
+// Blocks that a warp takes at a time (two: twice the independent work, and one maximum for both)
+template <int D>
+constexpr int kBlocks = D == 256 ? 1 : 2;
+template <int D>
+constexpr int kTile = kCacheBlock * kBlocks<D> * kWarps;  // tokens of a CTA at a time
 constexpr float kWeight = 16384.f;           // weights are scaled into fp16's range
 constexpr float kLog2e = 1.4426950408889634f;
+
+// 2^x (within 2 ulp; results below 2^-126 are 0)
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 struct AttendArgs {
   CacheView c;
@@ -55,14 +66,14 @@ struct Seq {
   int groups;       // column groups
 };
 
-template <int COLS>
+template <int D, int COLS>
 __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b) {
   Seq s;
   seq_rows(a.rows, b, &s.first, &s.n, a.err);
   s.len = seq_len(a.c, b, a.err);
   const int begin = a.window > 0 ? max(0, s.len - s.n - a.window + 1) : 0;
-  s.lo = min(begin, s.len) / kTile;
-  s.tiles = max(1, (s.len + kTile - 1) / kTile - s.lo);
+  s.lo = min(begin, s.len) / kTile<D>;
+  s.tiles = max(1, (s.len + kTile<D> - 1) / kTile<D> - s.lo);
   s.groups = (int)(((int64_t)s.n * a.group + COLS - 1) / COLS);
   return s;
 }
@@ -75,12 +86,12 @@ struct Unit {
 };
 
 // Tiles of all units (warp-wide).
-template <int COLS>
+template <int D, int COLS>
 __device__ int64_t total_tiles(const AttendArgs& a) {
   const int lane = threadIdx.x & 31;
   int64_t sum = 0;
   for (int b = lane; b < a.c.n_seq; b += 32) {
-    const Seq s = load_seq<COLS>(a, b);
+    const Seq s = load_seq<D, COLS>(a, b);
     sum += (int64_t)s.groups * s.tiles;
   }
 #pragma unroll
@@ -89,7 +100,7 @@ __device__ int64_t total_tiles(const AttendArgs& a) {
 }
 
 // The unit that holds position w of the line, 0 <= w < total (warp-wide).
-template <int COLS>
+template <int D, int COLS>
 __device__ Unit locate(const AttendArgs& a, int64_t w) {
   const int lane = threadIdx.x & 31;
   int64_t base = 0;
@@ -98,7 +109,7 @@ __device__ Unit locate(const AttendArgs& a, int64_t w) {
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
     int64_t cost = 0;
     if (b0 + lane < a.c.n_seq) {
-      const Seq s = load_seq<COLS>(a, b0 + lane);
+      const Seq s = load_seq<D, COLS>(a, b0 + lane);
       cost = (int64_t)s.groups * s.tiles * a.c.n_kv;
     }
     int64_t incl = cost;
@@ -116,7 +127,7 @@ __device__ Unit locate(const AttendArgs& a, int64_t w) {
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
-  u.s = load_seq<COLS>(a, u.b);
+  u.s = load_seq<D, COLS>(a, u.b);
   const int64_t rem = w - base;
   const int64_t idx = rem / u.s.tiles;
   u.tile = (int)(rem - idx * u.s.tiles);
@@ -174,34 +185,44 @@ __device__ __forceinline__ int word(const uint4& u, int i) {
   return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
 }
 
-// Codes of one block that a lane holds: K rows gid and gid + 8, V rows 2 tig, 2 tig + 1, + 8, + 9.
+// The pieces of one block that a lane needs: K rows key_row and key_row + 8 (16 codes from every 64), V rows
+// 2 tig, 2 tig + 1, + 8, + 9 (16 codes, 8 of 64). Every lane copies its own pieces to shared memory,
+// piece by piece with the lanes side by side: no bank conflicts, and no lane waits for another's copy.
 template <int D>
-struct BlockRegs {
-  static constexpr int kChunks = D / 64;                // 16-byte pieces of a key row per lane
-  static constexpr int kPieces = D >= 128 ? D / 128 : 1;  // 16-byte (D = 64: 8-byte) pieces of a value row
-  uint4 k[2][kChunks];
-  uint4 v[4][kPieces];
+struct Pieces {
+  static constexpr int kChunks = D / 64;                  // 16-byte pieces of a key row
+  static constexpr int kKeys = 2 * kChunks;
+  static constexpr int kValues = D == 64 ? 2 : D / 32;    // 16-byte units: D = 64 has two 8-byte pieces in one
+  static constexpr int kBytes = (kKeys + kValues) * 512;  // of a warp and block
 };
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Starts the copies of the block whose codes begin at byte `at` of K and V; dst: this warp's stage.
 template <int D>
-__device__ __forceinline__ void load_block(const CacheView& c, int64_t at, BlockRegs<D>& r) {
+__device__ __forceinline__ void start_block(const CacheView& c, int64_t at, uint32_t dst) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const uint8_t* k = c.K + at + gid * D + 16 * tig;
+  dst += lane * 16;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < BlockRegs<D>::kChunks; ++j)
-      r.k[i][j] = __ldg(reinterpret_cast<const uint4*>(c.K + at + (gid + 8 * i) * D + 64 * j + 16 * tig));
+    for (int j = 0; j < Pieces<D>::kChunks; ++j) copy16(dst + (i * Pieces<D>::kChunks + j) * 512, k + 8 * i * D + 64 * j);
+  dst += Pieces<D>::kKeys * 512;
+  const uint8_t* v = c.V + at + 2 * tig * D + (D == 64 ? 8 : 16) * gid;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint8_t* row = c.V + at + (2 * tig + (i & 1) + 8 * (i >> 1)) * D;
+    const uint8_t* row = v + ((i & 1) + 8 * (i >> 1)) * D;
+    if constexpr (D == 64) {
+      copy8(dst + (i >> 1) * 512 + (i & 1) * 8, row);
+    } else {
 #pragma unroll
-    for (int j = 0; j < BlockRegs<D>::kPieces; ++j) {
-      if constexpr (D == 64) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(row + 8 * gid));
-        r.v[i][j] = make_uint4(u.x, u.y, 0, 0);
-      } else {
-        r.v[i][j] = __ldg(reinterpret_cast<const uint4*>(row + 128 * j + 16 * gid));
-      }
+      for (int j = 0; j < D / 128; ++j) copy16(dst + (i * (D / 128) + j) * 512, row + 128 * j);
     }
   }
 }
@@ -211,39 +232,89 @@ struct Shape {
   static constexpr int kCols = 8 * NT;
   static constexpr int kQRow = D + 8;  // halves per query row, padded against bank conflicts
   static constexpr size_t kQ = (size_t)kCols * kQRow * 2 * (SPLIT ? 2 : 1);
-  static constexpr size_t kO = (size_t)kWarps * kCols * D * 4;
-  static constexpr size_t kSmem = kQ + kO + 4 * kCols * 4 + 3 * kWarps * kCols * 4;
+  // the ring of blocks on their way; at a unit's end each warp's outputs [kCols][D] lie in its own part
+  static constexpr int kStages = D == 128 ? 2 : 3;
+  static constexpr int kRing = Pieces<D>::kBytes * kBlocks<D> * kStages;
+  static_assert(kRing >= kCols * D * 4, "outputs fit the ring");
+  static constexpr size_t kSmem = kQ + (size_t)kWarps * kRing + 3 * kCols * 4 + 3 * kWarps * kCols * 4;
+  // CTAs per SM, by registers (128 threads of 128 or 168) and shared memory
+  static constexpr int kPerSm = D == 64 ? (NT == 1 ? 4 : 3) : (D == 128 ? 3 : 2);
   static constexpr int kSlot = kCols * (D + 2);  // floats of a part
 };
 
 template <int D, int NT, int FMT, bool SPLIT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, Shape<D, NT, FMT, SPLIT>::kPerSm)
 attend_kernel(const __grid_constant__ AttendArgs a) {
   using S = Shape<D, NT, FMT, SPLIT>;
   constexpr int COLS = S::kCols;
   extern __shared__ __align__(16) char sm[];
   __half* q_s = reinterpret_cast<__half*>(sm);                       // [split][COLS][kQRow]
-  float* o_s = reinterpret_cast<float*>(sm + S::kQ);                 // [kWarps][COLS][D]
-  float* f_s = o_s + kWarps * COLS * D;                              // [COLS] score factor
+  char* ring = sm + S::kQ;                                           // [kWarps][kStages][pieces][lane]
+  float* f_s = reinterpret_cast<float*>(ring + kWarps * S::kRing);   // [COLS] score factor
   int* beg_s = reinterpret_cast<int*>(f_s + COLS);                   // [COLS] first and last + 1 key seen
   int* end_s = beg_s + COLS;
-  float* m_s = reinterpret_cast<float*>(end_s + COLS) + COLS;        // [kWarps][COLS]
+  float* m_s = reinterpret_cast<float*>(end_s + COLS);               // [kWarps][COLS]
   float* l_s = m_s + kWarps * COLS;
   float* r_s = l_s + kWarps * COLS;                                  // value reference of a warp
-  pdl_trigger();
-  pdl_wait();
+  pdl_wait();  // (no early trigger: waiting blocks of the next kernels would take this one's places)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-  const int64_t total = total_tiles<COLS>(a);
-  const int64_t w0 = share_begin(total, blockIdx.x, a.shares);
-  const int64_t w1 = share_begin(total, blockIdx.x + 1, a.shares);
+  const int64_t total = total_tiles<D, COLS>(a);
+  const int shares = (int)min((int64_t)a.shares, total);
+  if ((int)blockIdx.x >= shares) return;
+  const int64_t w1 = share_begin(total, blockIdx.x + 1, shares);
+  char* mine = ring + warp * S::kRing;
+  const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
 
-  for (int64_t w = w0; w < w1;) {
-    const Unit u = locate<COLS>(a, w);
+  for (int64_t w = share_begin(total, blockIdx.x, shares); w < w1;) {
+    const Unit u = locate<D, COLS>(a, w);
     const int64_t unit_end = u.begin + u.s.tiles;
     const int t_end = (int)(min(unit_end, w1) - u.begin);
     const int len = u.s.len, group = a.group;
     const int col0 = u.cg * COLS, n_cols = min(COLS, u.s.n * group - col0);
     __syncthreads();  // the previous unit's shared memory has been read
+
+    // A lane looks up the place and the scales of every 32nd of this warp's blocks; the copies of
+    // kStages - 1 blocks are on their way ahead of the one in work.
+    const int reach = u.s.len - u.s.n + (col0 + n_cols - 1) / group + 1;  // past the last column's place
+    const int some_e = a.causal ? min(len, reach) : len;
+    const int some_b = a.window > 0 ? max(0, len - u.s.n + col0 / group - a.window + 1) : 0;
+    int64_t at_l = -1;
+    float sk_l = 0.f, sv_l = 0.f, sk_old = 0.f, sv_old = 0.f;
+    uint32_t has = 0, has_old = 0;  // blocks of the present 32 and of those before that some query sees
+    constexpr int NB = kBlocks<D>;
+    auto start = [&](int i) {       // the warp's i-th blocks NB i .., counted from the part's first tile
+      if (u.tile + i < t_end) {
+        const int i0 = i * NB;
+        if ((i0 & 31) == 0) {
+          sk_old = sk_l;
+          sv_old = sv_l;
+          has_old = has;
+          const int tl = u.tile + (i0 + lane) / NB;
+          const int tok = (u.s.lo + tl) * kTile<D> + (warp * NB + lane % NB) * kCacheBlock;
+          at_l = -1;
+          if (tl < t_end && tok < some_e && tok + kCacheBlock > some_b) {
+            const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
+            if (page >= 0) {
+              const int in = tok % a.c.page;
+              at_l = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
+              const int64_t at_s = (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock;
+              sk_l = __ldg(a.c.ks + at_s);
+              sv_l = __ldg(a.c.vs + at_s);
+            }
+          }
+          has = __ballot_sync(0xffffffffu, at_l >= 0);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int64_t at = __shfl_sync(0xffffffffu, at_l, (i0 + b) & 31);
+          if (at >= 0) start_block<D>(a.c, at, mine_u + ((i % S::kStages) * NB + b) * Pieces<D>::kBytes);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; ++i) start(i);
+
     // queries: a warp per column, relative to the power of two at its largest element
     for (int col = warp; col < COLS; col += kWarps) {
       float x[D / 32];
@@ -288,12 +359,11 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         kb[t][e] = beg_s[8 * t + 2 * tig + e];
         ke[t][e] = end_s[8 * t + 2 * tig + e];
       }
-    // keys that some / every column sees (positions do not fall from column to column)
-    const int some_b = beg_s[0], some_e = end_s[n_cols - 1];
+    // keys that every column sees (positions do not fall from column to column)
     const int every_b = beg_s[n_cols - 1], every_e = end_s[0];
 
     float o[D / 16][NT][4];
-    float m[NT][2], l[NT][2], ref = 0.f;
+    float m[NT][2], l[NT][2], ref = 0.f, inv_ref = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -308,165 +378,183 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         l[t][e] = 0.f;
       }
 
-    // A lane looks up the place and the scales of every 32nd of this warp's blocks.
-    int64_t at_l = -1;
-    float sk_l = 0.f, sv_l = 0.f;
-    auto look_up = [&](int t0) {
-      const int t = t0 + lane;
-      const int tok = (u.s.lo + t) * kTile + warp * kCacheBlock;
-      at_l = -1;
-      if (t < t_end && tok < some_e && tok + kCacheBlock > some_b) {
-        const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
-        if (page >= 0) {
-          const int in = tok % a.c.page;
-          at_l = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
-          const int64_t at_s = (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock;
-          sk_l = __ldg(a.c.ks + at_s);
-          sv_l = __ldg(a.c.vs + at_s);
-        }
+    const int n_tiles = t_end - u.tile;
+    for (int i = 0; i < n_tiles; ++i) {
+      start(i + S::kStages - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+      const bool old = (i * NB >> 5) != (min(i + S::kStages - 1, n_tiles - 1) * NB >> 5);
+      const uint32_t live = (old ? has_old : has) >> (i * NB & 31);
+      if ((live & ((1u << NB) - 1)) == 0) continue;
+      float sk[NB], sv[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        sk[b] = __shfl_sync(0xffffffffu, old ? sk_old : sk_l, (i * NB + b) & 31);
+        sv[b] = __shfl_sync(0xffffffffu, old ? sv_old : sv_l, (i * NB + b) & 31);
       }
-    };
-    BlockRegs<D> cur, nxt;
-    look_up(u.tile);
-    int64_t at = __shfl_sync(0xffffffffu, at_l, 0);
-    float sk = __shfl_sync(0xffffffffu, sk_l, 0), sv = __shfl_sync(0xffffffffu, sv_l, 0);
-    if (at >= 0) load_block<D>(a.c, at, cur);
-    for (int t = u.tile; t < t_end; ++t) {
-      const int step = (t + 1 - u.tile) & 31;
-      if (step == 0) look_up(t + 1);
-      const int64_t at_n = t + 1 < t_end ? __shfl_sync(0xffffffffu, at_l, step) : -1;
-      const float sk_n = __shfl_sync(0xffffffffu, sk_l, step), sv_n = __shfl_sync(0xffffffffu, sv_l, step);
-      if (at_n >= 0) load_block<D>(a.c, at_n, nxt);
-      if (at >= 0) {
-        const int tok = (u.s.lo + t) * kTile + warp * kCacheBlock;
-        float s[NT][4];
+      const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
+      const uint4* stage = reinterpret_cast<const uint4*>(mine + (i % S::kStages) * NB * Pieces<D>::kBytes) + lane;
+      constexpr int kUnits = Pieces<D>::kBytes / 16;
+
+      float s[NB][NT][4];
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-          uint32_t qv[SPLIT ? 2 : 1][NT][8];
+          for (int e = 0; e < 4; ++e) s[b][n][e] = 0.f;
 #pragma unroll
-          for (int z = 0; z < (SPLIT ? 2 : 1); ++z)
+      for (int j = 0; j < D / 64; ++j) {
+        uint32_t qv[SPLIT ? 2 : 1][NT][8];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-              const uint4* p = reinterpret_cast<const uint4*>(
-                  q_s + (z * COLS + 8 * i + gid) * S::kQRow + 64 * j + 16 * tig);
-              const uint4 x = p[0], y = p[1];
-              qv[z][i][0] = x.x; qv[z][i][1] = x.y; qv[z][i][2] = x.z; qv[z][i][3] = x.w;
-              qv[z][i][4] = y.x; qv[z][i][5] = y.y; qv[z][i][6] = y.z; qv[z][i][7] = y.w;
-            }
+        for (int z = 0; z < (SPLIT ? 2 : 1); ++z)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t x = word(cur.k[0][j], i), y = word(cur.k[1][j], i);
+          for (int n = 0; n < NT; ++n) {
+            const uint4* p = reinterpret_cast<const uint4*>(
+                q_s + (z * COLS + 8 * n + gid) * S::kQRow + 64 * j + 16 * tig);
+            const uint4 x = p[0], y = p[1];
+            qv[z][n][0] = x.x; qv[z][n][1] = x.y; qv[z][n][2] = x.z; qv[z][n][3] = x.w;
+            qv[z][n][4] = y.x; qv[z][n][5] = y.y; qv[z][n][6] = y.z; qv[z][n][7] = y.w;
+          }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const uint4 k0 = stage[b * kUnits + j * 32], k1 = stage[b * kUnits + (D / 64 + j) * 32];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t x = word(k0, w), y = word(k1, w);
             const uint32_t a0 = codes2<FMT, 0>(x), a2 = codes2<FMT, 1>(x);
             const uint32_t a1 = codes2<FMT, 0>(y), a3 = codes2<FMT, 1>(y);
 #pragma unroll
             for (int z = 0; z < (SPLIT ? 2 : 1); ++z)
 #pragma unroll
-              for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qv[z][n][2 * i], qv[z][n][2 * i + 1]);
+              for (int n = 0; n < NT; ++n) mma_f16(s[b][n], a0, a1, a2, a3, qv[z][n][2 * w], qv[z][n][2 * w + 1]);
           }
         }
-        // scores in units of log2, masked; the block's maxima
-        const bool whole = tok >= every_b && tok + kCacheBlock <= every_e;
-        float top[NT][2];
-        bool grew = false;
+      }
+      // scores in units of log2, masked (a block that no query sees: all of it); their maxima
+      const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e && (live & ((1u << NB) - 1)) == (1u << NB) - 1;
+      float top[NT][2];
+      bool grew = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float v = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const float g = f[n][e] * sk[b];
+            s[b][n][e] *= g;
+            s[b][n][e + 2] *= g;
+            if (!whole) {
+              const int t0 = tok + b * kCacheBlock + gid;
+              const bool in = live >> b & 1;
+              if (!in || t0 < kb[n][e] || t0 >= ke[n][e]) s[b][n][e] = -INFINITY;
+              if (!in || t0 + 8 < kb[n][e] || t0 + 8 >= ke[n][e]) s[b][n][e + 2] = -INFINITY;
+            }
+            v = fmaxf(v, fmaxf(s[b][n][e], s[b][n][e + 2]));
+          }
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+          top[n][e] = v;
+          grew = grew || v > m[n][e];
+        }
+      float sv_top = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        if (live >> b & 1) sv_top = fmaxf(sv_top, sv[b]);
+      if (sv_top > ref || __any_sync(0xffffffffu, grew)) {
+        float r = 1.f;
+        if (sv_top > ref) {
+          // the power of two at or above, within 2^-110 .. 2^127 (its reciprocal times kWeight is finite)
+          const float up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u,
+                                                     0x7f000000u)), 7.7037197775489434e-34f);
+          r = ref / up;
+          ref = up;
+          inv_ref = 1.f / up * kWeight;
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float g = f[n][e] * sk;
-            s[n][e] *= g;
-            s[n][e + 2] *= g;
-            if (!whole) {
-              const int t0 = tok + gid;
-              if (t0 < kb[n][e] || t0 >= ke[n][e]) s[n][e] = -INFINITY;
-              if (t0 + 8 < kb[n][e] || t0 + 8 >= ke[n][e]) s[n][e + 2] = -INFINITY;
+            const float mn = fmaxf(m[n][e], top[n][e]);
+            const float fac = m[n][e] == mn ? 1.f : pow2(m[n][e] - mn);
+            m[n][e] = mn;
+            l[n][e] *= fac;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+              o[d][n][e] *= fac * r;
+              o[d][n][e + 2] *= fac * r;
             }
-            float v = fmaxf(s[n][e], s[n][e + 2]);
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-            top[n][e] = v;
-            grew = grew || v > m[n][e];
           }
-        if (sv > ref || __any_sync(0xffffffffu, grew)) {
-          const float old = ref;
-          if (sv > ref) ref = __uint_as_float((__float_as_uint(sv) + 0x7fffffu) & 0x7f800000u);
-          const float r = old == ref ? 1.f : old / ref;
+      }
+      uint32_t pb[NB][2][NT][2];
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        const float m0 = m[n][0] == -INFINITY ? 0.f : m[n][0], m1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float mn = fmaxf(m[n][e], top[n][e]);
-              const float fac = m[n][e] == mn ? 1.f : exp2f(m[n][e] - mn);
-              m[n][e] = mn;
-              l[n][e] *= fac;
-#pragma unroll
-              for (int i = 0; i < D / 16; ++i) {
-                o[i][n][e] *= fac * r;
-                o[i][n][e + 2] *= fac * r;
-              }
-            }
+        for (int b = 0; b < NB; ++b) {
+          const float wv = sv[b] * inv_ref;
+          float p0 = pow2(s[b][n][0] - m0), p1 = pow2(s[b][n][1] - m1);
+          float p2 = pow2(s[b][n][2] - m0), p3 = pow2(s[b][n][3] - m1);
+          l[n][0] += p0 + p2;
+          l[n][1] += p1 + p3;
+          p0 *= wv; p1 *= wv; p2 *= wv; p3 *= wv;
+          const uint32_t h0 = half2_bits(p0, p1), h1 = half2_bits(p2, p3);
+          pb[b][0][n][0] = transpose8(h0);
+          pb[b][0][n][1] = transpose8(h1);
+          pb[b][1][n][0] = transpose8(half2_rest(p0, p1, h0));
+          pb[b][1][n][1] = transpose8(half2_rest(p2, p3, h1));
         }
-        const float wv = ref > 0.f ? sv / ref * kWeight : 0.f;
-        uint32_t pb[SPLIT ? 2 : 1][NT][2];
+      }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float p[4];
+      for (int b = 0; b < NB; ++b) {
+        if (!(live >> b & 1)) continue;  // (its place in shared memory holds anything)
+        const int t0 = tok + b * kCacheBlock;
+        const uint4* stage_v = stage + b * kUnits + Pieces<D>::kKeys * 32;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float mm = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1];
-            p[e] = exp2f(s[n][e] - mm);
+        for (int j = 0; j < (D == 64 ? 1 : D / 128); ++j) {
+          uint4 v[4];
+          if constexpr (D == 64) {
+            const uint4 x = stage_v[0], y = stage_v[32];
+            v[0] = make_uint4(x.x, x.y, 0, 0);
+            v[1] = make_uint4(x.z, x.w, 0, 0);
+            v[2] = make_uint4(y.x, y.y, 0, 0);
+            v[3] = make_uint4(y.z, y.w, 0, 0);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = stage_v[(k * (D / 128) + j) * 32];
           }
-          l[n][0] += p[0] + p[2];
-          l[n][1] += p[1] + p[3];
+          if (t0 + kCacheBlock > len) {  // places past the end hold anything: taken as codes of 0
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] *= wv;
-          const uint32_t h0 = half2_bits(p[0], p[1]), h1 = half2_bits(p[2], p[3]);
-          pb[0][n][0] = transpose8(h0);
-          pb[0][n][1] = transpose8(h1);
-          if constexpr (SPLIT) {
-            pb[1][n][0] = transpose8(half2_rest(p[0], p[1], h0));
-            pb[1][n][1] = transpose8(half2_rest(p[2], p[3], h1));
+            for (int k = 0; k < 4; ++k)
+              if (t0 + 2 * tig + (k & 1) + 8 * (k >> 1) >= len) v[k] = make_uint4(0, 0, 0, 0);
           }
-        }
-        if (tok + kCacheBlock > len) {  // places past the end hold anything: as codes of 0
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tok + 2 * tig + (i & 1) + 8 * (i >> 1) >= len)
-#pragma unroll
-              for (int j = 0; j < BlockRegs<D>::kPieces; ++j) cur.v[i][j] = make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < BlockRegs<D>::kPieces; ++j)
-#pragma unroll
-          for (int i = 0; i < (D == 64 ? 2 : 4); ++i) {
+          for (int w = 0; w < (D == 64 ? 2 : 4); ++w) {
             // tokens 2 tig, 2 tig + 1 side by side, channel by channel; then + 8, + 9
-            const uint32_t x0 = word(cur.v[0][j], i), x1 = word(cur.v[1][j], i);
-            const uint32_t y0 = word(cur.v[2][j], i), y1 = word(cur.v[3][j], i);
+            const uint32_t x0 = word(v[0], w), x1 = word(v[1], w);
+            const uint32_t y0 = word(v[2], w), y1 = word(v[3], w);
             const uint32_t xl = __byte_perm(x0, x1, 0x5140), xh = __byte_perm(x0, x1, 0x7362);
             const uint32_t yl = __byte_perm(y0, y1, 0x5140), yh = __byte_perm(y0, y1, 0x7362);
             const uint32_t a0 = codes2<FMT, 0>(xl), a1 = codes2<FMT, 1>(xl);
             const uint32_t a2 = codes2<FMT, 0>(yl), a3 = codes2<FMT, 1>(yl);
             const uint32_t c0 = codes2<FMT, 0>(xh), c1 = codes2<FMT, 1>(xh);
             const uint32_t c2 = codes2<FMT, 0>(yh), c3 = codes2<FMT, 1>(yh);
-            const int mt = 8 * j + 2 * i;
+            const int mt = 8 * j + 2 * w;
 #pragma unroll
-            for (int z = 0; z < (SPLIT ? 2 : 1); ++z)
+            for (int z = 0; z < 2; ++z)
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                mma_f16(o[mt][n], a0, a1, a2, a3, pb[z][n][0], pb[z][n][1]);
-                mma_f16(o[mt + 1][n], c0, c1, c2, c3, pb[z][n][0], pb[z][n][1]);
+                mma_f16(o[mt][n], a0, a1, a2, a3, pb[b][z][n][0], pb[b][z][n][1]);
+                mma_f16(o[mt + 1][n], c0, c1, c2, c3, pb[b][z][n][0], pb[b][z][n][1]);
               }
           }
+        }
       }
-      cur = nxt;
-      at = at_n;
-      sk = sk_n;
-      sv = sv_n;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();  // every lane has read its pieces: the ring takes the outputs
+    float* o_s = reinterpret_cast<float*>(mine);
 
     // join the warps
 #pragma unroll
@@ -483,7 +571,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
           l_s[warp * COLS + col] = v;
           r_s[warp * COLS + col] = ref;
         }
-        float* row = o_s + ((size_t)warp * COLS + col) * D;
+        float* row = o_s + col * D;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           // m-tile i: channels 2 i and 2 i + 1 of the lane's piece
@@ -502,7 +590,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
       float fac[kWarps];
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
-        const float x = exp2f(m_s[i * COLS + col] - mm);
+        const float x = pow2(m_s[i * COLS + col] - mm);
         L += l_s[i * COLS + col] * x;
         fac[i] = x * r_s[i * COLS + col] * (1.f / kWeight);
       }
@@ -513,7 +601,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         const int d = lane + 32 * e;
         float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) v += o_s[((size_t)i * COLS + col) * D + d] * fac[i];
+        for (int i = 0; i < kWarps; ++i) v += reinterpret_cast<const float*>(ring + i * S::kRing)[col * D + d] * fac[i];
         if (complete)
           store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + d, a.o.type, v * inv);
         else
@@ -533,47 +621,62 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
 }
 
 // Joins the parts of the unit that the boundary between shares blockIdx.x and blockIdx.x + 1 cuts, if
-// it is the first that does; the parts are added in the order of the shares.
+// it is the first that does: a warp per column, the parts in the order of the shares.
 template <int D, int COLS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(32 * COLS)
 attend_join_kernel(const __grid_constant__ AttendArgs a) {
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t total = total_tiles<COLS>(a);
-  const int i0 = blockIdx.x;
-  const int64_t before = share_begin(total, i0, a.shares), cut = share_begin(total, i0 + 1, a.shares);
-  if (before == cut || cut >= total) return;
-  const Unit u = locate<COLS>(a, cut);
-  if (u.begin == cut || u.begin < before) return;
+  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5;
+  const int64_t total = total_tiles<D, COLS>(a);
+  const int shares = (int)min((int64_t)a.shares, total), i0 = blockIdx.x;
+  if (i0 + 1 >= shares) return;
+  const int64_t cut = share_begin(total, i0 + 1, shares);
+  const Unit u = locate<D, COLS>(a, cut);
+  if (u.begin == cut || u.begin < share_begin(total, i0, shares)) return;
   const int64_t end = u.begin + u.s.tiles;
   constexpr int kSlot = COLS * (D + 2);
-  const int col0 = u.cg * COLS, n_cols = min(COLS, u.s.n * a.group - col0);
-  for (int col = warp; col < n_cols; col += kWarps) {
-    float M = -INFINITY, L = 0.f, o[D / 32];
+  const int col0 = u.cg * COLS;
+  if (col0 + col >= u.s.n * a.group) return;
+  int n = 1;  // shares that hold a part
+  while (i0 + n < shares && share_begin(total, i0 + n, shares) < end) ++n;
+  // slot of part 0: the share's last unit; of the others: their first (the unit began before them)
+  const float* part = a.part + (int64_t)2 * i0 * kSlot;
+  float M = -INFINITY, L = 0.f, o[D / 32];
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-    for (int i = i0; i < a.shares; ++i) {
-      const int64_t b = share_begin(total, i, a.shares);
-      if (b >= end) break;
-      if (b == share_begin(total, i + 1, a.shares)) continue;
-      const float* part = a.part + (int64_t)(2 * i + (u.begin >= b ? 1 : 0)) * kSlot;
-      const float mi = part[COLS * D + col], li = part[COLS * D + COLS + col];
-      const float mn = fmaxf(M, mi), mm = mn == -INFINITY ? 0.f : mn;
-      const float fo = exp2f(M - mm), fi = exp2f(mi - mm);
-      L = L * fo + li * fi;
+  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+  for (int p0 = 0; p0 < n; p0 += 32) {
+    const int p = p0 + lane;
+    const float* pl = part + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * kSlot + COLS * D + col;
+    const float mp = p < n ? pl[0] : -INFINITY, lp = p < n ? pl[COLS] : 0.f;
+    float mn = fmaxf(M, mp);
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = o[e] * fo + part[col * D + lane + 32 * e] * fi;
-      M = mn;
+    for (int d = 16; d > 0; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+    const float mm = mn == -INFINITY ? 0.f : mn;
+    const float f = pow2(mp - mm), back = pow2(M - mm);
+    float sum = lp * f;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    L = L * back + sum;
+    M = mn;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) o[e] *= back;
+    const int k = min(32, n - p0);
+#pragma unroll 8
+    for (int q = 0; q < k; ++q) {
+      const float fq = __shfl_sync(0xffffffffu, f, q);
+      const float* src = part + (int64_t)(2 * (p0 + q) + (p0 + q == 0 ? 1 : 0)) * kSlot + col * D + lane;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] += src[32 * e] * fq;
     }
-    const int j = (col0 + col) / a.group, h = u.h * a.group + (col0 + col) % a.group;
-    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-      store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + lane + 32 * e, a.o.type, o[e] * inv);
-    if (lane == 0 && a.lse)
-      a.lse[(u.s.first + j) * a.q.heads + h] = L > 0.f ? (M + log2f(L)) / kLog2e : (L == 0.f ? -INFINITY : L);
   }
+  const int j = (col0 + col) / a.group, h = u.h * a.group + (col0 + col) % a.group;
+  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+    store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + lane + 32 * e, a.o.type, o[e] * inv);
+  if (lane == 0 && a.lse)
+    a.lse[(u.s.first + j) * a.q.heads + h] = L > 0.f ? (M + log2f(L)) / kLog2e : (L == 0.f ? -INFINITY : L);
 }
 
 template <int D, int NT, int FMT, bool SPLIT>
@@ -581,16 +684,14 @@ crvq_status launch_attend(AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT, FMT, SPLIT>;
   auto kernel = attend_kernel<D, NT, FMT, SPLIT>;
   CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
-  // CTAs that an SM holds, by registers: 16 warps of 128, fewer with wide accumulators
-  constexpr int kPerSm = D == 256 ? 2 : (NT == 1 ? 4 : 3);
-  a.shares = sm_count() * kPerSm;
+  a.shares = sm_count() * S::kPerSm;
   Scratch mem;
   CRVQ_TRY(mem.alloc((size_t)2 * a.shares * S::kSlot * sizeof(float), stream));
   a.part = mem.as<float>();
   ProfScope ps("cache_attention", stream, (double)a.rows.n_tok * a.q.heads * D);
   CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)a.shares), dim3(kThreads), S::kSmem, stream, a));
   CRVQ_LAUNCHED();
-  CRVQ_CUDA(launch_pdl(attend_join_kernel<D, S::kCols>, dim3((unsigned)a.shares - 1), dim3(kThreads), 0, stream, a));
+  CRVQ_CUDA(launch_pdl(attend_join_kernel<D, S::kCols>, dim3((unsigned)a.shares - 1), dim3(32 * S::kCols), 0, stream, a));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }

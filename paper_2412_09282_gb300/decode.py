@@ -12,10 +12,21 @@ import math
 import torch
 
 from . import _lib
-from .api import _check, _L, _ptr, _stream
+from .api import _check, _L
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+_addressof, _empty = C.addressof, torch.empty
+# (a step's calls are short: the stream's handle without the Stream object around it, 2 us less)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _foreign(stream, *outputs):
+    """The handle of a stream given by the caller, on which the outputs are then in use."""
+    for t in outputs:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
 
 
 def _device(t, dtype, name):
@@ -26,20 +37,21 @@ def _device(t, dtype, name):
 
 
 def _type(t, name):
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}") from None
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    return code
 
 
 def _heads(t, name, head_dim):
     """crvq_heads of a tokens x heads x head_dim view with unit stride in the last dimension."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[2] != head_dim or stride[2] != 1:
+    code = _type(t, name)
+    stride = t.stride()
+    if len(stride) != 3 or stride[2] != 1 or t.shape[2] != head_dim:
         raise ValueError(f"{name} must be tokens x heads x {head_dim} with unit stride in the last dimension")
-    return _lib.crvq_heads(t.data_ptr(), stride[0], stride[1], shape[1], _type(t, name))
+    return _lib.crvq_heads(t.data_ptr(), stride[0], stride[1], t.shape[1], code)
 
 
 def _offsets(off, n_seq, name):
@@ -59,7 +71,7 @@ class KVCache:
     change from call to call; for other tensors make another handle."""
 
     __slots__ = ("K", "V", "k_scale", "v_scale", "pages", "lens", "_c", "_addr", "n_seq", "n_kv", "head_dim",
-                 "page", "device")
+                 "page", "device", "index")
 
     def __init__(self, K, V, k_scale, v_scale, pages, lens):
         if K.dtype not in _FORMATS:
@@ -88,18 +100,18 @@ class KVCache:
         ld = pages.stride(0) if pages.shape[0] > 1 else pages.shape[1]
         self.K, self.V, self.k_scale, self.v_scale, self.pages, self.lens = K, V, k_scale, v_scale, pages, lens
         self.n_seq, self.n_kv, self.page, self.head_dim = pages.shape[0], n_kv, page, d
-        self.device = K.device
+        self.device, self.index = K.device, K.get_device()
         self._c = _lib.crvq_kv_cache(K.data_ptr(), V.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                      pages.data_ptr(), lens.data_ptr(), n_pages, stride, ld, pages.shape[0],
                                      pages.shape[1], page, n_kv, d, _FORMATS[K.dtype])
-        self._addr = C.addressof(self._c)
+        self._addr = _addressof(self._c)
 
     @staticmethod
     def empty(n_pages, n_kv, page, head_dim, pages, lens, dtype=torch.int8):
         """A cache over a new pool of pages (its codes are whatever the memory holds)."""
         dev = pages.device
-        K = torch.empty((n_pages, n_kv, page, head_dim), device=dev, dtype=dtype)
-        s = torch.empty((n_pages, n_kv, page // 16), device=dev, dtype=torch.float32)
+        K = _empty((n_pages, n_kv, page, head_dim), device=dev, dtype=dtype)
+        s = _empty((n_pages, n_kv, page // 16), device=dev, dtype=torch.float32)
         return KVCache(K, torch.empty_like(K), s, torch.empty_like(s), pages, lens)
 
 
@@ -123,23 +135,24 @@ def crvq_cache_append(cache, k, v, new_off=None, cos=None, sin=None, positions=N
             _device(positions, torch.int32, "positions")
             if positions.shape != (n_tok,) or not positions.is_contiguous():
                 raise ValueError("positions must be contiguous with one entry per token")
-        rot = _lib.crvq_rotary(cos.data_ptr(), sin.data_ptr(), _ptr(positions), cos.shape[0],
+        rot = _lib.crvq_rotary(cos.data_ptr(), sin.data_ptr(), None if positions is None else positions.data_ptr(), cos.shape[0],
                                max(cos.stride(0), cos.shape[1]), cos.shape[1], int(bool(interleaved)))
     qc = oc = None
     if q is not None:
         if q.shape[0] != n_tok:
             raise ValueError("q and k differ in tokens")
         if q_out is None:
-            q_out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
+            q_out = _empty(q.shape, device=q.device, dtype=q.dtype)
         elif q_out.shape != q.shape:
             raise ValueError("q_out must have the shape of q")
         qc, oc = _heads(q, "q", d), _heads(q_out, "q_out", d)
-    _check(_L().crvq_cache_append(cache._addr, C.addressof(kc), C.addressof(vc), n_tok,
-                                  _offsets(new_off, cache.n_seq, "new_off"),
-                                  C.addressof(rot) if rot is not None else None,
-                                  C.addressof(qc) if qc is not None else None,
-                                  C.addressof(oc) if oc is not None else None,
-                                  _stream(stream, cache.device)))
+    st = _L().crvq_cache_append(cache._addr, _addressof(kc), _addressof(vc), n_tok,
+                                _offsets(new_off, cache.n_seq, "new_off"),
+                                None if rot is None else _addressof(rot), None if qc is None else _addressof(qc),
+                                None if oc is None else _addressof(oc),
+                                _raw_stream(cache.index) if stream is None else _foreign(stream, q_out))
+    if st:
+        _check(st)
     return q_out
 
 
@@ -150,17 +163,19 @@ def crvq_cache_read(cache, start, off, n_tok, dtype=torch.float32, K_out=None, V
     _device(start, torch.int32, "start")
     if start.shape != (cache.n_seq,) or not start.is_contiguous():
         raise ValueError("start must be contiguous with one entry per sequence")
-    outs = []
-    for name, t in (("K_out", K_out), ("V_out", V_out)):
-        if t is None:
-            t = torch.empty(shape, device=cache.device, dtype=dtype)
-        elif t.shape != shape or not t.is_contiguous() or t.dtype != dtype:
-            raise ValueError(f"{name} must be contiguous n_tok x n_kv x head_dim of {dtype}")
-        outs.append(t)
-    K_out, V_out = outs
-    _check(_L().crvq_cache_read(cache._addr, start.data_ptr(), _offsets(off, cache.n_seq, "off"), n_tok,
-                                _type(K_out, "K_out"), K_out.data_ptr(), V_out.data_ptr(),
-                                _stream(stream, cache.device)))
+    if K_out is None:
+        K_out = _empty(shape, device=cache.device, dtype=dtype)
+    elif K_out.shape != shape or not K_out.is_contiguous() or K_out.dtype != dtype:
+        raise ValueError(f"K_out must be contiguous n_tok x n_kv x head_dim of {dtype}")
+    if V_out is None:
+        V_out = _empty(shape, device=cache.device, dtype=dtype)
+    elif V_out.shape != shape or not V_out.is_contiguous() or V_out.dtype != dtype:
+        raise ValueError(f"V_out must be contiguous n_tok x n_kv x head_dim of {dtype}")
+    st = _L().crvq_cache_read(cache._addr, start.data_ptr(), _offsets(off, cache.n_seq, "off"), n_tok,
+                              _type(K_out, "K_out"), K_out.data_ptr(), V_out.data_ptr(),
+                              _raw_stream(cache.index) if stream is None else _foreign(stream, K_out, V_out))
+    if st:
+        _check(st)
     return K_out, V_out
 
 
@@ -171,15 +186,17 @@ def crvq_cache_attention(cache, q, q_off=None, scale=None, causal=True, window=0
     d = cache.head_dim
     qc = _heads(q, "q", d)
     if out is None:
-        out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
+        out = _empty(q.shape, device=q.device, dtype=q.dtype)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
     oc = _heads(out, "out", d)
-    lse = torch.empty(q.shape[:2], device=q.device, dtype=torch.float32) if want_lse else None
-    _check(_L().crvq_cache_attention(cache._addr, C.addressof(qc), q.shape[0],
-                                     _offsets(q_off, cache.n_seq, "q_off"),
-                                     1.0 / math.sqrt(d) if scale is None else scale, int(bool(causal)), window,
-                                     C.addressof(oc), _ptr(lse), _stream(stream, cache.device)))
+    lse = _empty(q.shape[:2], device=q.device, dtype=torch.float32) if want_lse else None
+    st = _L().crvq_cache_attention(cache._addr, _addressof(qc), q.shape[0], _offsets(q_off, cache.n_seq, "q_off"),
+                                   1.0 / math.sqrt(d) if scale is None else scale, causal, window,
+                                   _addressof(oc), None if lse is None else lse.data_ptr(),
+                                   _raw_stream(cache.index) if stream is None else _foreign(stream, out, lse))
+    if st:
+        _check(st)
     return (out, lse) if want_lse else out
 
 
@@ -188,7 +205,7 @@ class Q4Matrix:
     column in the low bits), scales [M x ceil(N / group)] bfloat16, zeros of that shape, uint8, or None (8).
     Rows that begin on 16-byte boundaries are read fastest."""
 
-    __slots__ = ("codes", "scales", "zeros", "M", "N", "group", "_c", "_addr", "device")
+    __slots__ = ("codes", "scales", "zeros", "M", "N", "group", "_c", "_addr", "device", "index")
 
     def __init__(self, codes, scales, zeros, N, group):
         _device(codes, torch.uint8, "codes")
@@ -202,52 +219,68 @@ class Q4Matrix:
             _device(zeros, torch.uint8, "zeros")
             if zeros.shape != scales.shape or zeros.stride() != scales.stride():
                 raise ValueError("zeros must have the shape and strides of scales")
+        self._set(codes, scales, zeros, M, N, group, codes.stride(0) if M > 1 else max(half, codes.stride(0)),
+                  scales.stride(0) if M > 1 else G)
+
+    def _set(self, codes, scales, zeros, M, N, group, ld_codes, ld_scales):
         self.codes, self.scales, self.zeros = codes, scales, zeros
-        self.M, self.N, self.group, self.device = M, N, group, codes.device
-        self._c = _lib.crvq_q4_matrix(codes.data_ptr(), scales.data_ptr(), _ptr(zeros), M, N,
-                                      codes.stride(0) if M > 1 else max(half, codes.stride(0)),
-                                      scales.stride(0) if M > 1 else G, group, 0)
-        self._addr = C.addressof(self._c)
+        self.M, self.N, self.group, self.device, self.index = M, N, group, codes.device, codes.get_device()
+        self._c = _lib.crvq_q4_matrix(codes.data_ptr(), scales.data_ptr(),
+                                      None if zeros is None else zeros.data_ptr(), M, N, ld_codes, ld_scales,
+                                      group, 0)
+        self._addr = _addressof(self._c)
 
     @staticmethod
     def empty(M, N, group, zeros=False, device="cuda"):
-        row = -(-((N + 1) // 2) // 16) * 16
-        codes = torch.empty((M, row), device=device, dtype=torch.uint8)[:, :(N + 1) // 2]
-        scales = torch.empty((M, -(-N // group)), device=device, dtype=torch.bfloat16)
-        z = torch.empty(scales.shape, device=device, dtype=torch.uint8) if zeros else None
-        return Q4Matrix(codes, scales, z, N, group)
+        """Memory for an M x N matrix, rows on 16-byte boundaries."""
+        half, G = (N + 1) // 2, -(-N // group)
+        row = (half + 15) // 16 * 16
+        codes = torch.empty_strided((M, half), (row, 1), device=device, dtype=torch.uint8)
+        scales = _empty((M, G), device=device, dtype=torch.bfloat16)
+        m = Q4Matrix.__new__(Q4Matrix)
+        m._set(codes, scales, _empty((M, G), device=device, dtype=torch.uint8) if zeros else None, M, N, group, row, G)
+        return m
 
 
 def crvq_q4_quantize(W, group=128, symmetric=True, want_W_hat=False, out=None, stream=None):
     """W (M x N, unit column stride) in 4 bits by rounding, with a zero point per group unless symmetric:
     returns (Q4Matrix, W_hat fp32 or None)."""
     t = _type(W, "W")
-    _device(W, None, "W")
-    if W.dim() != 2 or W.stride(1) != 1:
+    shape, stride = W.shape, W.stride()
+    if len(shape) != 2 or stride[1] != 1:
         raise ValueError("W must be a 2-D tensor with unit column stride")
-    M, N = W.shape
+    M, N = shape
     if out is None:
         out = Q4Matrix.empty(M, N, group, zeros=not symmetric, device=W.device)
     elif (out.M, out.N, out.group, out.zeros is None) != (M, N, group, bool(symmetric)):
         raise ValueError("out is for another matrix")
-    W_hat = torch.empty((M, N), device=W.device, dtype=torch.float32) if want_W_hat else None
-    _check(_L().crvq_q4_quantize(W.data_ptr(), W.stride(0) if M > 1 else N, t, out._addr, _ptr(W_hat),
-                                 _stream(stream, W.device)))
+    W_hat = _empty((M, N), device=W.device, dtype=torch.float32) if want_W_hat else None
+    st = _L().crvq_q4_quantize(W.data_ptr(), stride[0] if M > 1 else N, t, out._addr,
+                               None if W_hat is None else W_hat.data_ptr(),
+                               _raw_stream(out.index) if stream is None else _foreign(stream, W_hat, out.codes,
+                                                                                      out.scales, out.zeros))
+    if st:
+        _check(st)
     return out, W_hat
 
 
 def crvq_q4_matvec(X, matrix, Y=None, stream=None):
     """Y = X W^T (b x M, of X's type) for 1 to 32 inputs X (b x N; a 1-D input is one row)."""
     t = _type(X, "X")
-    _device(X, None, "X")
-    X2 = X.unsqueeze(0) if X.dim() == 1 else X
-    if X2.dim() != 2 or X2.stride(1) != 1 or X2.shape[1] != matrix.N:
+    if X.dim() == 1:
+        X = X.unsqueeze(0)
+    shape, stride, M = X.shape, X.stride(), matrix.M
+    if len(shape) != 2 or stride[1] != 1 or shape[1] != matrix.N:
         raise ValueError(f"X must be b x {matrix.N} with unit column stride")
-    b = X2.shape[0]
+    b = shape[0]
     if Y is None:
-        Y = torch.empty((b, matrix.M), device=X.device, dtype=X.dtype)
-    elif Y.shape != (b, matrix.M) or Y.dtype != X.dtype or Y.stride(1) != 1:
-        raise ValueError("Y must be b x M of X's type with unit column stride")
-    _check(_L().crvq_q4_matvec(matrix._addr, X2.data_ptr(), X2.stride(0) if b > 1 else matrix.N, b, t,
-                               Y.data_ptr(), Y.stride(0) if b > 1 else matrix.M, _stream(stream, X.device)))
+        Y, ldy = _empty((b, M), device=matrix.device, dtype=X.dtype), M
+    else:
+        if Y.shape != (b, M) or Y.dtype != X.dtype or Y.stride(1) != 1:
+            raise ValueError("Y must be b x M of X's type with unit column stride")
+        ldy = Y.stride(0) if b > 1 else M
+    st = _L().crvq_q4_matvec(matrix._addr, X.data_ptr(), stride[0] if b > 1 else shape[1], b, t, Y.data_ptr(), ldy,
+                             _raw_stream(matrix.index) if stream is None else _foreign(stream, Y))
+    if st:
+        _check(st)
     return Y
