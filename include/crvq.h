@@ -591,8 +591,10 @@ crvq_status crvq_q4_quantize(const void* W, int64_t ldw, int32_t type, const crv
 
 /*
  * Y = X W^T for b inputs (X b x N, Y b x M, both of `type`, row strides ldx and ldy). Codes minus
- * zero points are exact operands of the tensor cores, X one operand of its own type or, from fp32,
- * three bf16 ones (24 bits); sums are fp32 in a fixed order, each group's scaled once.
+ * zero points are exact fp16 operands of the tensor cores; fp16 inputs go as they are, others relative
+ * to a power of two per group and input in one fp16 operand (bf16: exact but for elements below 2^-14 of
+ * the group's largest) or two (fp32: to 2^-22 of an element or 2^-25 of the group's largest). Sums are
+ * fp32 in a fixed order, each group's scaled once.
  * Requires 1 <= b <= 32.
  */
 crvq_status crvq_q4_matvec(const crvq_q4_matrix* m, const void* X, int64_t ldx, int64_t b,

@@ -58,6 +58,10 @@ struct AttendArgs {
   unsigned* err;
 };
 
+// What a unit costs beside its tiles (its start, and joining its warps), in tiles: the first kStart places
+// of a unit on the line hold no tile.
+constexpr int kStart = 3;
+
 // A sequence's work.
 struct Seq {
   int len, n;       // tokens in the cache, queries
@@ -81,65 +85,106 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b) {
 struct Unit {
   Seq s;
   int b, h, cg;
-  int tile;         // of the position that was looked for
-  int64_t begin;    // the unit's first tile in the line
+  int tile;         // at the place that was looked for (0 before the first tile)
+  int64_t begin;    // the unit's first place on the line; its tiles begin kStart later
 };
 
-// Tiles of all units (warp-wide).
-template <int D, int COLS>
-__device__ int64_t total_tiles(const AttendArgs& a) {
-  const int lane = threadIdx.x & 31;
-  int64_t sum = 0;
-  for (int b = lane; b < a.c.n_seq; b += 32) {
-    const Seq s = load_seq<D, COLS>(a, b);
-    sum += (int64_t)s.groups * s.tiles;
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  return sum * a.c.n_kv;
-}
-
-// The unit that holds position w of the line, 0 <= w < total (warp-wide).
-template <int D, int COLS>
-__device__ Unit locate(const AttendArgs& a, int64_t w) {
-  const int lane = threadIdx.x & 31;
-  int64_t base = 0;
-  Unit u;
-  u.b = 0;
-  for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
-    int64_t cost = 0;
-    if (b0 + lane < a.c.n_seq) {
-      const Seq s = load_seq<D, COLS>(a, b0 + lane);
-      cost = (int64_t)s.groups * s.tiles * a.c.n_kv;
-    }
-    int64_t incl = cost;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += v;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, base + incl > w);
-    if (hit) {
-      const int src = __ffs(hit) - 1;
-      base += __shfl_sync(0xffffffffu, incl - cost, src);
-      u.b = b0 + src;
-      break;
-    }
-    base += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  u.s = load_seq<D, COLS>(a, u.b);
-  const int64_t rem = w - base;
-  const int64_t idx = rem / u.s.tiles;
-  u.tile = (int)(rem - idx * u.s.tiles);
-  u.h = (int)(idx / u.s.groups);
-  u.cg = (int)(idx - (int64_t)u.h * u.s.groups);
-  u.begin = w - u.tile;
-  return u;
+__device__ __forceinline__ int64_t divide(int64_t x, int y) {  // x >= 0, y > 0
+  return x >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
 }
 
 __device__ __forceinline__ int64_t share_begin(int64_t total, int i, int shares) {
-  return total * i / shares;
+  return divide(total * i, shares);
 }
+
+// The line of all units' tiles, warp-wide: every lane holds a sequence's end of the first 32.
+template <int D, int COLS>
+struct Line {
+  int64_t cost, end;  // of sequence `lane`
+  int64_t total;
+
+  static __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b) {
+    if (b >= a.c.n_seq) return 0;
+    const Seq s = load_seq<D, COLS>(a, b);
+    return (int64_t)s.groups * (s.tiles + kStart) * a.c.n_kv;
+  }
+  static __device__ __forceinline__ int64_t scan(int64_t v) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, v, d);
+      if ((int)(threadIdx.x & 31) >= d) v += x;
+    }
+    return v;
+  }
+  __device__ explicit Line(const AttendArgs& a) {
+    const int lane = threadIdx.x & 31;
+    cost = cost_of(a, lane);
+    end = scan(cost);
+    int64_t more = 0;
+    for (int b = 32 + lane; b < a.c.n_seq; b += 32) more += cost_of(a, b);
+    total = __shfl_sync(0xffffffffu, end, 31);
+    if (a.c.n_seq > 32) total += __shfl_sync(0xffffffffu, scan(more), 31);
+  }
+  // Unit number i (sequence by sequence, head by head); false past the last.
+  __device__ bool unit(const AttendArgs& a, int64_t i, Unit* u) const {
+    const int lane = threadIdx.x & 31;
+    int64_t base = 0;
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
+      int64_t units = 0, places = 0;
+      if (b0 + lane < a.c.n_seq) {
+        const Seq s = load_seq<D, COLS>(a, b0 + lane);
+        units = (int64_t)s.groups * a.c.n_kv;
+        places = units * (s.tiles + kStart);
+      }
+      const int64_t e = scan(units), pe = scan(places);
+      const unsigned hit = __ballot_sync(0xffffffffu, e > i);
+      if (hit) {
+        const int src = __ffs(hit) - 1;
+        i -= __shfl_sync(0xffffffffu, e - units, src);
+        u->b = b0 + src;
+        u->s = load_seq<D, COLS>(a, u->b);
+        u->begin = base + __shfl_sync(0xffffffffu, pe - places, src) + i * (u->s.tiles + kStart);
+        u->h = (int)divide(i, u->s.groups);
+        u->cg = (int)(i - (int64_t)u->h * u->s.groups);
+        u->tile = 0;
+        return true;
+      }
+      i -= __shfl_sync(0xffffffffu, e, 31);
+      base += __shfl_sync(0xffffffffu, pe, 31);
+    }
+    return false;
+  }
+  // The unit that holds position w, 0 <= w < total.
+  __device__ Unit locate(const AttendArgs& a, int64_t w) const {
+    const int lane = threadIdx.x & 31;
+    int64_t base = 0, c = cost, e = end;
+    Unit u;
+    u.b = 0;
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
+      if (b0) {
+        c = cost_of(a, b0 + lane);
+        e = scan(c);
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, base + e > w);
+      if (hit) {
+        const int src = __ffs(hit) - 1;
+        base += __shfl_sync(0xffffffffu, e - c, src);
+        u.b = b0 + src;
+        break;
+      }
+      base += __shfl_sync(0xffffffffu, e, 31);
+    }
+    u.s = load_seq<D, COLS>(a, u.b);
+    const int places = u.s.tiles + kStart;
+    const int64_t rem = w - base, idx = divide(rem, places);
+    const int at = (int)(rem - idx * places);
+    u.tile = max(0, at - kStart);
+    u.h = (int)divide(idx, u.s.groups);
+    u.cg = (int)(idx - (int64_t)u.h * u.s.groups);
+    u.begin = w - at;
+    return u;
+  }
+};
 
 __device__ __forceinline__ void mma_f16(float d[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                         uint32_t b0, uint32_t b1) {
@@ -185,45 +230,44 @@ __device__ __forceinline__ int word(const uint4& u, int i) {
   return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
 }
 
-// The pieces of one block that a lane needs: K rows key_row and key_row + 8 (16 codes from every 64), V rows
-// 2 tig, 2 tig + 1, + 8, + 9 (16 codes, 8 of 64). Every lane copies its own pieces to shared memory,
-// piece by piece with the lanes side by side: no bank conflicts, and no lane waits for another's copy.
+// A block's 16 rows of keys or values in shared memory: lines of eight 16-byte units, whose places are
+// exchanged within the line (by `turn` of the line) so that both readers are free of bank conflicts: keys
+// (eight lanes: two rows, four neighbouring units each) and values (eight lanes: every other row of
+// eight, two neighbouring units each; for 64 channels 16 lanes of half units).
 template <int D>
-struct Pieces {
-  static constexpr int kChunks = D / 64;                  // 16-byte pieces of a key row
-  static constexpr int kKeys = 2 * kChunks;
-  static constexpr int kValues = D == 64 ? 2 : D / 32;    // 16-byte units: D = 64 has two 8-byte pieces in one
-  static constexpr int kBytes = (kKeys + kValues) * 512;  // of a warp and block
+struct Tile {
+  static constexpr int kBytes = kCacheBlock * D;
+  static __device__ __forceinline__ uint32_t turn(int line) {
+    if constexpr (D == 64) return 2 * (line & 3);  // two rows in a line
+    const int r = D == 128 ? line : line >> 1;
+    return (r & 6) ^ ((r & 1) << 2);
+  }
+  // Byte offset of 16-byte unit c of row r.
+  static __device__ __forceinline__ uint32_t at(int r, int c) {
+    const int u = r * (D / 16) + c, line = u >> 3;
+    return (uint32_t)(line * 8 + ((u & 7) ^ turn(line))) * 16;
+  }
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// Asynchronous copies; PART: of the first n bytes, zeros for the rest.
+template <bool PART>
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int n) {
+  if constexpr (PART)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
-}
-
-// Starts the copies of the block whose codes begin at byte `at` of K and V; dst: this warp's stage.
-template <int D>
-__device__ __forceinline__ void start_block(const CacheView& c, int64_t at, uint32_t dst) {
-  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  const uint8_t* k = c.K + at + gid * D + 16 * tig;
-  dst += lane * 16;
+// Starts the copies of a block from src to its tile at dst, a warp's 32 lanes 512 consecutive bytes at a
+// time (lanes that copied just the pieces that they read, 8 rows of 64 bytes, got 5.2 TB/s instead of 7.0).
+// n: rows that there are (PART); the others are set to 0 (a page holds anything there).
+template <int D, bool PART>
+__device__ __forceinline__ void start_block(const uint8_t* src, uint32_t dst, int n) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < Pieces<D>::kChunks; ++j) copy16(dst + (i * Pieces<D>::kChunks + j) * 512, k + 8 * i * D + 64 * j);
-  dst += Pieces<D>::kKeys * 512;
-  const uint8_t* v = c.V + at + 2 * tig * D + (D == 64 ? 8 : 16) * gid;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint8_t* row = v + ((i & 1) + 8 * (i >> 1)) * D;
-    if constexpr (D == 64) {
-      copy8(dst + (i >> 1) * 512 + (i & 1) * 8, row);
-    } else {
-#pragma unroll
-      for (int j = 0; j < D / 128; ++j) copy16(dst + (i * (D / 128) + j) * 512, row + 128 * j);
-    }
+  for (int j = 0; j < Tile<D>::kBytes / 512; ++j) {
+    const int u = 32 * j + lane, line = u >> 3;
+    const bool in = !PART || u < n * (D / 16);
+    copy16<PART>(dst + (line * 8 + ((u & 7) ^ Tile<D>::turn(line))) * 16, src + (in ? u * 16 : 0), in ? 16 : 0);
   }
 }
 
@@ -232,9 +276,10 @@ struct Shape {
   static constexpr int kCols = 8 * NT;
   static constexpr int kQRow = D + 8;  // halves per query row, padded against bank conflicts
   static constexpr size_t kQ = (size_t)kCols * kQRow * 2 * (SPLIT ? 2 : 1);
-  // the ring of blocks on their way; at a unit's end each warp's outputs [kCols][D] lie in its own part
-  static constexpr int kStages = D == 128 ? 2 : 3;
-  static constexpr int kRing = Pieces<D>::kBytes * kBlocks<D> * kStages;
+  // keys and values on their way and in work; at a unit's end each warp's outputs [kCols][D] lie in its part
+  static constexpr int kStages = 2;
+  static constexpr int kHalf = Tile<D>::kBytes * kBlocks<D> * kStages;
+  static constexpr int kRing = 2 * kHalf;
   static_assert(kRing >= kCols * D * 4, "outputs fit the ring");
   static constexpr size_t kSmem = kQ + (size_t)kWarps * kRing + 3 * kCols * 4 + 3 * kWarps * kCols * 4;
   // CTAs per SM, by registers (128 threads of 128 or 168) and shared memory
@@ -249,7 +294,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int COLS = S::kCols;
   extern __shared__ __align__(16) char sm[];
   __half* q_s = reinterpret_cast<__half*>(sm);                       // [split][COLS][kQRow]
-  char* ring = sm + S::kQ;                                           // [kWarps][kStages][pieces][lane]
+  char* ring = sm + S::kQ;                                           // [kWarps][keys, values][kStages][blocks] tiles
   float* f_s = reinterpret_cast<float*>(ring + kWarps * S::kRing);   // [COLS] score factor
   int* beg_s = reinterpret_cast<int*>(f_s + COLS);                   // [COLS] first and last + 1 key seen
   int* end_s = beg_s + COLS;
@@ -258,75 +303,112 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
   float* r_s = l_s + kWarps * COLS;                                  // value reference of a warp
   pdl_wait();  // (no early trigger: waiting blocks of the next kernels would take this one's places)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-  const int64_t total = total_tiles<D, COLS>(a);
+  const Line<D, COLS> line(a);
+  const int64_t total = line.total;
   const int shares = (int)min((int64_t)a.shares, total);
   if ((int)blockIdx.x >= shares) return;
   const int64_t w1 = share_begin(total, blockIdx.x + 1, shares);
   char* mine = ring + warp * S::kRing;
   const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
+  const uint32_t key_at = Tile<D>::at(gid, tig);
+  const uint32_t val_at[2] = {D == 64 ? Tile<D>::at(2 * tig, gid >> 1) + (gid & 1) * 8 : Tile<D>::at(2 * tig, gid),
+                              D == 64 ? Tile<D>::at(2 * tig + 1, gid >> 1) + (gid & 1) * 8 : Tile<D>::at(2 * tig + 1, gid)};
 
   for (int64_t w = share_begin(total, blockIdx.x, shares); w < w1;) {
-    const Unit u = locate<D, COLS>(a, w);
-    const int64_t unit_end = u.begin + u.s.tiles;
-    const int t_end = (int)(min(unit_end, w1) - u.begin);
+    const Unit u = line.locate(a, w);
+    const int64_t tile0 = u.begin + kStart, unit_end = tile0 + u.s.tiles;
+    const int t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
+    w = min(unit_end, w1);
+    if (u.tile >= t_end) continue;  // (this share ends before the unit's first tile)
     const int len = u.s.len, group = a.group;
     const int col0 = u.cg * COLS, n_cols = min(COLS, u.s.n * group - col0);
     __syncthreads();  // the previous unit's shared memory has been read
 
-    // A lane looks up the place and the scales of every 32nd of this warp's blocks; the copies of
-    // kStages - 1 blocks are on their way ahead of the one in work.
+    // A lane looks up the place and the scales of every 32nd of this warp's blocks. Step i takes the warp's
+    // blocks NB i .. of the part; while it works on its values and on the next step's keys, the copies of
+    // the next values and of the keys after those are on their way.
     const int reach = u.s.len - u.s.n + (col0 + n_cols - 1) / group + 1;  // past the last column's place
     const int some_e = a.causal ? min(len, reach) : len;
     const int some_b = a.window > 0 ? max(0, len - u.s.n + col0 / group - a.window + 1) : 0;
-    int64_t at_l = -1;
-    float sk_l = 0.f, sv_l = 0.f, sk_old = 0.f, sv_old = 0.f;
-    uint32_t has = 0, has_old = 0;  // blocks of the present 32 and of those before that some query sees
     constexpr int NB = kBlocks<D>;
-    auto start = [&](int i) {       // the warp's i-th blocks NB i .., counted from the part's first tile
-      if (u.tile + i < t_end) {
-        const int i0 = i * NB;
-        if ((i0 & 31) == 0) {
-          sk_old = sk_l;
-          sv_old = sv_l;
-          has_old = has;
-          const int tl = u.tile + (i0 + lane) / NB;
-          const int tok = (u.s.lo + tl) * kTile<D> + (warp * NB + lane % NB) * kCacheBlock;
-          at_l = -1;
-          if (tl < t_end && tok < some_e && tok + kCacheBlock > some_b) {
-            const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
-            if (page >= 0) {
-              const int in = tok % a.c.page;
-              at_l = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
-              const int64_t at_s = (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock;
-              sk_l = __ldg(a.c.ks + at_s);
-              sv_l = __ldg(a.c.vs + at_s);
-            }
-          }
-          has = __ballot_sync(0xffffffffu, at_l >= 0);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const int64_t at = __shfl_sync(0xffffffffu, at_l, (i0 + b) & 31);
-          if (at >= 0) start_block<D>(a.c, at, mine_u + ((i % S::kStages) * NB + b) * Pieces<D>::kBytes);
+    constexpr uint32_t kAll = (1u << NB) - 1;
+    const int n_tiles = t_end - u.tile;
+    int64_t at_l = -1, at_old = -1;
+    float sk_l = 0.f, sv_l = 0.f, sk_old = 0.f, sv_old = 0.f;
+    uint32_t has = 0, has_old = 0;  // blocks of the present 32 and of the 32 before that some query sees
+    int batch = -1;
+    auto look_up = [&](int i) {     // before step i's keys are wanted, each i in turn
+      if (i >= n_tiles || (i * NB & 31) != 0) return;
+      at_old = at_l;
+      sk_old = sk_l;
+      sv_old = sv_l;
+      has_old = has;
+      batch = i * NB >> 5;
+      const int tl = u.tile + i + lane / NB;
+      const int tok = (u.s.lo + tl) * kTile<D> + (warp * NB + lane % NB) * kCacheBlock;
+      at_l = -1;
+      if (tl < t_end && tok < some_e && tok + kCacheBlock > some_b) {
+        const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
+        if (page >= 0) {
+          const int in = tok % a.c.page;
+          at_l = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
+          const int64_t at_s = (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock;
+          sk_l = __ldg(a.c.ks + at_s);
+          sv_l = __ldg(a.c.vs + at_s);
         }
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      has = __ballot_sync(0xffffffffu, at_l >= 0);
     };
+    auto start_k = [&](int i) {
+      if (i >= n_tiles) return;
+      const bool old = (i * NB >> 5) != batch;
 #pragma unroll
-    for (int i = 0; i < S::kStages - 1; ++i) start(i);
+      for (int b = 0; b < NB; ++b) {
+        const int64_t at = __shfl_sync(0xffffffffu, old ? at_old : at_l, (i * NB + b) & 31);
+        if (at >= 0) start_block<D, false>(a.c.K + at, mine_u + ((i & 1) * NB + b) * Tile<D>::kBytes, kCacheBlock);
+      }
+    };
+    auto start_v = [&](int i) {
+      if (i >= n_tiles) return;
+      const bool old = (i * NB >> 5) != batch;
+      const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int64_t at = __shfl_sync(0xffffffffu, old ? at_old : at_l, (i * NB + b) & 31);
+        const uint32_t dst = mine_u + S::kHalf + ((i & 1) * NB + b) * Tile<D>::kBytes;
+        const int n = at >= 0 ? len - (tok + b * kCacheBlock) : 0;
+        if (n >= kCacheBlock)
+          start_block<D, false>(a.c.V + at, dst, n);
+        else
+          start_block<D, true>(a.c.V + max(at, (int64_t)0), dst, max(n, 0));
+      }
+    };
+    float qx[COLS / kWarps][D / 32];
+#pragma unroll
+    for (int k = 0; k < COLS / kWarps; ++k) {
+      const int col = warp + k * kWarps, j = (col0 + col) / group, h = u.h * group + (col0 + col) % group;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+        qx[k][e] = col < n_cols ? load_elem(a.q.data, (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head + lane + 32 * e,
+                                            a.q.type)
+                                : 0.f;
+    }
+    look_up(0);
+    start_k(0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    look_up(1);
+    start_k(1);
+    start_v(0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
 
     // queries: a warp per column, relative to the power of two at its largest element
-    for (int col = warp; col < COLS; col += kWarps) {
-      float x[D / 32];
-      float top = 0.f;
-      const int j = (col0 + col) / group, h = u.h * group + (col0 + col) % group;
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) {
-        x[e] = col < n_cols ? load_elem(a.q.data, (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head + lane + 32 * e,
-                                        a.q.type)
-                            : 0.f;
-        top = fmaxf(top, fabsf(x[e]));
-      }
+    for (int k = 0; k < COLS / kWarps; ++k) {
+      const int col = warp + k * kWarps, j = (col0 + col) / group;
+      float* x = qx[k];
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) top = fmaxf(top, fabsf(x[e]));
       top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
       // 2^-e for a top in [2^e, 2^(e + 1)); 1 for zeros, subnormals and infinities
       const uint32_t ex = __float_as_uint(top) >> 23;
@@ -378,24 +460,9 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         l[t][e] = 0.f;
       }
 
-    const int n_tiles = t_end - u.tile;
-    for (int i = 0; i < n_tiles; ++i) {
-      start(i + S::kStages - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
-      const bool old = (i * NB >> 5) != (min(i + S::kStages - 1, n_tiles - 1) * NB >> 5);
-      const uint32_t live = (old ? has_old : has) >> (i * NB & 31);
-      if ((live & ((1u << NB) - 1)) == 0) continue;
-      float sk[NB], sv[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        sk[b] = __shfl_sync(0xffffffffu, old ? sk_old : sk_l, (i * NB + b) & 31);
-        sv[b] = __shfl_sync(0xffffffffu, old ? sv_old : sv_l, (i * NB + b) & 31);
-      }
-      const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
-      const uint4* stage = reinterpret_cast<const uint4*>(mine + (i % S::kStages) * NB * Pieces<D>::kBytes) + lane;
-      constexpr int kUnits = Pieces<D>::kBytes / 16;
-
-      float s[NB][NT][4];
+    // S^T of step i's keys (what lies there is masked later where no key does)
+    auto scores = [&](int i, float s[NB][NT][4]) {
+      const char* keys = mine + (i & 1) * NB * Tile<D>::kBytes;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -417,7 +484,10 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
           }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          const uint4 k0 = stage[b * kUnits + j * 32], k1 = stage[b * kUnits + (D / 64 + j) * 32];
+          // (8 rows on, the same turn; every other 64 channels, the other half of the line)
+          const char* k = keys + b * Tile<D>::kBytes + (j >> 1) * 128;
+          const uint4 k0 = *reinterpret_cast<const uint4*>(k + (key_at ^ (j & 1) * 64));
+          const uint4 k1 = *reinterpret_cast<const uint4*>(k + 8 * D + (key_at ^ (j & 1) * 64));
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const uint32_t x = word(k0, w), y = word(k1, w);
@@ -430,8 +500,29 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
           }
         }
       }
+    };
+    float s[NB][NT][4];
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+    scores(0, s);
+    for (int i = 0; i < n_tiles; ++i) {
+      const bool old = (i * NB >> 5) != batch;
+      const uint32_t live = (old ? has_old : has) >> (i * NB & 31);
+      float sk[NB], sv[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        sk[b] = __shfl_sync(0xffffffffu, old ? sk_old : sk_l, (i * NB + b) & 31);
+        sv[b] = __shfl_sync(0xffffffffu, old ? sv_old : sv_l, (i * NB + b) & 31);
+      }
+      __syncwarp();  // every lane has read what these copies overwrite
+      start_v(i + 1);
+      look_up(i + 2);
+      start_k(i + 2);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
+
       // scores in units of log2, masked (a block that no query sees: all of it); their maxima
-      const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e && (live & ((1u << NB) - 1)) == (1u << NB) - 1;
+      const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e && (live & kAll) == kAll;
       float top[NT][2];
       bool grew = false;
 #pragma unroll
@@ -493,7 +584,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         const float m0 = m[n][0] == -INFINITY ? 0.f : m[n][0], m1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          const float wv = sv[b] * inv_ref;
+          const float wv = live >> b & 1 ? sv[b] * inv_ref : 0.f;
           float p0 = pow2(s[b][n][0] - m0), p1 = pow2(s[b][n][1] - m1);
           float p2 = pow2(s[b][n][2] - m0), p3 = pow2(s[b][n][3] - m1);
           l[n][0] += p0 + p2;
@@ -506,28 +597,26 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
           pb[b][1][n][1] = transpose8(half2_rest(p2, p3, h1));
         }
       }
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      __syncwarp();
+      // the next step's scores and this one's outputs: independent, in the same stretch of code
+      float next[NB][NT][4];
+      scores(i + 1, next);
+      const char* values = mine + S::kHalf + (i & 1) * NB * Tile<D>::kBytes;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        if (!(live >> b & 1)) continue;  // (its place in shared memory holds anything)
-        const int t0 = tok + b * kCacheBlock;
-        const uint4* stage_v = stage + b * kUnits + Pieces<D>::kKeys * 32;
 #pragma unroll
         for (int j = 0; j < (D == 64 ? 1 : D / 128); ++j) {
           uint4 v[4];
-          if constexpr (D == 64) {
-            const uint4 x = stage_v[0], y = stage_v[32];
-            v[0] = make_uint4(x.x, x.y, 0, 0);
-            v[1] = make_uint4(x.z, x.w, 0, 0);
-            v[2] = make_uint4(y.x, y.y, 0, 0);
-            v[3] = make_uint4(y.z, y.w, 0, 0);
-          } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = stage_v[(k * (D / 128) + j) * 32];
-          }
-          if (t0 + kCacheBlock > len) {  // places past the end hold anything: taken as codes of 0
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (t0 + 2 * tig + (k & 1) + 8 * (k >> 1) >= len) v[k] = make_uint4(0, 0, 0, 0);
+          for (int k = 0; k < 4; ++k) {
+            const char* p = values + b * Tile<D>::kBytes + j * 128 + (k >> 1) * 8 * D + val_at[k & 1];
+            if constexpr (D == 64) {
+              const uint2 x = *reinterpret_cast<const uint2*>(p);
+              v[k] = make_uint4(x.x, x.y, 0, 0);
+            } else {
+              v[k] = *reinterpret_cast<const uint4*>(p);
+            }
           }
 #pragma unroll
           for (int w = 0; w < (D == 64 ? 2 : 4); ++w) {
@@ -551,6 +640,12 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
           }
         }
       }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[b][n][e] = next[b][n][e];
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();  // every lane has read its pieces: the ring takes the outputs
@@ -580,8 +675,8 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         }
       }
     __syncthreads();
-    const bool complete = w == u.begin && u.begin + t_end == unit_end;
-    float* part = a.part + (int64_t)(2 * blockIdx.x + (w == u.begin ? 1 : 0)) * S::kSlot;
+    const bool complete = u.tile == 0 && t_end == u.s.tiles;
+    float* part = a.part + (int64_t)(2 * blockIdx.x + (u.tile == 0 ? 1 : 0)) * S::kSlot;
     for (int col = warp; col < n_cols; col += kWarps) {
       float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -616,67 +711,128 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         }
       }
     }
-    w = u.begin + t_end;
   }
 }
 
-// Joins the parts of the unit that the boundary between shares blockIdx.x and blockIdx.x + 1 cuts, if
-// it is the first that does: a warp per column, the parts in the order of the shares.
-template <int D, int COLS>
-__global__ void __launch_bounds__(32 * COLS)
+// Joins the parts of units that lie in several shares, in the order of the shares. Two forms:
+//   BY_UNIT (few units, so many parts each): a block per unit (x) and column (y), whose warps take every
+//     eighth part;
+//   otherwise (few parts each): a block per boundary between shares
+//     x and x + 1, if it is the first that cuts its unit; a warp per column.
+constexpr int kJoinWarps = 8;
+
+template <int D, int COLS, bool BY_UNIT>
+__global__ void __launch_bounds__(32 * kJoinWarps)
 attend_join_kernel(const __grid_constant__ AttendArgs a) {
+  __shared__ float m_s[kJoinWarps], l_s[kJoinWarps], o_s[BY_UNIT ? kJoinWarps * D : 1];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5;
-  const int64_t total = total_tiles<D, COLS>(a);
-  const int shares = (int)min((int64_t)a.shares, total), i0 = blockIdx.x;
-  if (i0 + 1 >= shares) return;
-  const int64_t cut = share_begin(total, i0 + 1, shares);
-  const Unit u = locate<D, COLS>(a, cut);
-  if (u.begin == cut || u.begin < share_begin(total, i0, shares)) return;
-  const int64_t end = u.begin + u.s.tiles;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Line<D, COLS> line(a);
+  const int64_t total = line.total;
+  const int shares = (int)min((int64_t)a.shares, total);
+  Unit u;
+  int i0;  // the share that holds the unit's first tile
+  if constexpr (BY_UNIT) {
+    if (!line.unit(a, blockIdx.x, &u)) return;
+    const int64_t first = u.begin + kStart;
+    i0 = (int)min((int64_t)shares - 1, divide(first * shares, total));  // within one of it
+    while (i0 + 1 < shares && share_begin(total, i0 + 1, shares) <= first) ++i0;
+    while (i0 > 0 && share_begin(total, i0, shares) > first) --i0;
+  } else {
+    i0 = blockIdx.x;
+    if (i0 + 1 >= shares) return;
+    u = line.locate(a, share_begin(total, i0 + 1, shares));
+    if (u.tile == 0 || share_begin(total, i0, shares) > u.begin + kStart) return;
+  }
+  const int64_t end = u.begin + kStart + u.s.tiles;
   constexpr int kSlot = COLS * (D + 2);
-  const int col0 = u.cg * COLS;
-  if (col0 + col >= u.s.n * a.group) return;
+  const int col0 = u.cg * COLS, n_cols = min(COLS, u.s.n * a.group - col0);
   int n = 1;  // shares that hold a part
   while (i0 + n < shares && share_begin(total, i0 + n, shares) < end) ++n;
-  // slot of part 0: the share's last unit; of the others: their first (the unit began before them)
+  if (n == 1) return;  // (written whole)
+  constexpr int kPer = D / 32;  // neighbouring channels of a lane
   const float* part = a.part + (int64_t)2 * i0 * kSlot;
-  float M = -INFINITY, L = 0.f, o[D / 32];
+  // part p: its share's last unit (p = 0), or its first
+  auto slot = [&](int p) { return part + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * kSlot; };
+
+  for (int col = BY_UNIT ? (int)blockIdx.y : warp; col < n_cols; col += BY_UNIT ? COLS : kJoinWarps) {
+    float M = -INFINITY, L = 0.f, o[kPer];
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int p0 = 0; p0 < n; p0 += 32) {
-    const int p = p0 + lane;
-    const float* pl = part + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * kSlot + COLS * D + col;
-    const float mp = p < n ? pl[0] : -INFINITY, lp = p < n ? pl[COLS] : 0.f;
-    float mn = fmaxf(M, mp);
+    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+    constexpr int kBatch = 8;
+    for (int p0 = BY_UNIT ? warp : 0; p0 < n; p0 += kBatch * (BY_UNIT ? kJoinWarps : 1)) {
+      float mp[kBatch], lp[kBatch], v[kBatch][kPer];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
-    const float mm = mn == -INFINITY ? 0.f : mn;
-    const float f = pow2(mp - mm), back = pow2(M - mm);
-    float sum = lp * f;
+      for (int q = 0; q < kBatch; ++q) {
+        const int p = p0 + q * (BY_UNIT ? kJoinWarps : 1);
+        mp[q] = -INFINITY;
+        lp[q] = 0.f;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    L = L * back + sum;
-    M = mn;
+        for (int e = 0; e < kPer; ++e) v[q][e] = 0.f;
+        if (p >= n) continue;
+        const float* src = slot(p);
+        mp[q] = src[COLS * D + col];
+        lp[q] = src[COLS * D + COLS + col];
+        if constexpr (D == 64) {
+          const float2 x = reinterpret_cast<const float2*>(src + col * D)[lane];
+          v[q][0] = x.x; v[q][1] = x.y;
+        } else {
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] *= back;
-    const int k = min(32, n - p0);
-#pragma unroll 8
-    for (int q = 0; q < k; ++q) {
-      const float fq = __shfl_sync(0xffffffffu, f, q);
-      const float* src = part + (int64_t)(2 * (p0 + q) + (p0 + q == 0 ? 1 : 0)) * kSlot + col * D + lane;
+          for (int e = 0; e < kPer / 4; ++e) {
+            const float4 x = reinterpret_cast<const float4*>(src + col * D)[lane * (kPer / 4) + e];
+            v[q][4 * e] = x.x; v[q][4 * e + 1] = x.y; v[q][4 * e + 2] = x.z; v[q][4 * e + 3] = x.w;
+          }
+        }
+      }
+      float mn = M;
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] += src[32 * e] * fq;
+      for (int q = 0; q < kBatch; ++q) mn = fmaxf(mn, mp[q]);
+      const float mm = mn == -INFINITY ? 0.f : mn, back = pow2(M - mm);
+      M = mn;
+      L *= back;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) o[e] *= back;
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        const float f = pow2(mp[q] - mm);
+        L += lp[q] * f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] += v[q][e] * f;
+      }
     }
-  }
-  const int j = (col0 + col) / a.group, h = u.h * a.group + (col0 + col) % a.group;
-  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+    if constexpr (BY_UNIT) {  // the warps' shares of the parts
+      if (lane == 0) {
+        m_s[warp] = M;
+        l_s[warp] = L;
+      }
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
-    store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + lane + 32 * e, a.o.type, o[e] * inv);
-  if (lane == 0 && a.lse)
-    a.lse[(u.s.first + j) * a.q.heads + h] = L > 0.f ? (M + log2f(L)) / kLog2e : (L == 0.f ? -INFINITY : L);
+      for (int e = 0; e < kPer; ++e) o_s[warp * D + lane * kPer + e] = o[e];
+      __syncthreads();
+      if (warp > 0) return;
+      M = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kJoinWarps; ++i) M = fmaxf(M, m_s[i]);
+      const float mm = M == -INFINITY ? 0.f : M;
+      L = 0.f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kJoinWarps; ++i) {
+        const float f = pow2(m_s[i] - mm);
+        L += l_s[i] * f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] += o_s[i * D + lane * kPer + e] * f;
+      }
+    }
+    const int j = (col0 + col) / a.group, h = u.h * a.group + (col0 + col) % a.group;
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + lane * kPer + e, a.o.type, o[e] * inv);
+    if (lane == 0 && a.lse)
+      a.lse[(u.s.first + j) * a.q.heads + h] = L > 0.f ? (M + log2f(L)) / kLog2e : (L == 0.f ? -INFINITY : L);
+  }
 }
 
 template <int D, int NT, int FMT, bool SPLIT>
@@ -691,7 +847,14 @@ crvq_status launch_attend(AttendArgs& a, cudaStream_t stream) {
   ProfScope ps("cache_attention", stream, (double)a.rows.n_tok * a.q.heads * D);
   CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)a.shares), dim3(kThreads), S::kSmem, stream, a));
   CRVQ_LAUNCHED();
-  CRVQ_CUDA(launch_pdl(attend_join_kernel<D, S::kCols>, dim3((unsigned)a.shares - 1), dim3(32 * S::kCols), 0, stream, a));
+  // an upper bound of the units: every sequence's columns, rounded up to whole groups
+  const int64_t units = (a.rows.n_tok * a.group / S::kCols + a.c.n_seq) * a.c.n_kv;
+  const dim3 threads(32 * kJoinWarps);
+  // (8 units of 40 parts: 24 us by boundaries, 18 by units; 64 units of 7 parts: 16.5 and 20.5)
+  if (units * kJoinWarps <= a.shares)
+    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, S::kCols, true>, dim3((unsigned)units, S::kCols), threads, 0, stream, a));
+  else
+    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, S::kCols, false>, dim3((unsigned)a.shares - 1), threads, 0, stream, a));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }

@@ -2,15 +2,26 @@
 // and the product with 1 to 32 inputs,
 //   y_b[i] = sum_groups s_ig sum_{j in group} (code_ij - zero_ig) x_bj.
 //
-// Product. code - zero is an integer of at most 15: exact in bf16 and fp16, so the inner sums run on
-// mma.sync.m16n8k16 with the weights as A (16 rows) and up to 8 NT inputs as B, in the inputs' own type;
-// fp32 inputs are cut into three bf16 pieces of 8 bits each (their sum is the input). A group's sum is
-// scaled once, in fp32. The order of the inner index is free: a lane holds 32 (16, 8) consecutive codes
-// of a row, one 16- (8-, 4-) byte load, and pairs nibbles e and e + 4 of a word, which three shifts and
-// four masks turn into 16-bit floats (1024 + code, or 128 + code, less 1024 + zero or 128 + zero); the
-// lane's piece of the inputs is loaded in the same order.
-//   A CTA owns 16 RT rows; its eight warps take every eighth 128 inputs, and their sums meet in shared
-// memory in a fixed order. One launch, no scratch.
+// Product. code - zero is an integer of at most 15, exact in fp16, so the inner sums run on
+// mma.sync.m16n8k16 with the weights as A (16 rows) and up to 8 NT inputs as B. fp16 inputs go as they are;
+// bf16 inputs are taken relative to a power of two per group and input (exact but for elements below 2^-14 of
+// the group's largest), fp32 inputs so in two pieces (22 bits). A group's sum is scaled once, in fp32. The
+// order of the inner index is free: a lane holds 32 (16, 8) consecutive codes of a row and pairs nibbles
+// e and e + 4 of a word; one shift and four masks turn a word into fp16 pairs 1024 + code or 1024 + 16 code, one
+// fp16 operation each into code - zero. The lane's piece of the inputs is laid out in the same order.
+//
+// Split. One CTA per SM owns an equal run of tiles (16 RT rows). It lays the inputs out in operand order in
+// shared memory once (or in chunks, where they do not fit), and each of its warps takes an equal share of the
+// line of all (tile, step) pairs, a step being 256 inputs: 128 bytes of a row's codes, copied ahead to the
+// warp's own ring, every copy instruction four whole 128-byte lines; the scales follow in registers. A warp
+// whose share begins inside a tile leaves that tile's sum in a slot of its own; the slots are added in warp
+// order. Where there are fewer tiles than SMs the inputs are sliced over a cluster, whose sums meet in
+// distributed shared memory. One launch, no scratch, sums in a fixed order. (A CTA per tile spent
+// most of its time on laying out inputs and on its own start: 28672 x 8192, one input, 73 us.)
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
 #include "cache.cuh"
 
 #include "kernels.h"
@@ -19,10 +30,10 @@ namespace crvq {
 
 namespace {
 
-constexpr int kQWarps = 8;
-constexpr int kQThreads = 32 * kQWarps;
-constexpr int kStep = 128;  // inputs per warp step
+constexpr int kStep = 256;       // inputs per warp step: 128 bytes of a row's codes
+constexpr int kTileBytes = 16 * kStep / 2;
 constexpr int kMaxInputs = 32;
+constexpr int kMaxSlices = 8;
 
 struct Q4View {
   uint8_t* codes;
@@ -37,211 +48,499 @@ struct MatvecQ4 {
   int64_t ldx;
   void* Y;
   int64_t ldy;
-  int b, type;
+  int b;
   bool vec_w, vec_x;
+  int cols;           // columns laid out: b, or 8 NT
+  int chunk;          // steps laid out at a time
+  int group;          // tiles whose sums are held at a time
 };
 
-template <bool BF16>
 __device__ __forceinline__ void mma16(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
-  if constexpr (BF16)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Codes e and e + 4 of a word, less the zero point (zc: 128 + zero in bf16 or 1024 + zero in fp16, twice).
-template <bool BF16>
-__device__ __forceinline__ uint32_t codes_pair(uint32_t w, int e, uint32_t zc) {
-  const uint32_t u = ((w >> (4 * e)) & 0x000f000fu) | (BF16 ? 0x43004300u : 0x64006400u);
-  if constexpr (BF16) {
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u),
-                                     *reinterpret_cast<const __nv_bfloat162*>(&zc));
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u), *reinterpret_cast<const __half2*>(&zc));
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
+// The same into zeros (no registers are cleared for it).
+__device__ __forceinline__ void mma16_first(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// x = p[0] + p[1] + p[2] exactly, each the upper half of an fp32 (8 significant bits).
-__device__ __forceinline__ void cut3(float x, uint32_t p[3]) {
-  p[0] = __float_as_uint(x);
-  const float r = fabsf(x) == INFINITY ? 0.f : x - __uint_as_float(p[0] & 0xffff0000u);
-  p[1] = __float_as_uint(r);
-  p[2] = __float_as_uint(r - __uint_as_float(p[1] & 0xffff0000u));
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+
+// Codes e and e + 4 of a word (e = 0 .. 3) less the zero point z; lo: 1024 + z twice, hi: -(64 + z) twice. The
+// integers' low bits are the mantissa's, so both forms are exact: (1024 + c) - (1024 + z), (1024 + 16 c) / 16 - (64 + z).
+__device__ __forceinline__ uint32_t take(uint32_t v, uint32_t mask) {  // (v & mask) | 1024 twice, in one operation
+  uint32_t u;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(u) : "r"(v), "r"(mask), "r"(0x64006400u));
+  return u;
 }
 
-// The inputs k .. k + 7 of row `row` of X (null: zeros) as B operand pairs (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ uint32_t codes_pair(uint32_t w, int e, uint32_t lo, uint32_t hi) {
+  const uint32_t v = e >= 2 ? w >> 8 : w;
+  if (e & 1) return bits(__hfma2(as_half2(take(v, 0x00f000f0u)), as_half2(0x2c002c00u), as_half2(hi)));
+  return bits(__hsub2(as_half2(take(v, 0x000f000fu)), as_half2(lo)));
+}
+
+// The inputs k .. k + 7 of row `row` of X (zeros past N), unless fp16 as fp32.
 template <int TYPE>
-__device__ __forceinline__ void load_x(const MatvecQ4& a, int64_t row, bool live, int64_t k,
-                                       uint32_t v[TYPE == CRVQ_F32 ? 3 : 1][4]) {
-  if constexpr (TYPE == CRVQ_F32) {
-    float x[8];
-    const float* p = static_cast<const float*>(a.X) + row * a.ldx;
-    if (live && k + 8 <= a.m.N) {
-      load8(p, k, CRVQ_F32, a.vec_x, x);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = live && k + j < a.m.N ? p[k + j] : 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t lo[3], hi[3];
-      cut3(x[e], lo);
-      cut3(x[e + 4], hi);
-#pragma unroll
-      for (int z = 0; z < 3; ++z) v[z][e] = __byte_perm(lo[z], hi[z], 0x7632);
-    }
+__device__ __forceinline__ void load_x(const MatvecQ4& a, int64_t row, int64_t k, float x[8]) {
+  const char* p = static_cast<const char*>(a.X) + row * a.ldx * (TYPE == CRVQ_F32 ? 4 : 2);
+  if (k + 8 <= a.m.N) {
+    load8(p, k, TYPE, a.vec_x, x);
   } else {
-    const uint16_t* p = static_cast<const uint16_t*>(a.X) + row * a.ldx;
-    uint32_t w[4];
-    if (live && a.vec_x && k + 8 <= a.m.N) {
-      const uint4 u = *reinterpret_cast<const uint4*>(p + k);
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = live && k + 2 * j < a.m.N ? p[k + 2 * j] : 0;
-        const uint32_t hi = live && k + 2 * j + 1 < a.m.N ? p[k + 2 * j + 1] : 0;
-        w[j] = lo | hi << 16;
-      }
-    }
-    v[0][0] = __byte_perm(w[0], w[2], 0x5410);
-    v[0][1] = __byte_perm(w[0], w[2], 0x7632);
-    v[0][2] = __byte_perm(w[1], w[3], 0x5410);
-    v[0][3] = __byte_perm(w[1], w[3], 0x7632);
+    for (int j = 0; j < 8; ++j) x[j] = k + j < a.m.N ? load_elem(p, k + j, TYPE) : 0.f;
   }
 }
 
-// WORDS consecutive words of a row's codes from byte `at` on, zeros past the row's end.
-template <int WORDS>
-__device__ __forceinline__ void load_codes(const MatvecQ4& a, const uint8_t* row, int64_t at, uint32_t w[WORDS]) {
-  const int64_t bytes = (a.m.N + 1) / 2;
-  if (a.vec_w && at + 4 * WORDS <= bytes) {
-    if constexpr (WORDS == 4) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(row + at));
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-    } else if constexpr (WORDS == 2) {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(row + at));
-      w[0] = u.x; w[1] = u.y;
-    } else {
-      w[0] = __ldg(reinterpret_cast<const uint32_t*>(row + at));
+// Eight inputs as fp16 B operand pairs (0, 4), (1, 5), (2, 6), (3, 7); rest: what the pairs leave over, or null.
+__device__ __forceinline__ uint4 operand_pairs(const float x[8], uint4* rest) {
+  uint32_t v[4], r[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 h = __floats2half2_rn(x[e], x[e + 4]);
+    v[e] = bits(h);
+    if (rest) {
+      const float2 f = __half22float2(h);
+      r[e] = bits(__floats2half2_rn(fabsf(f.x) == INFINITY ? 0.f : x[e] - f.x,
+                                    fabsf(f.y) == INFINITY ? 0.f : x[e + 4] - f.y));
+    }
+  }
+  if (rest) *rest = make_uint4(r[0], r[1], r[2], r[3]);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// A row's 128 bytes in shared memory: eight 16-byte units, exchanged by the row so that eight lanes (two rows, four
+// neighbouring units) read without bank conflicts.
+__device__ __forceinline__ uint32_t unit_at(int r, int c) {
+  return (uint32_t)(r * 8 + (c ^ ((r & 6) ^ ((r & 1) << 2)))) * 16;
+}
+
+// Offset of lane (row r, tig) in a tile's rows; the words of half j (128 inputs, 64 bytes) follow by exchanging
+// bits of it (load_words): of each group of 4 x 8 WORDS inputs, lane tig holds the tig-th WORDS words, so
+// that the four lanes of a row hold one group at a time.
+template <int GROUP>
+__device__ __forceinline__ uint32_t words_at(int r, int tig) {
+  return GROUP == 128 ? unit_at(r, tig) : GROUP == 64 ? unit_at(r, tig >> 1) + (tig & 1) * 8 : unit_at(r, 0) + tig * 4;
+}
+
+template <int GROUP>
+__device__ __forceinline__ void load_words(const char* tile, uint32_t at, int j, uint32_t w[4]) {
+  at ^= 64 * j;
+  if constexpr (GROUP == 128) {
+    const uint4 u = *reinterpret_cast<const uint4*>(tile + at);
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+  } else if constexpr (GROUP == 64) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint2 u = *reinterpret_cast<const uint2*>(tile + (at ^ 32 * s));
+      w[2 * s] = u.x; w[2 * s + 1] = u.y;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      w[i] = 0;
+    for (int s = 0; s < 4; ++s) w[s] = *reinterpret_cast<const uint32_t*>(tile + (at ^ 16 * s));
+  }
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Copies 16 rows' codes of one step to a tile where rows or inputs may end in it, or rows are not aligned.
+__device__ __noinline__ void start_tile_edge(const MatvecQ4& a, int64_t row0, int64_t k, char* tile) {
+  const int lane = threadIdx.x & 31;
+  const int64_t bytes = (a.m.N + 1) / 2, at = k / 2 + (lane & 7) * 16;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * i + (lane >> 3);
+    const uint8_t* src = a.m.codes + min(row0 + r, a.m.M - 1) * a.m.ld_codes;
+    const int n = (int)max((int64_t)0, min((int64_t)16, bytes - at));
+    char* dst = tile + unit_at(r, lane & 7);
+    if (a.vec_w) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)),
+                   "l"(src + (n > 0 ? at : 0)), "r"(n)
+                   : "memory");
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (at + 4 * i + j < bytes) w[i] |= (uint32_t)__ldg(row + at + 4 * i + j) << (8 * j);
+      for (int j = 0; j < 16; ++j)
+        if (j < n) w[j / 4] |= (uint32_t)__ldg(src + at + j) << (8 * (j % 4));
+      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
 
 template <int TYPE, int GROUP, int NT, int RT>
-__global__ void __launch_bounds__(kQThreads)
+struct MatvecShape {
+  static constexpr int kPieces = TYPE == CRVQ_F32 ? 2 : 1;
+  static constexpr bool kScaled = TYPE != CRVQ_F16;           // inputs relative to a power of two per group
+  static constexpr int kWarps = NT == 4 ? 8 : 12;
+  static constexpr int kStages = NT == 1 ? 3 : 2;             // (more leave less room for inputs)
+
+  static constexpr int kGroups = kStep / GROUP;               // groups in a step
+  static constexpr int kScales = 16 * RT * kGroups;           // scales of a step's rows, with zero points, 4 bytes
+  static constexpr int kStage = RT * kTileBytes + kScales * 4;
+  static constexpr int kRing = kStages * kStage;
+  static constexpr int kSums = 8 * NT * 16 * RT;              // outputs of a tile
+  static constexpr size_t kFixed = (size_t)kWarps * kRing + (size_t)kWarps * kSums * 4 + 16;
+  // a step's inputs, and their powers of two; the steps that fit beside the rest
+  static int step_bytes(int cols) { return cols * (kPieces * 2 * kStep + (kScaled ? 4 * kGroups : 0)); }
+  static size_t smem(int chunk, int group, int cols) {
+    return kFixed + (size_t)group * kSums * 4 + (size_t)step_bytes(cols) * chunk;
+  }
+  static int64_t chunk(int64_t group, int cols) {
+    return ((int64_t)(225 * 1024 - kFixed) - group * kSums * 4) / step_bytes(cols);
+  }
+};
+
+template <int TYPE, int GROUP, int NT, int RT>
+__global__ void __launch_bounds__(32 * MatvecShape<TYPE, GROUP, NT, RT>::kWarps, 1)
 q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
-  constexpr bool BF16 = TYPE != CRVQ_F16;
-  constexpr int kPieces = TYPE == CRVQ_F32 ? 3 : 1;
-  constexpr int kSubs = kStep / GROUP, WORDS = GROUP / 32;
-  constexpr int R = 16 * RT, COLS = 8 * NT;
-  extern __shared__ __align__(16) float red[];  // [kQWarps][COLS][R]
+  namespace cg = cooperative_groups;
+  using S = MatvecShape<TYPE, GROUP, NT, RT>;
+  constexpr int W = S::kWarps, kThreads = 32 * W, R = 16 * RT, COLS = 8 * NT, WORDS = GROUP / 32;
+  extern __shared__ __align__(128) char sm[];
+  __shared__ int slot_tile[W];
   pdl_trigger();
   pdl_wait();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int slices = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-  const int64_t r0 = (int64_t)blockIdx.x * R;
   const Q4View& m = a.m;
-  const int64_t steps = (m.N + kStep - 1) / kStep, n_groups = (m.N + GROUP - 1) / GROUP;
+  // this CTA's tiles and steps
+  const int64_t tiles = (m.M + R - 1) / R, ctas = gridDim.x / slices, me = blockIdx.x / slices;
+  const int64_t tile0 = tiles * me / ctas;
+  const int n_tiles = (int)(tiles * (me + 1) / ctas - tile0);
+  const int all_steps = (int)((m.N + kStep - 1) / kStep);
+  const int step0 = (int)((int64_t)all_steps * rank / slices);
+  const int n_steps = (int)((int64_t)all_steps * (rank + 1) / slices) - step0;
+  const int n_chunks = (n_steps + a.chunk - 1) / a.chunk;
 
-  int64_t row[RT][2];
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) row[t][i] = min(r0 + 16 * t + gid + 8 * i, m.M - 1);
+  const int ring = warp * S::kRing;  // (offsets from sm: 32-bit shared-memory addresses)
+  float* slots = reinterpret_cast<float*>(sm + W * S::kRing);  // [W][COLS][R]
+  float* sums = slots + W * S::kSums;                          // [group][COLS][R]
+  uint4* none = reinterpret_cast<uint4*>(sums + a.group * S::kSums);  // zeros, for columns past the inputs
+  uint4* xs = none + 1;                                        // [pieces][half step][word][cols][4]
+  const int cols = NT > 1 ? COLS : a.cols;
+  float* xf = reinterpret_cast<float*>(xs + S::kPieces * a.chunk * 32 * cols);  // [group][cols] powers of two
+  if (tid == 0) *none = make_uint4(0, 0, 0, 0);
+  // this lane's column of the inputs: its first word's place, and how far the next word's is
+  const bool laid = gid < cols;
+  const int x_lane = (int)(laid ? reinterpret_cast<char*>(xs + gid * 4 + tig) - sm : reinterpret_cast<char*>(none) - sm);
+  const int x_word = laid ? 64 * cols : 0, x_piece = laid ? a.chunk * 512 * cols : 0;
+  const int xf_lane = (int)(reinterpret_cast<char*>(xf + 2 * tig) - sm);
+  const uint32_t w_lane = words_at<GROUP>(gid, tig);
 
-  float acc[RT][NT][4];
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[t][n][e] = 0.f;
+  // A place on this warp's way: tiles t0 .. of the present group, the chunk from step c0 on, and in it the
+  // share [i, end) of the line of (tile, step) pairs.
+  struct Place {
+    int t0, c0, i, end, tile, st, nst;
+  };
+  auto enter = [&](Place& p) {  // the first place of the group and chunk that t0 and c0 name
+    const int nt = min(a.group, n_tiles - p.t0);
+    p.nst = min(a.chunk, n_steps - p.c0);
+    const int line = nt * p.nst;
+    p.i = line * warp / W;
+    p.end = line * (warp + 1) / W;
+    p.tile = p.i / p.nst;
+    p.st = p.i - p.tile * p.nst;
+  };
+  auto leave = [&](Place& p) {  // to the next chunk or group that has a share; false past the last
+    while (p.i >= p.end) {
+      p.c0 += a.chunk;
+      if (p.c0 >= n_steps) {
+        p.c0 = 0;
+        p.t0 += a.group;
+        if (p.t0 >= n_tiles) return false;
+      }
+      enter(p);
+    }
+    return true;
+  };
+  auto next = [&](Place& p) {
+    ++p.i;
+    if (++p.st == p.nst) {
+      p.st = 0;
+      ++p.tile;
+    }
+  };
 
-  for (int64_t st = warp; st < steps; st += kQWarps) {
-#pragma unroll
-    for (int sub = 0; sub < kSubs; ++sub) {
-      const int64_t g = min(st * kSubs + sub, n_groups - 1);
-      const int64_t k = st * kStep + sub * GROUP + tig * (GROUP / 4);
-      uint32_t w[RT][2][WORDS], zc[RT][2];
-      float sc[RT][2];
+  // Copies ahead: a step's codes, and its scales and zero points, which wait in registers until the step
+  // after (lane: row lane / 2 of each 16, half of its groups).
+  constexpr int kMine = S::kGroups / 2;
+  uint32_t held[RT][kMine];
+  int held_slot = -1;
+  Place ahead = {0, 0, 0, 0, 0, 0, 0};
+  bool more = n_tiles > 0 && n_steps > 0, inside = false;
+  const uint8_t* codes = nullptr;  // this lane's first 16 bytes of the step ahead, and its first scale there
+  const __nv_bfloat16* scales = nullptr;
+  int64_t zeros = 0;               // (the zero points' offset)
+  auto point = [&]() {             // after a tile's or a chunk's first place
+    const int64_t k = (int64_t)(step0 + ahead.c0 + ahead.st) * kStep, row0 = (tile0 + ahead.t0 + ahead.tile) * R;
+    inside = a.vec_w && row0 + R <= m.M;
+    codes = m.codes + (row0 + (lane >> 3)) * m.ld_codes + k / 2 + (lane & 7) * 16;
+    zeros = (row0 + (lane >> 1)) * m.ld_scales + k / GROUP + (lane & 1) * kMine;
+    scales = m.scales + zeros;
+  };
+  if (more) {
+    enter(ahead);
+    more = leave(ahead);
+    if (more) point();
+  }
+  const int64_t ld4 = 4 * m.ld_codes, ld16 = 16 * m.ld_scales;
+  const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(sm + ring), dst0 = unit_at(lane >> 3, lane & 7);
+  auto start = [&](int slot) {
+    if (held_slot >= 0) {
+      uint32_t* sc = reinterpret_cast<uint32_t*>(sm + ring + held_slot * S::kStage + RT * kTileBytes);
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          load_codes<WORDS>(a, m.codes + row[t][i] * m.ld_codes, k / 2, w[t][i]);
-          sc[t][i] = __bfloat162float(m.scales[row[t][i] * m.ld_scales + g]);
-          const uint32_t z = m.zeros ? __ldg(m.zeros + row[t][i] * m.ld_scales + g) & 15u : 8u;
-          // 128 + z in bf16, 1024 + z in fp16: the integer's low bits are the mantissa's
-          zc[t][i] = ((BF16 ? 0x4300u : 0x6400u) + z) * 0x10001u;
+        for (int e = 0; e < kMine; ++e) sc[((lane & 1) * kMine + e) * R + 16 * t + (lane >> 1)] = held[t][e];
+      held_slot = -1;
+    }
+    if (more) {
+      const int step = step0 + ahead.c0 + ahead.st;
+      if (inside && (int64_t)(step + 1) * kStep <= m.N) {
+        const uint8_t* src = codes;
+        const uint32_t dst = ring_u + slot * S::kStage;
+#pragma unroll
+        for (int i = 0; i < 4 * RT; ++i) {
+          // (rows 4 i on: the unit's exchange differs in one bit for odd i)
+          copy16(dst + (dst0 ^ (i & 1) * 64) + i * 512, src);
+          src += ld4;
         }
-      float part[RT][NT][4];
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) part[t][n][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) {
-        uint32_t x[NT][kPieces][4];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) load_x<TYPE>(a, 8 * n + gid, 8 * n + gid < a.b, k + 8 * i, x[n]);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            uint32_t A[4];
-            A[0] = codes_pair<BF16>(w[t][0][i], e, zc[t][0]);
-            A[1] = codes_pair<BF16>(w[t][1][i], e, zc[t][1]);
-            A[2] = codes_pair<BF16>(w[t][0][i], e + 1, zc[t][0]);
-            A[3] = codes_pair<BF16>(w[t][1][i], e + 1, zc[t][1]);
+          for (int e = 0; e < kMine; ++e) {
+            const uint32_t s = __bfloat16_as_ushort(scales[t * ld16 + e]);
+            held[t][e] = s << 16 | (m.zeros ? __ldg(m.zeros + zeros + t * ld16 + e) & 15u : 8u);
+          }
+      } else {
+        const int64_t k = (int64_t)step * kStep, row0 = (tile0 + ahead.t0 + ahead.tile) * R;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          start_tile_edge(a, row0 + 16 * t, k, sm + ring + slot * S::kStage + t * kTileBytes);
+          const int64_t row = min(row0 + 16 * t + (lane >> 1), m.M - 1) * m.ld_scales;
+#pragma unroll
+          for (int e = 0; e < kMine; ++e) {
+            const int64_t g = k / GROUP + (lane & 1) * kMine + e;
+            const bool in = g * GROUP < m.N;  // (past N: 0)
+            const uint32_t s = in ? __bfloat16_as_ushort(m.scales[row + g]) : 0u;
+            held[t][e] = s << 16 | (in && m.zeros ? __ldg(m.zeros + row + g) & 15u : 8u);
+          }
+        }
+      }
+      held_slot = slot;
+      const int tile = ahead.tile, c0 = ahead.c0, group0 = ahead.t0;
+      next(ahead);
+      codes += kStep / 2;
+      scales += S::kGroups;
+      zeros += S::kGroups;
+      more = leave(ahead);
+      if (more && (ahead.tile != tile || ahead.c0 != c0 || ahead.t0 != group0)) point();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < S::kStages - 1; ++i) start(i);
+
+  int slot = 0;
+  for (int t0 = 0; t0 < n_tiles; t0 += a.group) {
+    const int nt = min(a.group, n_tiles - t0);
+    if (t0) __syncthreads();  // the previous group's sums have been read
+    for (int e = tid; e < nt * S::kSums; e += kThreads) sums[e] = 0.f;
+    for (int ch = 0; ch < n_chunks; ++ch) {
+      Place p = {t0, ch * a.chunk, 0, 0, 0, 0, 0};
+      enter(p);
+      if (n_chunks > 1 || t0 == 0) {
+        __syncthreads();  // the inputs before these have been read
+        const int cn = p.nst * (kStep / 8);  // eights of inputs
+        const int all = cn * cols;
+        constexpr int kAhead = TYPE == CRVQ_F32 ? 2 : 4;  // loads on their way together
+        for (int e0 = 0; e0 < all; e0 += kThreads * kAhead) {  // (whole warps: 32 eights of one column)
+          float xa[kAhead][8];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int e = e0 + u * kThreads + tid, col = e / cn, o = e - col * cn;
+            if (e < all && col < a.b) {  // neighbouring threads read neighbouring inputs
+              load_x<TYPE>(a, col, (int64_t)(step0 + p.c0) * kStep + 8 * o, xa[u]);
+            } else {
+#pragma unroll
+              for (int z = 0; z < 8; ++z) xa[u][z] = 0.f;
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int e = e0 + u * kThreads + tid, col = e / cn, o = e - col * cn;
+            if (e >= all) break;
+            // the half step, and the word and lane that want it: of each group, lane t the t-th quarter
+            const int j = o / 16, in = o % 16 * 8, sub = in / GROUP, rest = in % GROUP;
+            const int t = rest / (GROUP / 4), i = sub * WORDS + rest % (GROUP / 4) / 8;
+            uint4* dst = xs + ((j * 4 + i) * cols + col) * 4 + t;
+            float* x = xa[u];
+            if constexpr (S::kScaled) {
+              float top = 0.f;
+#pragma unroll
+              for (int z = 0; z < 8; ++z) top = fmaxf(top, fabsf(x[z]));
+#pragma unroll
+              for (int d = GROUP / 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              // 2^-e for a top in [2^e, 2^(e + 1)); 1 for zeros, subnormals and infinities
+              const uint32_t ex = __float_as_uint(top) >> 23;
+              const bool plain = ex == 0 || ex == 255;
+              const float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
+#pragma unroll
+              for (int z = 0; z < 8; ++z) x[z] *= inv;
+              if (rest == 0) xf[(j * (128 / GROUP) + sub) * cols + col] = plain ? 1.f : __uint_as_float(ex << 23);
+            }
+            if constexpr (S::kPieces == 2)
+              *dst = operand_pairs(x, dst + a.chunk * 32 * cols);
+            else
+              *dst = operand_pairs(x, nullptr);
+          }
+        }
+      }
+      if (tid < W) slot_tile[tid] = -1;
+      __syncthreads();
+
+      float acc[RT][NT][4];
+      bool fresh = true, first = false;  // at a new tile; its sum begins with this warp
+      while (p.i < p.end) {
+        if (fresh) {
+          first = p.st == 0;
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-              for (int z = 0; z < kPieces; ++z) mma16<BF16>(part[t][n], A, x[n][z][e], x[n][z][e + 1]);
+              for (int e = 0; e < 4; ++e) acc[t][n][e] = 0.f;
+        }
+        __syncwarp();  // every lane has read the stage that these copies overwrite
+        start(slot == 0 ? S::kStages - 1 : slot - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+        __syncwarp();
+        const int stage = ring + slot * S::kStage, sc = stage + RT * kTileBytes + gid * 4;
+        int xp = x_lane + p.st * 8 * x_word;
+        const int xfp = xf_lane + p.st * S::kGroups * cols * 4;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t w[RT][2][4];
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) load_words<GROUP>(sm + stage + t * kTileBytes + h * 1024, w_lane, j, w[t][h]);
+#pragma unroll
+          for (int sub = 0; sub < 128 / GROUP; ++sub) {
+            uint32_t sz[RT][2], lo[RT][2], hi[RT][2];
+            float part[RT][NT][4];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                sz[t][h] = *reinterpret_cast<const uint32_t*>(sm + sc + ((j * (128 / GROUP) + sub) * R + 16 * t + 8 * h) * 4);
+                const uint32_t z = sz[t][h] & 15u;
+                lo[t][h] = z * 0x10001u + 0x64006400u;
+                hi[t][h] = z * 0x100010u + 0xd400d400u;
+              }
+            }
+#pragma unroll
+            for (int i = sub * WORDS; i < (sub + 1) * WORDS; ++i) {
+              uint4 x[NT][S::kPieces];
+#pragma unroll
+              for (int z = 0; z < S::kPieces; ++z)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[n][z] = *reinterpret_cast<const uint4*>(sm + xp + z * x_piece + 512 * n);
+              xp += x_word;
+#pragma unroll
+              for (int t = 0; t < RT; ++t) {
+                uint32_t A[4];
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                  A[0] = codes_pair(w[t][0][i], e, lo[t][0], hi[t][0]);
+                  A[1] = codes_pair(w[t][1][i], e, lo[t][1], hi[t][1]);
+                  A[2] = codes_pair(w[t][0][i], e + 1, lo[t][0], hi[t][0]);
+                  A[3] = codes_pair(w[t][1][i], e + 1, lo[t][1], hi[t][1]);
+#pragma unroll
+                  for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int z = 0; z < S::kPieces; ++z)
+                      if (i == sub * WORDS && z == 0 && e == 0)
+                        mma16_first(part[t][n], A, x[n][z].x, x[n][z].y);
+                      else
+                        mma16(part[t][n], A, e ? x[n][z].z : x[n][z].x, e ? x[n][z].w : x[n][z].y);
+                }
+              }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float f[2] = {1.f, 1.f};
+              if constexpr (S::kScaled) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  f[e] = NT > 1 || 2 * tig + e < cols
+                             ? *reinterpret_cast<const float*>(sm + xfp + ((j * (128 / GROUP) + sub) * cols + 8 * n + e) * 4)
+                             : 0.f;
+              }
+#pragma unroll
+              for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float s = __uint_as_float(sz[t][e >> 1] & 0xffff0000u);
+                  acc[t][n][e] = fmaf(S::kScaled ? s * f[e & 1] : s, part[t][n][e], acc[t][n][e]);
+                }
+            }
           }
+        }
+        slot = slot + 1 == S::kStages ? 0 : slot + 1;
+        const int tile = p.tile;
+        next(p);
+        fresh = p.tile != tile;
+        if (fresh || p.i == p.end) {
+          // the tile's sum of this chunk begins here: to the sums themselves; else to this warp's slot
+          float* dst = first ? sums + tile * S::kSums : slots + warp * S::kSums;
+          if (!first && lane == 0) slot_tile[warp] = tile;
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float* q = dst + (8 * n + 2 * tig + (e & 1)) * R + 16 * t + gid + 8 * (e >> 1);
+                *q = first ? *q + acc[t][n][e] : acc[t][n][e];
+              }
+        }
       }
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][n][e] = fmaf(sc[t][e >> 1], part[t][n][e], acc[t][n][e]);
+      __syncthreads();
+      for (int e = tid; e < S::kSums; e += kThreads)
+        for (int i = 0; i < W; ++i)
+          if (slot_tile[i] >= 0) sums[slot_tile[i] * S::kSums + e] += slots[i * S::kSums + e];
     }
-  }
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        red[((size_t)warp * COLS + 8 * n + 2 * tig + (e & 1)) * R + 16 * t + gid + 8 * (e >> 1)] = acc[t][n][e];
-  __syncthreads();
-  for (int e = tid; e < a.b * R; e += kQThreads) {
-    const int col = e / R, r = e - col * R;
-    if (r0 + r >= m.M) continue;
-    float v = 0.f;
-#pragma unroll
-    for (int i = 0; i < kQWarps; ++i) v += red[((size_t)i * COLS + col) * R + r];
-    store_elem(a.Y, col * a.ldy + r0 + r, TYPE, v);
+    const int64_t r0 = (tile0 + t0) * R;
+    if (slices == 1) {
+      for (int e = tid; e < S::kSums; e += kThreads) {
+        const int col = e / R, r = e - col * R;
+        if (col >= a.b) break;
+        for (int t = 0; t < nt; ++t)
+          if (r0 + t * R + r < m.M) store_elem(a.Y, col * a.ldy + r0 + t * R + r, TYPE, sums[t * S::kSums + e]);
+      }
+    } else {
+      cluster.sync();
+      for (int e = rank * kThreads + tid; e < nt * S::kSums; e += slices * kThreads) {
+        const int t = e / S::kSums, col = (e - t * S::kSums) / R, r = e % R;
+        float v = 0.f;
+        for (int i = 0; i < slices; ++i) v += cluster.map_shared_rank(sums, i)[e];
+        if (col < a.b && r0 + t * R + r < m.M) store_elem(a.Y, col * a.ldy + r0 + t * R + r, TYPE, v);
+      }
+      cluster.sync();  // nobody's sums are read any more
+    }
   }
 }
 
@@ -345,27 +644,72 @@ crvq_status make_q4(const crvq_q4_matrix* m, Q4View* out) {
 }
 
 template <int TYPE, int GROUP, int NT, int RT>
-crvq_status launch_matvec(const MatvecQ4& a, cudaStream_t stream) {
+crvq_status launch_matvec(MatvecQ4& a, cudaStream_t stream) {
+  using S = MatvecShape<TYPE, GROUP, NT, RT>;
   auto kernel = q4_matvec_kernel<TYPE, GROUP, NT, RT>;
-  constexpr size_t smem = (size_t)kQWarps * 8 * NT * 16 * RT * sizeof(float);
+  a.cols = a.b <= 8 ? a.b : 8 * NT;
+  const int64_t tiles = ceil_div(a.m.M, 16 * RT), sms = sm_count();
+  const int64_t steps = ceil_div(a.m.N, kStep);
+  if (steps > (1 << 24)) return fail(CRVQ_ERR_UNSUPPORTED, "N = %lld is too large", (long long)a.m.N);
+  // Slices, and the tiles whose sums are held at a time: the choice with the least (tile, step) pairs of one row
+  // tile on the busiest SM, with what else costs time in such pairs (about 50 ns): laying out inputs a
+  // third per step and column, ten per chunk and group, 20 per group of a cluster. Clusters that are resident
+  // at one CTA per SM: 152, 76, 36 and 15 (of 1, 2, 4 and 8).
+  int slices = 1;
+  int64_t clusters = 0;
+  double best = 0;
+  for (int n = 1; n <= kMaxSlices && n <= steps; n *= 2) {
+    const int64_t slots = std::max<int64_t>(1, n == 8 ? sms * 4 / 5 / 8 : n == 4 ? sms * 18 / 19 / 4 : sms / n);
+    const int64_t own = ceil_div(tiles, slots), st = ceil_div(steps, n);
+    for (int64_t parts = 1; parts <= own; parts = parts < 8 ? parts + 1 : 2 * parts) {
+      const int64_t group = ceil_div(own, parts), chunk = std::min(st, S::chunk(group, a.cols));
+      if (chunk < 1) continue;
+      const int64_t chunks = ceil_div(st, chunk), groups = ceil_div(own, group);
+      const double pairs = (double)ceil_div(group * chunk, S::kWarps) * S::kWarps * RT * (double)(chunks * groups);
+      const double cost = pairs + 0.33 * (double)st * a.cols * (chunks > 1 ? (double)groups : 1.0) +
+                          10.0 * (double)(chunks * groups) + (n > 1 ? 20.0 * (double)groups : 0.0);
+      if (clusters == 0 || cost < best) {
+        best = cost;
+        slices = n;
+        clusters = std::min(tiles, slots);
+        a.group = (int)group;
+        a.chunk = (int)chunk;
+      }
+    }
+  }
+  if (clusters == 0) return fail(CRVQ_ERR_UNSUPPORTED, "matrix too large");
+  const size_t smem = S::smem(a.chunk, a.group, a.cols);
   CRVQ_TRY(smem_limit((const void*)kernel, smem));
-  const int64_t grid = ceil_div(a.m.M, 16 * RT);
-  if (grid >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many rows");
   ProfScope ps("q4_matvec", stream, (double)a.m.M * a.m.N * a.b);
-  CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)grid), dim3(kQThreads), smem, stream, a));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(clusters * slices));
+  cfg.blockDim = dim3(32 * S::kWarps);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)slices;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = slices > 1 ? 2 : 1;
+  CRVQ_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }
 
 template <int TYPE, int GROUP>
-crvq_status pick_inputs(const MatvecQ4& a, cudaStream_t stream) {
-  if (a.b <= 8) return launch_matvec<TYPE, GROUP, 1, 1>(a, stream);
-  if (a.b <= 16) return launch_matvec<TYPE, GROUP, 2, 1>(a, stream);
-  return launch_matvec<TYPE, GROUP, 4, 1>(a, stream);
+crvq_status pick_inputs(MatvecQ4& a, cudaStream_t stream) {
+  // more inputs take more of shared memory's bandwidth: two row tiles then share what is read of them
+  if (a.b <= 8) return launch_matvec<TYPE, GROUP, 1, 2>(a, stream);
+  if (a.b <= 16) return launch_matvec<TYPE, GROUP, 2, 2>(a, stream);
+  return launch_matvec<TYPE, GROUP, 4, 2>(a, stream);
 }
 
 template <int TYPE>
-crvq_status pick_group(const MatvecQ4& a, int group, cudaStream_t stream) {
+crvq_status pick_group(MatvecQ4& a, int group, cudaStream_t stream) {
   if (group == 32) return pick_inputs<TYPE, 32>(a, stream);
   if (group == 64) return pick_inputs<TYPE, 64>(a, stream);
   return pick_inputs<TYPE, 128>(a, stream);
@@ -388,7 +732,6 @@ crvq_status matvec(const crvq_q4_matrix* m, const void* X, int64_t ldx, int64_t 
   a.Y = Y;
   a.ldy = ldy;
   a.b = (int)b;
-  a.type = type;
   a.vec_w = ((uintptr_t)m->codes & 15u) == 0 && m->ld_codes % 16 == 0;
   a.vec_x = ((uintptr_t)X & 15u) == 0 && (b == 1 || ldx * (int64_t)wide % 16 == 0);
   if (type == CRVQ_F32) return pick_group<CRVQ_F32>(a, m->group, stream);
