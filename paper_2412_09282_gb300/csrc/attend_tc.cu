@@ -1,0 +1,585 @@
+// Attention over the paged 8-bit cache for many queries per sequence (chunks of prompts), on tcgen05.
+//
+// A unit is 256 columns (query token, query head) of one kv head: two groups of 128 rows, the lanes of
+// tensor memory. Per tile of 128 tokens and group X:
+//   S_X = Q_X K^T (fp16 x fp16 codes, fp32 in tensor memory), softmax in registers, P_X = weights in fp16 over
+//   S_X's own columns, O_X += P_X V (P_X read from tensor memory).
+// Twelve warps and one: two softmax groups of four warps (thread = row), four warps that turn the tile's codes into
+// fp16 operands (exact), one that issues the products. While one group's softmax runs, the other group's
+// products do: the tensor core and the softmax each take about half of the time of a tile.
+//   Keys and values have one layout, core matrices of 8 tokens x 8 channels: K-major for Q K^T, and
+// MN-major (channels along N) for P V, so values need no transposition.
+//   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
+// exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
+// only when a row's maximum grows by more than 2^8 (weights are then at most 2^14 in fp16) or ref grows.
+// Work is split like attend.cu's: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
+#include "attend.cuh"
+#include "tc_ops.cuh"
+
+namespace crvq {
+
+namespace {
+
+constexpr int kRows = 128;                // rows of a group
+constexpr int kUnit = 2 * kRows;          // columns of a unit
+constexpr int kKeys = 128;                // tokens of a tile
+constexpr int kTcThreads = 13 * 32;
+constexpr float kTcWeight = 64.f;         // weights are scaled by it (and up to 2^8 more before a rescale)
+constexpr float kTcLogWeight = 6.f;
+constexpr float kLazy = 8.f;
+constexpr uint32_t kTmemCols = 512;       // S_0, S_1 at 0, 128; O_0, O_1 at 256, 384
+
+template <int D>
+struct TcShape {
+  static_assert(kTile<D> == kKeys, "the line's tiles are this kernel's");
+  static constexpr int kQ = kRows * D * 2;
+  static constexpr int kSide = kKeys * D * 2;  // keys or values of a tile
+  static constexpr uint32_t kBand = D * 16;    // bytes of 8 tokens (rows)
+  static constexpr size_t kSmem = 2 * kQ + 4 * kSide + 128;
+  static constexpr int kSlot = kUnit * (D + 2);
+};
+
+// Byte offset of the 16-byte piece c (8 channels) of row r.
+template <int D>
+__device__ __forceinline__ uint32_t piece(int r, int c) {
+  return (uint32_t)(r >> 3) * TcShape<D>::kBand + c * 128 + (r & 7) * 16;
+}
+
+// kind::f16, fp16 operands, fp32 accumulator; bn: B is MN-major.
+constexpr uint32_t idesc_f16(int M, int N, bool bn) {
+  return (1u << 4) | ((bn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Bounded wait; false once any wait of the CTA has run out.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* dead, unsigned* err) {
+  const uint32_t b = tc::smem_u32(bar);
+  if (tc::mbar_try_wait(b, parity)) return true;
+  const unsigned long long t0 = tc::globaltimer();
+  while (!tc::mbar_try_wait(b, parity)) {
+    if (*dead) return false;
+    if (tc::globaltimer() - t0 > tc::kWaitNs) {
+      raise_error(err, ERRBIT_TIMEOUT);
+      *dead = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// Sixteen codes of a token as fp16, to two neighbouring pieces.
+template <int FMT>
+__device__ __forceinline__ void store_codes(char* dst, const uint4& u) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint32_t h[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h[2 * i] = codes2<FMT, 0>(w[i]);
+    h[2 * i + 1] = codes2<FMT, 1>(w[i]);
+  }
+  *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
+}
+
+// A share's part of a unit.
+struct Part {
+  Unit u;
+  int t_end;
+  int col0, n_cols;
+  int some_b, some_e;   // keys that some column sees
+  int every_b, every_e; // keys that every column sees
+  int first, n;         // tokens before the first tile that holds such a key; tiles
+};
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kTcThreads, 1)
+attend_tc_kernel(const __grid_constant__ AttendArgs a) {
+  using S = TcShape<D>;
+  extern __shared__ __align__(128) char sm[];
+  __shared__ __align__(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2],
+      q_full[2], all_done;
+  __shared__ float sk_s[2][8], sv_s[2][8], lg_s[2][8];  // scales of a tile's blocks, log2 of the values'
+  __shared__ int live_s[2][8];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int dead_s;
+  volatile int* dead = &dead_s;
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Line<D, kUnit> line(a);
+  const int64_t total = line.total;
+  const int shares = (int)min((int64_t)a.shares, total);
+  if ((int)blockIdx.x >= shares) return;
+  const int64_t w1 = share_begin(total, blockIdx.x + 1, shares);
+
+  if (warp == 12) tc::tmem_alloc(&tmem_slot, kTmemCols);
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(tc::smem_u32(&k_full[i]), 128);
+      tc::mbar_init(tc::smem_u32(&k_empty[i]), 1 + 8);  // the products, and every softmax warp (scales)
+      tc::mbar_init(tc::smem_u32(&v_full[i]), 128);
+      tc::mbar_init(tc::smem_u32(&v_empty[i]), 1);
+      tc::mbar_init(tc::smem_u32(&s_full[i]), 1);
+      tc::mbar_init(tc::smem_u32(&p_full[i]), 128);
+      tc::mbar_init(tc::smem_u32(&pv_done[i]), 1);
+      tc::mbar_init(tc::smem_u32(&q_full[i]), 128);
+    }
+    tc::mbar_init(tc::smem_u32(&all_done), 1);
+    dead_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  char* q_sm = sm;
+  char* k_sm = sm + 2 * S::kQ;
+  char* v_sm = k_sm + 2 * S::kSide;
+
+  // The parts of this share, in order (whole warps).
+  int64_t w = share_begin(total, blockIdx.x, shares);
+  auto next_part = [&](Part& p) {
+    while (w < w1) {
+      p.u = line.locate(a, w);
+      const Seq& s = p.u.s;
+      const int64_t tile0 = p.u.begin + kStart, unit_end = tile0 + s.tiles;
+      p.t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
+      w = min(unit_end, w1);
+      if (p.u.tile >= p.t_end) continue;
+      p.col0 = p.u.cg * kUnit;
+      p.n_cols = min(kUnit, s.n * a.group - p.col0);
+      const int pos0 = s.len - s.n + p.col0 / a.group, pos1 = s.len - s.n + (p.col0 + p.n_cols - 1) / a.group;
+      p.some_e = a.causal ? min(s.len, pos1 + 1) : s.len;
+      p.some_b = a.window > 0 ? max(0, pos0 - a.window + 1) : 0;
+      p.every_e = a.causal ? min(s.len, pos0 + 1) : s.len;
+      p.every_b = a.window > 0 ? max(0, pos1 - a.window + 1) : 0;
+      const int t0 = max(p.u.tile, p.some_b / kKeys - s.lo);
+      const int t1 = min(p.t_end, (max(0, p.some_e) + kKeys - 1) / kKeys - s.lo);
+      p.first = (s.lo + t0) * kKeys;
+      p.n = p.some_b < p.some_e ? max(0, t1 - t0) : 0;
+      return true;
+    }
+    return false;
+  };
+  Part p;
+  bool ok = true;
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax: thread = row of group X
+    const int X = warp >> 2, row = tid & (kRows - 1);
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + lanes + X * 128, o_at = tmem + lanes + 256 + X * 128;
+    char* q_mine = q_sm + X * S::kQ;
+    uint32_t tile_no = 0, mine_no = 0;  // tiles of the share; of those that this group works on
+    while (ok && next_part(p)) {
+      const int r = X * kRows + row, c = p.col0 + r;
+      const bool valid = r < p.n_cols, active = X == 0 || p.n_cols > kRows;
+      const int j = valid ? c / a.group : 0, h = p.u.h * a.group + (valid ? c % a.group : 0);
+      const int pos = p.u.s.len - p.u.s.n + j;
+      const int kb = a.window > 0 ? max(0, pos - a.window + 1) : 0, ke = a.causal ? min(p.u.s.len, pos + 1) : p.u.s.len;
+      float f = 0.f;
+      if (active && p.n > 0) {
+        // the row of Q relative to the power of two at its largest element, in fp16 (sign of the scale included)
+        const int64_t src = (p.u.s.first + j) * a.q.ld_tok + h * a.q.ld_head;
+        float top = 0.f;
+        uint4 raw[D / 8];
+#pragma unroll
+        for (int e = 0; e < D / 8; ++e) {
+          float x[8];
+          if (valid) {
+            load8(a.q.data, src + 8 * e, a.q.type, a.vec_q, x);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+          raw[e] = make_uint4(pack2(x[0], x[1], a.q.type), pack2(x[2], x[3], a.q.type), pack2(x[4], x[5], a.q.type),
+                              pack2(x[6], x[7], a.q.type));
+        }
+        const uint32_t ex = __float_as_uint(top) >> 23;
+        const bool plain = ex == 0 || ex == 255;
+        float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
+        f = (plain ? 1.f : __uint_as_float(ex << 23)) * fabsf(a.scale);
+        if (a.scale < 0.f) inv = -inv;
+#pragma unroll
+        for (int e = 0; e < D / 8; ++e) {
+          const uint32_t u[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float2 x;
+            if (a.q.type == CRVQ_BF16)
+              x = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+            else
+              x = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            o[i] = half2_bits(x.x * inv, x.y * inv);
+          }
+          *reinterpret_cast<uint4*>(q_mine + piece<D>(row, e)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        tc::fence_async_smem();
+        tc::mbar_arrive(tc::smem_u32(&q_full[X]));
+      }
+      float m = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f;
+      for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
+        const int buf = tile_no & 1;
+        if (active) {
+          ok = wait_for(&s_full[X], mine_no & 1, dead, a.err);
+          tc::tc_fence_after();
+        }
+        ok = ok && wait_for(&k_full[buf], (tile_no >> 1) & 1, dead, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (active) {
+          const int tok = p.first + i * kKeys;
+          float sv_top = 0.f;
+          bool all_live = true;
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            sv_top = fmaxf(sv_top, sv_s[buf][b]);
+            all_live = all_live && live_s[buf][b];
+          }
+          const bool whole = all_live && tok >= p.every_b && tok + kKeys <= p.every_e;
+          auto mask16 = [&](float* v, int b) {  // block b's scores that this row does not see
+            const int t0 = tok + 16 * b;
+            const bool in = live_s[buf][b];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (!in || t0 + e < kb || t0 + e >= ke) v[e] = -INFINITY;
+          };
+          // the row's maximum over the tile
+          float mt = -INFINITY;
+#pragma unroll 1
+          for (int ch = 0; ch < 4; ++ch) {
+            float v[32];
+            tc::tmem_ld32(s_at + ch * 32, v);
+#pragma unroll
+            for (int b2 = 0; b2 < 2; ++b2) {
+              float* x = v + 16 * b2;
+              const float sk = sk_s[buf][2 * ch + b2];
+              if (sk < 0.f) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = -x[e];
+              }
+              if (!whole) mask16(x, 2 * ch + b2);
+              float t = x[0];
+#pragma unroll
+              for (int e = 1; e < 16; ++e) t = fmaxf(t, x[e]);
+              if (t != -INFINITY) mt = fmaxf(mt, t * (fabsf(sk) * f));
+            }
+          }
+          float up = ref;
+          if (sv_top > ref || i == 0)
+            up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u, 0x7f000000u)),
+                       7.7037197775489434e-34f);
+          const bool need = mt > m + kLazy || (m == -INFINITY && mt > m) || up > ref;
+          if (i == 0) {
+            m = mt;
+          } else if (__any_sync(0xffffffffu, need)) {
+            ok = wait_for(&pv_done[X], (mine_no - 1) & 1, dead, a.err);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const float mn = need ? fmaxf(m, mt) : m;
+            const float back = m == mn ? 1.f : pow2(m - mn), fac = back * (ref / up);
+            m = mn;
+            l *= back;
+#pragma unroll 1
+            for (int ch = 0; ch < D / 32; ++ch) {
+              float v[32];
+              tc::tmem_ld32(o_at + ch * 32, v);
+              uint32_t u[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(v[e] * fac);
+              tc::tmem_st32_wait(o_at + ch * 32, u);
+            }
+          }
+          if (up != ref) {
+            ref = up;
+            lref = (float)((int)(__float_as_uint(ref) >> 23) - 127);
+          }
+          // weights, over S's own columns (a chunk's scores are in registers before they are overwritten)
+          const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            uint32_t packed[32];
+#pragma unroll
+            for (int c2 = 0; c2 < 2; ++c2) {
+              float v[32];
+              tc::tmem_ld32(s_at + half * 64 + c2 * 32, v);
+#pragma unroll
+              for (int b2 = 0; b2 < 2; ++b2) {
+                float* x = v + 16 * b2;
+                const int b = 4 * half + 2 * c2 + b2;
+                const float sc = sk_s[buf][b] * f, lw = fmaxf(lg_s[buf][b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
+                float sum = 0.f;
+                if (whole) {
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) {
+                    x[e] = pow2(fmaf(x[e], sc, bias));
+                    sum += x[e];
+                  }
+                } else {
+                  const int t0 = tok + 16 * b;
+                  const bool in = live_s[buf][b];
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) {
+                    x[e] = in && t0 + e >= kb && t0 + e < ke ? pow2(fmaf(x[e], sc, bias)) : 0.f;
+                    sum += x[e];
+                  }
+                }
+                l = fmaf(sum, pow2(-lw), l);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) packed[16 * c2 + 8 * b2 + e] = half2_bits(x[2 * e], x[2 * e + 1]);
+              }
+            }
+            tc::tmem_st32_wait(s_at + half * 32, packed);
+          }
+          tc::tc_fence_before();
+          tc::mbar_arrive(tc::smem_u32(&p_full[X]));
+          ++mine_no;
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&k_empty[buf]));
+      }
+      if (!ok) break;
+      // the part's rows
+      const bool complete = p.u.tile == 0 && p.t_end == p.u.s.tiles;
+      if (active && p.n > 0) {
+        ok = wait_for(&pv_done[X], (mine_no - 1) & 1, dead, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc::tc_fence_after();
+      }
+      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+      const float fac = p.n > 0 ? ref * (1.f / kTcWeight) * (complete ? inv : 1.f) : 0.f;
+      float* part = a.part + (int64_t)(2 * blockIdx.x + (p.u.tile == 0 ? 1 : 0)) * S::kSlot;
+      const int64_t dst = (p.u.s.first + j) * a.o.ld_tok + h * a.o.ld_head;
+      if (active) {
+#pragma unroll 1
+        for (int ch = 0; ch < D / 32; ++ch) {
+          float v[32];
+          if (p.n > 0) {
+            tc::tmem_ld32(o_at + ch * 32, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] *= fac;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = 0.f;
+          }
+          if (valid) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (complete)
+                store8(a.o.data, dst + ch * 32 + 8 * e, a.o.type, a.vec_o, v + 8 * e);
+              else
+                store8(part + r * D + ch * 32 + 8 * e, 0, CRVQ_F32, true, v + 8 * e);
+            }
+          }
+        }
+        tc::tc_fence_before();  // (O is overwritten after this group's next arrival)
+        if (valid) {
+          if (!complete) {
+            part[kUnit * D + r] = m;
+            part[kUnit * D + kUnit + r] = l;
+          } else if (a.lse) {
+            a.lse[(p.u.s.first + j) * a.q.heads + h] = l > 0.f ? (m + log2f(l)) / kLog2e : (l == 0.f ? -INFINITY : l);
+          }
+        }
+      }
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------ codes to operands: 32 tokens per warp
+    const int cw = warp - 8;
+    constexpr int UH = D / 64;
+    uint4 kr[4][UH], vr[4][UH];
+    int64_t at[2], at_n[2];
+    float sk[2], sv[2], sk_n[2], sv_n[2];
+    uint32_t tile_no = 0;
+    while (ok && next_part(p)) {
+      const int len = p.u.s.len, tok0 = p.first + 32 * cw;
+      auto look_up = [&](int i) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int tok = tok0 + i * kKeys + 16 * b;
+          at_n[b] = -1;
+          sk_n[b] = sv_n[b] = 0.f;
+          if (i < p.n && tok < p.some_e && tok + kCacheBlock > p.some_b) {
+            const int64_t page = seq_page(a.c, p.u.b, tok / a.c.page, a.err);
+            if (page >= 0) {
+              const int in = tok % a.c.page;
+              at_n[b] = page * a.c.page_stride + ((int64_t)p.u.h * a.c.page + in) * D;
+              const int64_t at_s = (page * a.c.n_kv + p.u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock;
+              sk_n[b] = __ldg(a.c.ks + at_s);
+              sv_n[b] = __ldg(a.c.vs + at_s);
+            }
+          }
+        }
+      };
+      // lane: rows (lane & 7) of each 8, 16-byte units (lane >> 3) of each 4
+      auto load = [&](const uint8_t* base, int i, bool values, uint4 (&x)[4][UH]) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int r = 8 * g + (lane & 7);
+          const bool in = at_n[g >> 1] >= 0 && !(values && tok0 + i * kKeys + r >= len);
+#pragma unroll
+          for (int u = 0; u < UH; ++u)
+            x[g][u] = in ? __ldg(reinterpret_cast<const uint4*>(base + at_n[g >> 1] + (8 * (g & 1) + (lane & 7)) * D +
+                                                                (4 * u + (lane >> 3)) * 16))
+                         : make_uint4(0, 0, 0, 0);
+        }
+      };
+      auto store = [&](char* dst, const uint4 (&x)[4][UH]) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int u = 0; u < UH; ++u)
+            store_codes<FMT>(dst + piece<D>(32 * cw + 8 * g + (lane & 7), 2 * (4 * u + (lane >> 3))), x[g][u]);
+      };
+      auto take = [&]() {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          at[b] = at_n[b];
+          sk[b] = sk_n[b];
+          sv[b] = sv_n[b];
+        }
+      };
+      if (p.n > 0) {
+        look_up(0);
+        load(a.c.K, 0, false, kr);
+        load(a.c.V, 0, true, vr);
+        take();
+        look_up(1);
+      }
+      for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
+        const int buf = tile_no & 1;
+        const uint32_t ph = ((tile_no >> 1) & 1) ^ 1;
+        ok = wait_for(&k_empty[buf], ph, dead, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane < 2) {
+          sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
+          sv_s[buf][2 * cw + lane] = lane ? sv[1] : sv[0];
+          lg_s[buf][2 * cw + lane] = log2f(lane ? sv[1] : sv[0]);
+          live_s[buf][2 * cw + lane] = (lane ? at[1] : at[0]) >= 0;
+        }
+        store(k_sm + buf * S::kSide, kr);
+        tc::fence_async_smem();
+        __syncwarp();
+        tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
+        if (i + 1 < p.n) load(a.c.K, i + 1, false, kr);
+        ok = wait_for(&v_empty[buf], ph, dead, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        store(v_sm + buf * S::kSide, vr);
+        tc::fence_async_smem();
+        tc::mbar_arrive(tc::smem_u32(&v_full[buf]));
+        if (i + 1 < p.n) load(a.c.V, i + 1, true, vr);
+        take();
+        look_up(i + 2);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ products: one thread issues
+    constexpr uint32_t kQk = idesc_f16(kRows, kKeys, false), kPv = idesc_f16(kRows, D, true);
+    const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
+    uint32_t tile_no = 0, mine_no[2] = {0, 0}, q_no[2] = {0, 0};
+    while (next_part(p)) {
+      if (lane == 0 && ok && p.n > 0) {
+        const int groups = p.n_cols > kRows ? 2 : 1;
+        auto scores = [&](int X, int buf) {  // S_X = Q_X K^T
+          const uint32_t d = tmem + X * 128;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+            mma_ss(d, tc::smem_desc(q_at + X * S::kQ + ks * 256, 128, S::kBand),
+                   tc::smem_desc(k_at + buf * S::kSide + ks * 256, 128, S::kBand), kQk, ks > 0);
+          tc::mma_commit(tc::smem_u32(&s_full[X]));
+        };
+        for (int X = 0; X < groups && ok; ++X) {
+          ok = wait_for(&q_full[X], q_no[X] & 1, dead, a.err);
+          ++q_no[X];
+        }
+        ok = ok && wait_for(&k_full[tile_no & 1], (tile_no >> 1) & 1, dead, a.err);
+        if (ok) {
+          tc::tc_fence_after();
+          for (int X = 0; X < groups; ++X) scores(X, tile_no & 1);
+          tc::mma_commit(tc::smem_u32(&k_empty[tile_no & 1]));
+        }
+        for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
+          const int buf = tile_no & 1, nbuf = buf ^ 1;
+          ok = wait_for(&v_full[buf], (tile_no >> 1) & 1, dead, a.err);
+          for (int X = 0; X < groups && ok; ++X) {
+            ok = wait_for(&p_full[X], mine_no[X] & 1, dead, a.err);
+            if (!ok) break;
+            tc::tc_fence_after();
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+              mma_ts(tmem + 256 + X * 128, tmem + X * 128 + ks * 8,
+                     tc::smem_desc(v_at + buf * S::kSide + ks * 2 * S::kBand, S::kBand, 128), kPv, i > 0 || ks > 0);
+            tc::mma_commit(tc::smem_u32(&pv_done[X]));
+            if (X == groups - 1) tc::mma_commit(tc::smem_u32(&v_empty[buf]));
+            if (i + 1 < p.n) {
+              if (X == 0) ok = wait_for(&k_full[nbuf], ((tile_no + 1) >> 1) & 1, dead, a.err);
+              // the weights lie where the next scores go
+              ok = ok && wait_for(&pv_done[X], mine_no[X] & 1, dead, a.err);
+              if (!ok) break;
+              tc::tc_fence_after();
+              scores(X, nbuf);
+              if (X == groups - 1) tc::mma_commit(tc::smem_u32(&k_empty[nbuf]));
+            }
+            ++mine_no[X];
+          }
+        }
+      }
+      __syncwarp();
+    }
+    if (lane == 0) {  // whatever was issued has ended before tensor memory is freed
+      tc::mma_commit(tc::smem_u32(&all_done));
+      tc::mbar_wait(tc::smem_u32(&all_done), 0, a.err);
+    }
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  if (warp == 12) tc::tmem_dealloc(tmem, kTmemCols);
+}
+
+template <int D, int FMT>
+crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
+  using S = TcShape<D>;
+  auto kernel = attend_tc_kernel<D, FMT>;
+  CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
+  a.shares = sm_count();
+  Scratch mem;
+  CRVQ_TRY(mem.alloc((size_t)2 * a.shares * S::kSlot * sizeof(float), stream));
+  a.part = mem.as<float>();
+  ProfScope ps("cache_attention", stream, (double)a.rows.n_tok * a.q.heads * D);
+  CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)a.shares), dim3(kTcThreads), S::kSmem, stream, a));
+  CRVQ_LAUNCHED();
+  return launch_join<D, kUnit>(a, stream);
+}
+
+}  // namespace
+
+crvq_status launch_attend_many(AttendArgs& a, int D, int format, cudaStream_t stream) {
+  if (D == 64)
+    return format == CRVQ_KV_INT8 ? launch_tc<64, CRVQ_KV_INT8>(a, stream) : launch_tc<64, CRVQ_KV_E4M3>(a, stream);
+  return format == CRVQ_KV_INT8 ? launch_tc<128, CRVQ_KV_INT8>(a, stream) : launch_tc<128, CRVQ_KV_E4M3>(a, stream);
+}
+
+}  // namespace crvq

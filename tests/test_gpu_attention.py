@@ -36,7 +36,7 @@ def _check(host, gpu, q, counts, dtype, ragged=True, scale=None, causal=True, wi
     n = int(max(host["lens"]))
     per = 2.0 ** -23 + (2.0 ** -21 / (d + 16) if dtype == "f32" else 0.0)
     rel = 2 * U.WEIGHT_ROUND[dtype] + 2.0 ** -21 * n / 16 + 4 * per * shake[..., None] + 2.0 ** -19
-    bound = U.OUT_ROUND[dtype] * np.abs(ref) + rel * mass + 1e-30
+    bound = U.OUT_ROUND[dtype] * np.abs(ref) + rel * mass + (2.0 ** -25 if dtype == "f16" else 1e-30)  # (fp16's subnormals)
     got = U.exactly(out).astype(np.float64)
     empty = ~np.isfinite(lse_ref)
     assert np.all(np.abs(got - ref) <= bound), float((np.abs(got - ref) / bound).max())
@@ -151,3 +151,64 @@ def test_refusals():
     with pytest.raises(ValueError):
         P.crvq_cache_attention(gpu, torch.ones((2, 4, 128), device="cuda"))
     assert P.crvq_cache_attention(gpu, q[:0], q_off=torch.zeros(3, dtype=torch.int32, device="cuda")).shape[0] == 0
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 70), (False, 0)])
+@pytest.mark.parametrize("d,page,n_kv,group,lens,counts", [
+    (128, 64, 2, 2, [300, 129], [150, 129]),        # two groups of rows, whole prompts, ends inside tiles
+    (64, 16, 1, 8, [40, 700, 5, 0], [40, 33, 9, 2]),  # a short unit, more queries than keys, an empty sequence
+    (128, 48, 1, 1, [1000], [700]),                 # three units of one sequence
+])
+def test_chunks_of_prompts(fmt, dtype, causal, window, d, page, n_kv, group, lens, counts):
+    host, gpu = U.make(40, lens, page, n_kv, d, fmt, page_gap=1)
+    q = _queries(41, sum(counts), n_kv * group, d, dtype, 1.5)
+    _check(host, gpu, q, counts, dtype, causal=causal, window=window, gap=8 if group == 2 else 3)
+
+
+def test_chunks_with_growing_maxima_and_scales_and_not_finite_queries():
+    """Keys and value scales that grow along the sequence (outputs are rescaled many times), and rows with
+    NaN and infinities beside finite ones."""
+    import paper_2412_09282_gb300 as P
+    host, _ = U.make(42, [900], 16, 1, 128, "int8")
+    order = host["pages"][0, :57]
+    ramp = np.exp(np.linspace(-2.0, 1.5, 57)).astype(np.float32)
+    host["k_scale"][order, 0, 0] *= ramp
+    host["v_scale"][order, 0, 0] *= np.exp(np.linspace(-8, 8, 57)).astype(np.float32)
+    host["v_scale"][order[20], 0, 0] = 0.0
+    gpu = U.on_gpu(host, "int8")
+    q = _queries(43, 130, 2, 128, "f16", 1.0)
+    _check(host, gpu, q, [130], "f16")
+    ref = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f16")))
+    q[7, 1, 3], q[100, 0, 5] = np.nan, np.inf
+    out = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f16")))
+    again = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f16")))
+    P.crvq_sync()
+    same = np.ones((130, 2), bool)
+    same[7, 1] = same[100, 0] = False
+    assert np.array_equal(out[same], ref[same]) and np.isnan(out[~same]).all()
+    assert np.array_equal(out, again, equal_nan=True)
+
+
+def test_chunks_report_bad_pages_and_skip_them():
+    import paper_2412_09282_gb300 as P
+    host, _ = U.make(44, [400], 64, 1, 64, "int8")
+    host["pages"][0, 2] = 1000
+    gpu = U.on_gpu(host, "int8")
+    q = _queries(45, 200, 1, 64, "bf16")
+    out = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "bf16")))
+    with pytest.raises(P.CrvqError) as e:
+        P.crvq_sync()
+    assert e.value.status == -7
+    assert np.isfinite(out).all()
+    # what is skipped counts as not cached: the same softmax without the tokens 128 .. 191
+    K, V = (np.delete(np.concatenate([D.values(host, n, 0, 0, 128), np.zeros((64, 1, 64)), D.values(host, n, 0, 192, 400)]),
+                      slice(128, 192), 0) for n in ("K", "V"))
+    t = np.delete(np.arange(400), slice(128, 192))
+    for j in (0, 57, 199):
+        z = (K[:, 0] @ q[j, 0].astype(np.float64)) / 8
+        z[t > 200 + j] = -np.inf
+        w = np.exp(z - z.max())
+        ref = (w / w.sum()) @ V[:, 0]
+        assert np.abs(out[j, 0] - ref).max() <= 2.0 ** -7 * np.abs(V).max()
