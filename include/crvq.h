@@ -477,7 +477,7 @@ typedef struct crvq_heads {
  * A paged cache of n_seq sequences. Page p of kv head h holds `page` tokens of head_dim codes:
  *   code of token slot t: K[p * page_stride + (h * page + t) * head_dim + c]   (V the same),
  *   its scale:            k_scale[(p * n_kv + h) * (page / 16) + t / 16],
- * one fp32 scale per 16 tokens ("block") and head; the value is code * scale. Token i of sequence b
+ * one fp32 scale per 16 tokens ("block") and head, not negative; the value is code * scale. Token i of sequence b
  * lies in slot i % page of page pages[b * ld_pages + i / page]. Only pages that hold tokens are
  * looked up. Entries outside [0, n_pages) and lengths outside [0, max_pages * page] are skipped and
  * reported as CRVQ_ERR_DEVICE by crvq_sync (what is skipped counts as not cached).

@@ -196,7 +196,7 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
 // Joins the parts of units that lie in several shares, in the order of the shares. Two forms:
 //   BY_UNIT (few units, so many parts each): a block per unit (x) and column (y), whose warps take every
 //     eighth part;
-//   otherwise (few parts each): blocks (y: eight columns each) per boundary between shares x and x + 1, if
+//   otherwise (few parts each): blocks (y: some of the columns each) per boundary between shares x and x + 1, if
 //     it is the first that cuts its unit; a warp per column.
 constexpr int kJoinWarps = 8;
 
@@ -235,7 +235,8 @@ attend_join_kernel(const __grid_constant__ AttendArgs a) {
   // part p: its share's last unit (p = 0), or its first
   auto slot = [&](int p) { return part + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * kSlot; };
 
-  for (int col = BY_UNIT ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp; col < n_cols; col += COLS) {
+  for (int col = BY_UNIT ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp; col < n_cols;
+       col += BY_UNIT ? COLS : (int)gridDim.y * kJoinWarps) {
     float M = -INFINITY, L = 0.f, o[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] = 0.f;
@@ -323,8 +324,8 @@ crvq_status launch_join(const AttendArgs& a, cudaStream_t stream) {
   if (units * kJoinWarps <= a.shares)
     CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, true>, dim3((unsigned)units, COLS), threads, 0, stream, a));
   else
-    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, false>, dim3((unsigned)a.shares - 1, COLS / kJoinWarps), threads, 0,
-                         stream, a));
+    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, false>, dim3((unsigned)a.shares - 1, COLS > 32 ? 8 : COLS / kJoinWarps),
+                         threads, 0, stream, a));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }

@@ -11,7 +11,7 @@
 // MN-major (channels along N) for P V, so values need no transposition.
 //   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
 // exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
-// only when a row's maximum grows by more than 2^8 (weights are then at most 2^14 in fp16) or ref grows.
+// only when a row's maximum grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows.
 // Work is split like attend.cu's: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
 #include "attend.cuh"
 #include "tc_ops.cuh"
@@ -24,7 +24,7 @@ constexpr int kRows = 128;                // rows of a group
 constexpr int kUnit = 2 * kRows;          // columns of a unit
 constexpr int kKeys = 128;                // tokens of a tile
 constexpr int kTcThreads = 13 * 32;
-constexpr float kTcWeight = 64.f;         // weights are scaled by it (and up to 2^8 more before a rescale)
+constexpr float kTcWeight = 64.f;         // weights are scaled by it, and up to 2^8 more before a rescale
 constexpr float kTcLogWeight = 6.f;
 constexpr float kLazy = 8.f;
 constexpr uint32_t kTmemCols = 512;       // S_0, S_1 at 0, 128; O_0, O_1 at 256, 384
@@ -50,19 +50,28 @@ constexpr uint32_t idesc_f16(int M, int N, bool bn) {
   return (1u << 4) | ((bn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// Issued by one lane of a whole warp (always the same): the operands are then the warp's, in uniform registers. From
+// a branch that only lane 0 took, an issue cost about 100 cycles, more than the product itself.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+      " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(tc::smem_u32(bar))
       : "memory");
 }
 
@@ -94,6 +103,22 @@ __device__ __forceinline__ void store_codes(char* dst, const uint4& u) {
   }
   *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
   *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
+}
+
+// Which of the 32 tokens from t0 on (two blocks) a row sees, as bits.
+__device__ __forceinline__ uint32_t seen32(int t0, const int* live, int kb, int ke) {
+  const int lo = min(max(kb - t0, 0), 32), hi = min(max(ke - t0, 0), 32);
+  const uint32_t below = hi == 32 ? 0xffffffffu : (1u << hi) - 1u, from = lo == 32 ? 0u : 0xffffffffu << lo;
+  return below & from & ((live[0] ? 0xffffu : 0u) | (live[1] ? 0xffff0000u : 0u));
+}
+
+// Stores 16 consecutive columns of this thread's lane (waited for by tcgen05.wait::st).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t r[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 
 // A share's part of a unit.
@@ -195,22 +220,32 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
       if (active && p.n > 0) {
         // the row of Q relative to the power of two at its largest element, in fp16 (sign of the scale included)
         const int64_t src = (p.u.s.first + j) * a.q.ld_tok + h * a.q.ld_head;
-        float top = 0.f;
         uint4 raw[D / 8];
+        if (valid && a.vec_q) {  // (all loads on their way before the first is used)
+          const uint4* row_q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.data) + src);
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) raw[e] = row_q[e];
+        } else {
+          const uint16_t* row_q = static_cast<const uint16_t*>(a.q.data) + src;
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              u[i] = valid ? row_q[8 * e + 2 * i] | (uint32_t)row_q[8 * e + 2 * i + 1] << 16 : 0u;
+            raw[e] = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+        }
+        // the largest magnitude, as bits (either type's order like integers); in fp32
+        uint32_t top2 = 0;
 #pragma unroll
         for (int e = 0; e < D / 8; ++e) {
-          float x[8];
-          if (valid) {
-            load8(a.q.data, src + 8 * e, a.q.type, a.vec_q, x);
-          } else {
+          const uint32_t u[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
-          raw[e] = make_uint4(pack2(x[0], x[1], a.q.type), pack2(x[2], x[3], a.q.type), pack2(x[4], x[5], a.q.type),
-                              pack2(x[6], x[7], a.q.type));
+          for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, u[i] & 0x7fff7fffu);
         }
+        const uint32_t top16 = max(top2 & 0xffffu, top2 >> 16);
+        const float top = a.q.type == CRVQ_BF16 ? __uint_as_float(top16 << 16) : __half2float(__ushort_as_half((uint16_t)top16));
         const uint32_t ex = __float_as_uint(top) >> 23;
         const bool plain = ex == 0 || ex == 255;
         float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
@@ -254,32 +289,37 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
             all_live = all_live && live_s[buf][b];
           }
           const bool whole = all_live && tok >= p.every_b && tok + kKeys <= p.every_e;
-          auto mask16 = [&](float* v, int b) {  // block b's scores that this row does not see
-            const int t0 = tok + 16 * b;
-            const bool in = live_s[buf][b];
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (!in || t0 + e < kb || t0 + e >= ke) v[e] = -INFINITY;
-          };
-          // the row's maximum over the tile
+          // The row's maximum over the tile, then (after the rescale) its weights, 32 columns at a time, in rolled
+          // loops: unrolled, the warps' different code overflowed the instruction caches.
           float mt = -INFINITY;
+          if (whole) {
 #pragma unroll 1
-          for (int ch = 0; ch < 4; ++ch) {
-            float v[32];
-            tc::tmem_ld32(s_at + ch * 32, v);
+            for (int half = 0; half < 2; ++half) {
+              uint32_t u[64];
+              tc::tmem_ld64_wait(s_at + half * 64, u);
 #pragma unroll
-            for (int b2 = 0; b2 < 2; ++b2) {
-              float* x = v + 16 * b2;
-              const float sk = sk_s[buf][2 * ch + b2];
-              if (sk < 0.f) {
+              for (int b = 0; b < 4; ++b) {
+                float t[8];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = -x[e];
+                for (int e = 0; e < 8; ++e)
+                  t[e] = fmaxf(__uint_as_float(u[16 * b + e]), __uint_as_float(u[16 * b + 8 + e]));
+#pragma unroll
+                for (int w2 = 4; w2 > 0; w2 >>= 1)
+#pragma unroll
+                  for (int e = 0; e < w2; ++e) t[e] = fmaxf(t[e], t[e + w2]);
+                mt = fmaxf(mt, t[0] * (sk_s[buf][4 * half + b] * f));
               }
-              if (!whole) mask16(x, 2 * ch + b2);
-              float t = x[0];
+            }
+          } else {
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
+              float v[32];
+              tc::tmem_ld32(s_at + ch * 32, v);
+              const uint32_t seen = seen32(tok + 32 * ch, &live_s[buf][2 * ch], kb, ke);
+              const float s0 = sk_s[buf][2 * ch] * f, s1 = sk_s[buf][2 * ch + 1] * f;
 #pragma unroll
-              for (int e = 1; e < 16; ++e) t = fmaxf(t, x[e]);
-              if (t != -INFINITY) mt = fmaxf(mt, t * (fabsf(sk) * f));
+              for (int e = 0; e < 32; ++e)
+                if (seen >> e & 1) mt = fmaxf(mt, v[e] * (e < 16 ? s0 : s1));
             }
           }
           float up = ref;
@@ -314,41 +354,54 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           }
           // weights, over S's own columns (a chunk's scores are in registers before they are overwritten)
           const float mm = m == -INFINITY ? 0.f : m;
+          if (whole) {
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            uint32_t packed[32];
+            for (int half = 0; half < 2; ++half) {
+              uint32_t u[64];
+              tc::tmem_ld64_wait(s_at + half * 64, u);
+              uint32_t packed[32];
 #pragma unroll
-            for (int c2 = 0; c2 < 2; ++c2) {
+              for (int b = 0; b < 4; ++b) {
+                const float lw = fmaxf(lg_s[buf][4 * half + b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
+                const float g = sk_s[buf][4 * half + b] * f;
+                float sum[4];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                  const float x = pow2(fmaf(__uint_as_float(u[16 * b + e]), g, bias));
+                  const float y = pow2(fmaf(__uint_as_float(u[16 * b + e + 1]), g, bias));
+                  sum[e / 2 & 3] = e < 8 ? x + y : sum[e / 2 & 3] + (x + y);
+                  packed[8 * b + e / 2] = half2_bits(x, y);
+                }
+                l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), pow2(-lw), l);
+              }
+              tmem_st16(s_at + half * 32, packed);
+              tmem_st16(s_at + half * 32 + 16, packed + 16);
+            }
+          } else {
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
               float v[32];
-              tc::tmem_ld32(s_at + half * 64 + c2 * 32, v);
+              tc::tmem_ld32(s_at + ch * 32, v);
+              uint32_t packed[16];
+              const uint32_t seen = seen32(tok + 32 * ch, &live_s[buf][2 * ch], kb, ke);
 #pragma unroll
-              for (int b2 = 0; b2 < 2; ++b2) {
-                float* x = v + 16 * b2;
-                const int b = 4 * half + 2 * c2 + b2;
-                const float sc = sk_s[buf][b] * f, lw = fmaxf(lg_s[buf][b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
+              for (int b = 0; b < 2; ++b) {
+                const float lw = fmaxf(lg_s[buf][2 * ch + b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
+                const float g = sk_s[buf][2 * ch + b] * f;
                 float sum = 0.f;
-                if (whole) {
 #pragma unroll
-                  for (int e = 0; e < 16; ++e) {
-                    x[e] = pow2(fmaf(x[e], sc, bias));
-                    sum += x[e];
-                  }
-                } else {
-                  const int t0 = tok + 16 * b;
-                  const bool in = live_s[buf][b];
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) {
-                    x[e] = in && t0 + e >= kb && t0 + e < ke ? pow2(fmaf(x[e], sc, bias)) : 0.f;
-                    sum += x[e];
-                  }
+                for (int e = 0; e < 16; ++e) {
+                  float& x = v[16 * b + e];
+                  x = seen >> (16 * b + e) & 1 ? pow2(fmaf(x, g, bias)) : 0.f;
+                  sum += x;
+                  if (e & 1) packed[8 * b + e / 2] = half2_bits(v[16 * b + e - 1], x);
                 }
                 l = fmaf(sum, pow2(-lw), l);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) packed[16 * c2 + 8 * b2 + e] = half2_bits(x[2 * e], x[2 * e + 1]);
               }
+              tmem_st16(s_at + ch * 16, packed);
             }
-            tc::tmem_st32_wait(s_at + half * 32, packed);
           }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           tc::tc_fence_before();
           tc::mbar_arrive(tc::smem_u32(&p_full[X]));
           ++mine_no;
@@ -368,8 +421,11 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
       const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
       const float fac = p.n > 0 ? ref * (1.f / kTcWeight) * (complete ? inv : 1.f) : 0.f;
       float* part = a.part + (int64_t)(2 * blockIdx.x + (p.u.tile == 0 ? 1 : 0)) * S::kSlot;
-      const int64_t dst = (p.u.s.first + j) * a.o.ld_tok + h * a.o.ld_head;
       if (active) {
+        // 32 columns at a time through this warp's rows of Q's memory (read whole by now), then rows by neighbouring
+        // lanes: a thread's own row, 16 bytes in each of 32 lines per store, took 9000 cycles
+        float* stage = reinterpret_cast<float*>(q_mine + (warp & 3) * (S::kQ / 4));
+        const int r0 = X * kRows + (warp & 3) * 32;  // this warp's first row
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
           float v[32];
@@ -381,13 +437,32 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = 0.f;
           }
-          if (valid) {
+          __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (complete)
-                store8(a.o.data, dst + ch * 32 + 8 * e, a.o.type, a.vec_o, v + 8 * e);
-              else
-                store8(part + r * D + ch * 32 + 8 * e, 0, CRVQ_F32, true, v + 8 * e);
+          for (int e = 0; e < 8; ++e)  // (16-byte units exchanged by the row: no bank conflicts)
+            *reinterpret_cast<float4*>(stage + lane * 32 + ((e ^ lane & 7) * 4)) =
+                make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          __syncwarp();
+          auto unit = [&](int rr, int e) {
+            return *reinterpret_cast<const float4*>(stage + rr * 32 + ((e ^ rr & 7) * 4));
+          };
+          if (!complete) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int rr = 4 * k + (lane >> 3);
+              if (r0 + rr < p.n_cols)
+                *reinterpret_cast<float4*>(part + (r0 + rr) * D + ch * 32 + (lane & 7) * 4) = unit(rr, lane & 7);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int rr = 8 * k + (lane >> 2), cc = p.col0 + r0 + rr;
+              if (r0 + rr < p.n_cols) {
+                const float4 x = unit(rr, 2 * (lane & 3)), y = unit(rr, 2 * (lane & 3) + 1);
+                const float o[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                store8(a.o.data, (p.u.s.first + cc / a.group) * a.o.ld_tok + (p.u.h * a.group + cc % a.group) * a.o.ld_head +
+                                     ch * 32 + (lane & 3) * 8, a.o.type, a.vec_o, o);
+              }
             }
           }
         }
@@ -494,63 +569,61 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
       }
     }
   } else {
-    // ------------------------------------------------------------------ products: one thread issues
+    // ------------------------------------------------------------------ products (the whole warp, one lane issues)
     constexpr uint32_t kQk = idesc_f16(kRows, kKeys, false), kPv = idesc_f16(kRows, D, true);
-    const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
+    const uint64_t q_desc = tc::smem_desc(tc::smem_u32(q_sm), 128, S::kBand);
+    const uint64_t k_desc = tc::smem_desc(tc::smem_u32(k_sm), 128, S::kBand);
+    const uint64_t v_desc = tc::smem_desc(tc::smem_u32(v_sm), S::kBand, 128);
     uint32_t tile_no = 0, mine_no[2] = {0, 0}, q_no[2] = {0, 0};
-    while (next_part(p)) {
-      if (lane == 0 && ok && p.n > 0) {
-        const int groups = p.n_cols > kRows ? 2 : 1;
-        auto scores = [&](int X, int buf) {  // S_X = Q_X K^T
-          const uint32_t d = tmem + X * 128;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && wait_for(bar, parity, dead, a.err);
+      ok = __all_sync(0xffffffffu, ok);
+      return ok;
+    };
+    auto scores = [&](int X, int buf) {  // S_X = Q_X K^T (descriptors count 16 bytes)
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            mma_ss(d, tc::smem_desc(q_at + X * S::kQ + ks * 256, 128, S::kBand),
-                   tc::smem_desc(k_at + buf * S::kSide + ks * 256, 128, S::kBand), kQk, ks > 0);
-          tc::mma_commit(tc::smem_u32(&s_full[X]));
-        };
-        for (int X = 0; X < groups && ok; ++X) {
-          ok = wait_for(&q_full[X], q_no[X] & 1, dead, a.err);
-          ++q_no[X];
-        }
-        ok = ok && wait_for(&k_full[tile_no & 1], (tile_no >> 1) & 1, dead, a.err);
-        if (ok) {
+      for (int ks = 0; ks < D / 16; ++ks)
+        mma_ss(tmem + X * 128, q_desc + (X * S::kQ + ks * 256) / 16, k_desc + (buf * S::kSide + ks * 256) / 16, kQk, ks > 0);
+      commit(&s_full[X]);
+    };
+    while (ok && next_part(p)) {
+      if (p.n == 0) continue;
+      const int groups = p.n_cols > kRows ? 2 : 1;
+      for (int X = 0; X < groups; ++X) {
+        if (!wait(&q_full[X], q_no[X] & 1)) break;
+        ++q_no[X];
+      }
+      if (!wait(&k_full[tile_no & 1], (tile_no >> 1) & 1)) break;
+      tc::tc_fence_after();
+      for (int X = 0; X < groups; ++X) scores(X, tile_no & 1);
+      commit(&k_empty[tile_no & 1]);
+      for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
+        const int buf = tile_no & 1, nbuf = buf ^ 1;
+        if (!wait(&v_full[buf], (tile_no >> 1) & 1)) break;
+        for (int X = 0; X < groups; ++X) {
+          if (!wait(&p_full[X], mine_no[X] & 1)) break;
           tc::tc_fence_after();
-          for (int X = 0; X < groups; ++X) scores(X, tile_no & 1);
-          tc::mma_commit(tc::smem_u32(&k_empty[tile_no & 1]));
-        }
-        for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
-          const int buf = tile_no & 1, nbuf = buf ^ 1;
-          ok = wait_for(&v_full[buf], (tile_no >> 1) & 1, dead, a.err);
-          for (int X = 0; X < groups && ok; ++X) {
-            ok = wait_for(&p_full[X], mine_no[X] & 1, dead, a.err);
-            if (!ok) break;
-            tc::tc_fence_after();
 #pragma unroll
-            for (int ks = 0; ks < kKeys / 16; ++ks)
-              mma_ts(tmem + 256 + X * 128, tmem + X * 128 + ks * 8,
-                     tc::smem_desc(v_at + buf * S::kSide + ks * 2 * S::kBand, S::kBand, 128), kPv, i > 0 || ks > 0);
-            tc::mma_commit(tc::smem_u32(&pv_done[X]));
-            if (X == groups - 1) tc::mma_commit(tc::smem_u32(&v_empty[buf]));
-            if (i + 1 < p.n) {
-              if (X == 0) ok = wait_for(&k_full[nbuf], ((tile_no + 1) >> 1) & 1, dead, a.err);
-              // the weights lie where the next scores go
-              ok = ok && wait_for(&pv_done[X], mine_no[X] & 1, dead, a.err);
-              if (!ok) break;
-              tc::tc_fence_after();
-              scores(X, nbuf);
-              if (X == groups - 1) tc::mma_commit(tc::smem_u32(&k_empty[nbuf]));
-            }
-            ++mine_no[X];
+          for (int ks = 0; ks < kKeys / 16; ++ks)
+            mma_ts(tmem + 256 + X * 128, tmem + X * 128 + ks * 8, v_desc + (buf * S::kSide + ks * 2 * (int)S::kBand) / 16, kPv,
+                   i > 0 || ks > 0);
+          commit(&pv_done[X]);
+          if (X == groups - 1) commit(&v_empty[buf]);
+          if (i + 1 < p.n) {
+            if (X == 0 && !wait(&k_full[nbuf], ((tile_no + 1) >> 1) & 1)) break;
+            // the weights lie where the next scores go
+            if (!wait(&pv_done[X], mine_no[X] & 1)) break;
+            tc::tc_fence_after();
+            scores(X, nbuf);
+            if (X == groups - 1) commit(&k_empty[nbuf]);
           }
+          ++mine_no[X];
         }
       }
-      __syncwarp();
     }
-    if (lane == 0) {  // whatever was issued has ended before tensor memory is freed
-      tc::mma_commit(tc::smem_u32(&all_done));
-      tc::mbar_wait(tc::smem_u32(&all_done), 0, a.err);
-    }
+    __syncwarp();
+    commit(&all_done);  // whatever was issued has ended before tensor memory is freed
+    tc::mbar_wait(tc::smem_u32(&all_done), 0, a.err);
     __syncwarp();
   }
   tc::tc_fence_before();
