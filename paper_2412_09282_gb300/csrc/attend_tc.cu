@@ -75,12 +75,11 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
       : "memory");
 }
 
-// Bounded wait; false once any wait of the CTA has run out.
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* dead, unsigned* err) {
-  const uint32_t b = tc::smem_u32(bar);
-  if (tc::mbar_try_wait(b, parity)) return true;
+// Bounded wait; false once any wait of the CTA has run out. (Out of line but for the first look: the roles' code
+// together overflowed the instruction caches.)
+__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int* dead, unsigned* err) {
   const unsigned long long t0 = tc::globaltimer();
-  while (!tc::mbar_try_wait(b, parity)) {
+  while (!tc::mbar_try_wait(bar, parity)) {
     if (*dead) return false;
     if (tc::globaltimer() - t0 > tc::kWaitNs) {
       raise_error(err, ERRBIT_TIMEOUT);
@@ -89,6 +88,11 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
     }
   }
   return true;
+}
+
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* dead, unsigned* err) {
+  const uint32_t b = tc::smem_u32(bar);
+  return tc::mbar_try_wait(b, parity) || wait_longer(b, parity, dead, err);
 }
 
 // Sixteen codes of a token as fp16, to two neighbouring pieces.
@@ -131,6 +135,33 @@ struct Part {
   int first, n;         // tokens before the first tile that holds such a key; tiles
 };
 
+// The next part of a share whose places [*w, w1) are left; false past the last (whole warps, out of line).
+template <int D>
+__device__ __noinline__ bool find_part(const AttendArgs& a, const Line<D, kUnit>& line, int64_t* w, int64_t w1, Part* part) {
+  Part& p = *part;
+  while (*w < w1) {
+    p.u = line.locate(a, *w);
+    const Seq& s = p.u.s;
+    const int64_t tile0 = p.u.begin + kStart, unit_end = tile0 + s.tiles;
+    p.t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
+    *w = min(unit_end, w1);
+    if (p.u.tile >= p.t_end) continue;
+    p.col0 = p.u.cg * kUnit;
+    p.n_cols = min(kUnit, s.n * a.group - p.col0);
+    const int pos0 = s.len - s.n + p.col0 / a.group, pos1 = s.len - s.n + (p.col0 + p.n_cols - 1) / a.group;
+    p.some_e = a.causal ? min(s.len, pos1 + 1) : s.len;
+    p.some_b = a.window > 0 ? max(0, pos0 - a.window + 1) : 0;
+    p.every_e = a.causal ? min(s.len, pos0 + 1) : s.len;
+    p.every_b = a.window > 0 ? max(0, pos1 - a.window + 1) : 0;
+    const int t0 = max(p.u.tile, p.some_b / kKeys - s.lo);
+    const int t1 = min(p.t_end, (max(0, p.some_e) + kKeys - 1) / kKeys - s.lo);
+    p.first = (s.lo + t0) * kKeys;
+    p.n = p.some_b < p.some_e ? max(0, t1 - t0) : 0;
+    return true;
+  }
+  return false;
+}
+
 template <int D, int FMT>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attend_tc_kernel(const __grid_constant__ AttendArgs a) {
@@ -138,8 +169,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(128) char sm[];
   __shared__ __align__(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2],
       q_full[2], all_done;
-  __shared__ float sk_s[2][8], sv_s[2][8], lg_s[2][8];  // scales of a tile's blocks, log2 of the values'
-  __shared__ int live_s[2][8];
+  __shared__ __align__(16) float sk_s[2][8], sv_s[2][8], lg_s[2][8];  // scales of a tile's blocks, log2 of the values'
+  __shared__ __align__(16) int live_s[2][8];
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_s;
   volatile int* dead = &dead_s;
@@ -175,31 +206,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   char* k_sm = sm + 2 * S::kQ;
   char* v_sm = k_sm + 2 * S::kSide;
 
-  // The parts of this share, in order (whole warps).
   int64_t w = share_begin(total, blockIdx.x, shares);
-  auto next_part = [&](Part& p) {
-    while (w < w1) {
-      p.u = line.locate(a, w);
-      const Seq& s = p.u.s;
-      const int64_t tile0 = p.u.begin + kStart, unit_end = tile0 + s.tiles;
-      p.t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
-      w = min(unit_end, w1);
-      if (p.u.tile >= p.t_end) continue;
-      p.col0 = p.u.cg * kUnit;
-      p.n_cols = min(kUnit, s.n * a.group - p.col0);
-      const int pos0 = s.len - s.n + p.col0 / a.group, pos1 = s.len - s.n + (p.col0 + p.n_cols - 1) / a.group;
-      p.some_e = a.causal ? min(s.len, pos1 + 1) : s.len;
-      p.some_b = a.window > 0 ? max(0, pos0 - a.window + 1) : 0;
-      p.every_e = a.causal ? min(s.len, pos0 + 1) : s.len;
-      p.every_b = a.window > 0 ? max(0, pos1 - a.window + 1) : 0;
-      const int t0 = max(p.u.tile, p.some_b / kKeys - s.lo);
-      const int t1 = min(p.t_end, (max(0, p.some_e) + kKeys - 1) / kKeys - s.lo);
-      p.first = (s.lo + t0) * kKeys;
-      p.n = p.some_b < p.some_e ? max(0, t1 - t0) : 0;
-      return true;
-    }
-    return false;
-  };
+  auto next_part = [&](Part& p) { return find_part<D>(a, line, &w, w1, &p); };
   Part p;
   bool ok = true;
 
@@ -281,14 +289,11 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
         if (!ok) break;
         if (active) {
           const int tok = p.first + i * kKeys;
-          float sv_top = 0.f;
-          bool all_live = true;
-#pragma unroll
-          for (int b = 0; b < 8; ++b) {
-            sv_top = fmaxf(sv_top, sv_s[buf][b]);
-            all_live = all_live && live_s[buf][b];
-          }
-          const bool whole = all_live && tok >= p.every_b && tok + kKeys <= p.every_e;
+          const float4 sv0 = *reinterpret_cast<const float4*>(&sv_s[buf][0]), sv1 = *reinterpret_cast<const float4*>(&sv_s[buf][4]);
+          const int4 lv0 = *reinterpret_cast<const int4*>(&live_s[buf][0]), lv1 = *reinterpret_cast<const int4*>(&live_s[buf][4]);
+          const float sv_top = fmaxf(fmaxf(fmaxf(sv0.x, sv0.y), fmaxf(sv0.z, sv0.w)), fmaxf(fmaxf(sv1.x, sv1.y), fmaxf(sv1.z, sv1.w)));
+          const bool whole = (lv0.x & lv0.y & lv0.z & lv0.w & lv1.x & lv1.y & lv1.z & lv1.w) != 0 && tok >= p.every_b &&
+                             tok + kKeys <= p.every_e;
           // The row's maximum over the tile, then (after the rescale) its weights, 32 columns at a time, in rolled
           // loops: unrolled, the warps' different code overflowed the instruction caches.
           float mt = -INFINITY;
@@ -533,36 +538,35 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           sv[b] = sv_n[b];
         }
       };
-      if (p.n > 0) {
-        look_up(0);
-        load(a.c.K, 0, false, kr);
-        load(a.c.V, 0, true, vr);
-        take();
-        look_up(1);
-      }
-      for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
+      if (p.n > 0) look_up(0);
+      for (int i = -1; i < p.n && ok; ++i) {  // tile i's operands are written, tile i + 1's codes loaded
         const int buf = tile_no & 1;
         const uint32_t ph = ((tile_no >> 1) & 1) ^ 1;
-        ok = wait_for(&k_empty[buf], ph, dead, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane < 2) {
-          sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
-          sv_s[buf][2 * cw + lane] = lane ? sv[1] : sv[0];
-          lg_s[buf][2 * cw + lane] = log2f(lane ? sv[1] : sv[0]);
-          live_s[buf][2 * cw + lane] = (lane ? at[1] : at[0]) >= 0;
+        if (i >= 0) {
+          ok = wait_for(&k_empty[buf], ph, dead, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane < 2) {
+            sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
+            sv_s[buf][2 * cw + lane] = lane ? sv[1] : sv[0];
+            lg_s[buf][2 * cw + lane] = log2f(lane ? sv[1] : sv[0]);
+            live_s[buf][2 * cw + lane] = (lane ? at[1] : at[0]) >= 0;
+          }
+          store(k_sm + buf * S::kSide, kr);
+          tc::fence_async_smem();
+          __syncwarp();
+          tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
         }
-        store(k_sm + buf * S::kSide, kr);
-        tc::fence_async_smem();
-        __syncwarp();
-        tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
         if (i + 1 < p.n) load(a.c.K, i + 1, false, kr);
-        ok = wait_for(&v_empty[buf], ph, dead, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        store(v_sm + buf * S::kSide, vr);
-        tc::fence_async_smem();
-        tc::mbar_arrive(tc::smem_u32(&v_full[buf]));
+        if (i >= 0) {
+          ok = wait_for(&v_empty[buf], ph, dead, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          store(v_sm + buf * S::kSide, vr);
+          tc::fence_async_smem();
+          tc::mbar_arrive(tc::smem_u32(&v_full[buf]));
+          ++tile_no;
+        }
         if (i + 1 < p.n) load(a.c.V, i + 1, true, vr);
         take();
         look_up(i + 2);
