@@ -207,8 +207,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   char* v_sm = k_sm + 2 * S::kSide;
 
   int64_t w = share_begin(total, blockIdx.x, shares);
-  auto next_part = [&](Part& p) { return find_part<D>(a, line, &w, w1, &p); };
-  Part p;
+  Part found;
+  auto next_part = [&]() { return find_part<D>(a, line, &w, w1, &found); };
   bool ok = true;
 
   if (warp < 8) {
@@ -218,7 +218,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
     const uint32_t s_at = tmem + lanes + X * 128, o_at = tmem + lanes + 256 + X * 128;
     char* q_mine = q_sm + X * S::kQ;
     uint32_t tile_no = 0, mine_no = 0;  // tiles of the share; of those that this group works on
-    while (ok && next_part(p)) {
+    while (ok && next_part()) {
+      const Part p = found;  // (in registers)
       const int r = X * kRows + row, c = p.col0 + r;
       const bool valid = r < p.n_cols, active = X == 0 || p.n_cols > kRows;
       const int j = valid ? c / a.group : 0, h = p.u.h * a.group + (valid ? c % a.group : 0);
@@ -490,7 +491,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
     int64_t at[2], at_n[2];
     float sk[2], sv[2], sk_n[2], sv_n[2];
     uint32_t tile_no = 0;
-    while (ok && next_part(p)) {
+    while (ok && next_part()) {
+      const Part p = found;  // (in registers)
       const int len = p.u.s.len, tok0 = p.first + 32 * cw;
       auto look_up = [&](int i) {
 #pragma unroll
@@ -590,7 +592,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
         mma_ss(tmem + X * 128, q_desc + (X * S::kQ + ks * 256) / 16, k_desc + (buf * S::kSide + ks * 256) / 16, kQk, ks > 0);
       commit(&s_full[X]);
     };
-    while (ok && next_part(p)) {
+    while (ok && next_part()) {
+      const Part p = found;  // (in registers)
       if (p.n == 0) continue;
       const int groups = p.n_cols > kRows ? 2 : 1;
       for (int X = 0; X < groups; ++X) {
