@@ -5,9 +5,10 @@
 //   s = max(max_i |x_i| * (1 / Q), s0 if there are old tokens),  Q = 127 or 448,
 //   c_i <- round(c_i * (s0 / s)) for the old,  c_i = round(x_i / s) for the new,
 // with x the rotated key (a cos - b sin, b cos + a sin) or the value. One CTA owns one block of one
-// head's keys or values, so a scale is found and every code written by the same threads: no atomics,
-// no second pass over the inputs. A thread holds 16 channels of one token in registers, eight at i and
-// eight at i + D/2 (or 2 x 8 neighbours for interleaved pairs), so a rotation pair is one thread's.
+// head's keys and values, so a scale is found and every code written by the same threads: no atomics,
+// no second pass over the inputs. A thread holds 16 channels of a token's key and of its value, four at
+// 4 c + k D / 4, k = 0 .. 3: a rotation pair of either form is one thread's, and every load of a row covers
+// whole lines. What does not wait for another lookup is loaded first (the new rows beside the page).
 // The grid has a slot for every block that could be touched (the lengths are on the device); the ones
 // that are not leave at once. Each product, difference and quotient is rounded to fp32 by itself (no
 // fused multiply-add): codes do not depend on how the compiler contracts.
@@ -31,11 +32,13 @@ struct AppendArgs {
   int64_t n_pos, ld_rot;
   int half;          // rotated pairs (0: none)
   bool interleaved;
-  bool pair_regs;    // a rotation pair lies within a thread's 16 channels
+  bool pair_regs;    // a rotation pair lies within a thread's 16 channels, read whole from the tables
   bool vec_k, vec_v, vec_q, vec_qo, vec_rot;
   int64_t slots;     // block slots of all sequences
   int per_seq;       // slots per sequence (rows.off null)
-  int64_t n_append;  // CTAs of the append; the rest rotate queries
+  int n_append;      // CTAs of the append; the rest rotate queries
+  int n_rows;        // (token, head) rows of queries
+  Divisor by_kv, by_page, by_heads, by_per, by_slots;  // n_kv, page, query heads, rows.per, per_seq
   unsigned* err;
 };
 
@@ -43,8 +46,8 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466
 
 // The 16 channels of a thread, c the thread's index in its row (0 .. D/16 - 1): channel of element e.
 template <int D>
-__device__ __forceinline__ int channel(int c, int e, bool split) {
-  return split ? (e < 8 ? 8 * c + e : D / 2 + 8 * c + e - 8) : 16 * c + e;
+__device__ __forceinline__ int channel(int c, int e) {
+  return 4 * c + (e >> 2) * (D / 4) + (e & 3);
 }
 
 __device__ __forceinline__ void turn(float& u, float& w, float c, float s) {
@@ -53,44 +56,99 @@ __device__ __forceinline__ void turn(float& u, float& w, float c, float s) {
   w = __fadd_rn(__fmul_rn(w, c), __fmul_rn(x, s));
 }
 
-// x: this thread's 16 channels of (token row t, head h), rotated by the angle row `pos` (-1: not).
+// Four consecutive fp32 elements (vec: 16-byte aligned).
+__device__ __forceinline__ void load4(const float* p, bool vec, float v[4]) {
+  if (vec) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __ldg(p + j);
+  }
+}
+
+__device__ __forceinline__ void store4(void* p, int64_t i, int type, bool vec, const float v[4]) {
+  if (!vec) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) store_elem(p, i + j, type, v[j]);
+  } else if (type == CRVQ_F32) {
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(pack2(v[0], v[1], type), pack2(v[2], v[3], type));
+  }
+}
+
+// A thread's 16 channels of (token row t, head h).
 template <int D>
-__device__ __forceinline__ void load_rotated(const AppendArgs& a, const HeadsView& src, bool vec,
-                                             int64_t t, int h, int c, bool split, int64_t pos,
-                                             float x[16]) {
+__device__ __forceinline__ void load_row(const HeadsView& src, bool vec, int64_t t, int h, int c, float x[16]) {
   const int64_t row = t * src.ld_tok + h * src.ld_head;
-  load8(src.data, row + channel<D>(c, 0, split), src.type, vec, x);
-  load8(src.data, row + channel<D>(c, 8, split), src.type, vec, x + 8);
+  if (!vec) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = load_elem(src.data, row + channel<D>(c, e), src.type);
+  } else if (src.type == CRVQ_F32) {
+    const float* p = static_cast<const float*>(src.data) + row + 4 * c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 a = *reinterpret_cast<const float4*>(p + k * (D / 4));
+      x[4 * k] = a.x; x[4 * k + 1] = a.y; x[4 * k + 2] = a.z; x[4 * k + 3] = a.w;
+    }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(src.data) + row + 4 * c;
+    uint2 u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = *reinterpret_cast<const uint2*>(p + k * (D / 4));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float* v = x + 4 * k;
+      if (src.type == CRVQ_BF16) {
+        v[0] = __uint_as_float(u[k].x << 16); v[1] = __uint_as_float(u[k].x & 0xffff0000u);
+        v[2] = __uint_as_float(u[k].y << 16); v[3] = __uint_as_float(u[k].y & 0xffff0000u);
+      } else {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&u[k].x));
+        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&u[k].y));
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+      }
+    }
+  }
+}
+
+// The same, turned by the tables' row `pos` (-1: not).
+template <int D>
+__device__ __forceinline__ void rotate_row(const AppendArgs& a, const HeadsView& src, int64_t t, int h, int c,
+                                           int64_t pos, float x[16]) {
   if (pos < 0) return;
   const float* cs = a.cos + pos * a.ld_rot;
   const float* sn = a.sin + pos * a.ld_rot;
-  if (a.pair_regs) {
-    float cv[8], sv[8];
-    const int i0 = 8 * c;  // both forms: the thread's eight pairs are 8c .. 8c + 7
-    if (a.vec_rot && i0 + 8 <= a.half) {
-      load8(cs, i0, CRVQ_F32, true, cv);
-      load8(sn, i0, CRVQ_F32, true, sv);
-    } else {
+  if (a.pair_regs && a.interleaved) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = i0 + j < a.half;
-        cv[j] = in ? __ldg(cs + i0 + j) : 1.f;
-        sv[j] = in ? __ldg(sn + i0 + j) : 0.f;
+    for (int k = 0; k < 4; ++k) {
+      const int i = channel<D>(c, 4 * k) / 2;  // (even: pairs i and i + 1)
+      float* v = x + 4 * k;
+      if (a.vec_rot && i + 1 < a.half) {
+        const float2 cv = __ldg(reinterpret_cast<const float2*>(cs + i));
+        const float2 sv = __ldg(reinterpret_cast<const float2*>(sn + i));
+        turn(v[0], v[1], cv.x, sv.x);
+        turn(v[2], v[3], cv.y, sv.y);
+      } else {  // (an unrotated channel keeps its bits)
+        if (i < a.half) turn(v[0], v[1], __ldg(cs + i), __ldg(sn + i));
+        if (i + 1 < a.half) turn(v[2], v[3], __ldg(cs + i + 1), __ldg(sn + i + 1));
       }
     }
+  } else if (a.pair_regs) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (i0 + j >= a.half) continue;  // (an unrotated channel keeps its bits, infinities too)
-      if (split)
-        turn(x[j], x[j + 8], cv[j], sv[j]);
-      else
-        turn(x[2 * j], x[2 * j + 1], cv[j], sv[j]);
+    for (int k = 0; k < 2; ++k) {
+      float cv[4], sv[4];
+      load4(cs + channel<D>(c, 4 * k), a.vec_rot, cv);
+      load4(sn + channel<D>(c, 4 * k), a.vec_rot, sv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) turn(x[4 * k + j], x[4 * k + 8 + j], cv[j], sv[j]);
     }
   } else {
     // pairs (i, i + half) with half < D/2: the partner is another thread's, read again
+    const int64_t row = t * src.ld_tok + h * src.ld_head;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int ch = channel<D>(c, e, split);
+      const int ch = channel<D>(c, e);
       if (ch >= 2 * a.half) continue;
       const bool first = ch < a.half;
       const int i = first ? ch : ch - a.half;
@@ -113,16 +171,16 @@ __device__ __forceinline__ int64_t rot_row(const AppendArgs& a, int64_t t, int p
   return pos;
 }
 
-template <int FMT>
+// Codes of four values (SMALL: magnitudes below Q + 1/2). int8: adding 1.5 * 2^23 rounds to an integer, which
+// the sum's low byte is in two's complement.
+template <int FMT, bool SMALL>
 __device__ __forceinline__ uint32_t encode4(const float v[4]) {
   if constexpr (FMT == CRVQ_KV_INT8) {
-    uint32_t w = 0;
+    uint32_t b[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int q = (int)rintf(fminf(fmaxf(v[j], -127.f), 127.f));
-      w |= (uint32_t)(q & 255) << (8 * j);
-    }
-    return w;
+    for (int j = 0; j < 4; ++j)
+      b[j] = __float_as_uint(__fadd_rn(SMALL ? v[j] : fminf(fmaxf(v[j], -127.f), 127.f), 12582912.f));
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   } else {
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
@@ -146,193 +204,272 @@ __device__ __forceinline__ void decode4(uint32_t w, float v[4]) {
   }
 }
 
+// x / s rounded once, for inv = 1 / s rounded once: the first correction brings the product within one unit in the
+// last place, and then the remainder is exact and the second one rounds correctly (Markstein 1990). For s
+// in (2^-80, 2^80) no step that a code depends on leaves the normal numbers.
+__device__ __forceinline__ float quotient(float x, float s, float inv) {
+  float q = __fmul_rn(x, inv);
+  q = __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
+  return __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
+}
+
+// One head's keys or values of a block: this thread's new values x (is_new) or old codes to new codes, with
+// the block's scale, from the largest new magnitude (bits) and the old scale.
 template <int D, int FMT>
-__global__ void __launch_bounds__(D) append_kernel(const __grid_constant__ AppendArgs a) {
+__device__ __forceinline__ void encode_block(float x[16], bool is_new, bool is_old, float s0, uint32_t top,
+                                             uint8_t* codes, float* scale, int col) {
+  constexpr float kInv = (float)(1.0 / (FMT == CRVQ_KV_INT8 ? 127.0 : 448.0));
+  const float s = fmaxf(__fmul_rn(__uint_as_float(top), kInv), s0);
+  uint32_t w[4];
+  if (is_new) {
+    if (s > 0x1p-80f && s < 0x1p80f) {
+      const float inv = __frcp_rn(s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = quotient(x[e], s, inv);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = encode4<FMT, true>(x + 4 * e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = s > 0.f ? __fdiv_rn(x[e], s) : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = encode4<FMT, false>(x + 4 * e);
+    }
+  } else if (is_old && s != s0) {
+    const float ratio = s > 0.f ? __fdiv_rn(s0, s) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float v[4];
+      decode4<FMT>(*reinterpret_cast<const uint32_t*>(codes + channel<D>(col, 4 * e)), v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], ratio);
+      w[e] = encode4<FMT, false>(v);
+    }
+  }
+  if (is_new || (is_old && s != s0)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(codes + channel<D>(col, 4 * e)) = w[e];
+  }
+  if (threadIdx.x == 0) *scale = s;  // (s0 was read by every thread before the barrier)
+}
+
+// The largest magnitude (bits) of 16 values; those that are not finite are set to 0 and reported.
+__device__ __forceinline__ uint32_t top_of(float x[16], unsigned* err) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  if (top < 0x7f800000u) return top;
+  raise_error(err, ERRBIT_NUMERIC);
+  top = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    if (!finite(x[e])) x[e] = 0.f;
+    top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  }
+  return top;
+}
+
+// (1536 threads per SM: three fp32 prompts of up to 4091 tokens, 32 heads, are appended and read back in 152 us;
+// with the registers left open, 162)
+template <int D, int FMT>
+__global__ void __launch_bounds__(D, 1536 / D) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kRow = D / 16;  // threads per token
   __shared__ int32_t off_s[kOffShared + 1];
   __shared__ uint32_t top_s[D / 32];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x;
-  const int32_t* off = a.rows.off;
   const CacheView& c = a.c;
-  if (off && c.n_seq <= kOffShared) {
+  const int32_t* off = a.rows.off;
+  // the sequence of a slot: sequence i's begin at off[i] / 16 + 2 i, n tokens touch at most n / 16 + 2 blocks
+  auto sequence = [&](int64_t v) {
+    auto key = [&](int i) { return (int64_t)off[i] / kCacheBlock + 2 * i; };
+    if (c.n_seq > 32) return last_not_above(c.n_seq, v, key);
+    const int lane = tid & 31;  // (whole warps: one look for up to 32 sequences)
+    const int64_t mine = lane < c.n_seq ? key(lane) : v + 1;
+    return 31 - __clz(max(1u, __ballot_sync(0xffffffffu, mine <= v)));
+  };
+  if (off && c.n_seq > 32 && c.n_seq <= kOffShared) {
     for (int i = tid; i <= c.n_seq; i += D) off_s[i] = __ldg(a.rows.off + i);
     __syncthreads();
     off = off_s;
   }
-  const int col = tid % kRow, r = tid / kRow;
-  const bool split = !a.interleaved;
-  int64_t id = blockIdx.x;
-  if (id >= a.n_append) {  // queries: 16 (token, head) rows per CTA
-    const int64_t at = (id - a.n_append) * 16 + r;
-    bool live = at < a.rows.n_tok * a.q.heads;
-    const int64_t t = at / a.q.heads;
-    const int h = (int)(at - t * a.q.heads);
-    int p = 0;
-    if (live && a.half && !a.positions) {
-      const int b = off ? last_not_above(c.n_seq, t, [&](int i) { return (int64_t)off[i]; })
-                        : (int)(t / a.rows.per);
-      int64_t first;
-      int n;
-      seq_rows(a.rows, b, &first, &n, a.err);
-      live = t >= first && t < first + n;  // (rows outside every sequence stay unwritten)
-      p = seq_len(c, b, a.err) - n + (int)(t - first);
+  // the same for rows that differ within a warp
+  auto sequence_of = [&](int64_t t) {
+    if (c.n_seq > 32) return last_not_above(c.n_seq, t, [&](int i) { return (int64_t)off[i]; });
+    const int lane = tid & 31;
+    const int mine = lane < c.n_seq ? off[lane] : INT32_MAX;
+    int b = 0;
+#pragma unroll
+    for (int step = 16; step; step >>= 1) {
+      const int at = __shfl_sync(0xffffffffu, mine, b + step);
+      if (at <= t) b += step;
     }
+    return b;
+  };
+  const int col = tid % kRow, r = tid / kRow;
+  const int id = blockIdx.x;
+  if (id >= a.n_append) {  // queries: 16 (token, head) rows
+    const unsigned row = (unsigned)(id - a.n_append) * 16 + r;
+    bool live = row < (unsigned)a.n_rows;
+    const int at = live ? (int)row : 0, t = a.by_heads.div(at), h = at - t * a.q.heads;
     float x[16];
-    if (live) load_rotated<D>(a, a.q, a.vec_q, t, h, col, split, rot_row(a, t, p), x);
-    const int64_t row = t * a.qo.ld_tok + h * a.qo.ld_head;
+    if (live) load_row<D>(a.q, a.vec_q, t, h, col, x);
+    int p = 0;
+    if (a.half && !a.positions) {
+      const int b = off ? sequence_of(t) : live ? a.by_per.div(t) : 0;
+      if (live) {
+        int64_t first;
+        int n;
+        seq_rows(a.rows, b, &first, &n, a.err);
+        live = t >= first && t < first + n;  // (rows outside every sequence stay unwritten)
+        p = seq_len(c, b, a.err) - n + (int)(t - first);
+      }
+    }
+    if (live) rotate_row<D>(a, a.q, t, h, col, rot_row(a, t, p), x);
     __syncwarp();  // in place: a warp's rows are read whole before they are written
     if (live) {
-      store8(a.qo.data, row + channel<D>(col, 0, split), a.qo.type, a.vec_qo, x);
-      store8(a.qo.data, row + channel<D>(col, 8, split), a.qo.type, a.vec_qo, x + 8);
+      const int64_t out = t * a.qo.ld_tok + h * a.qo.ld_head;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) store4(a.qo.data, out + channel<D>(col, 4 * k), a.qo.type, a.vec_qo, x + 4 * k);
     }
     return;
   }
-  // which block: sequence b, its j-th touched one; which head, keys or values
-  const bool values = id & 1;
-  id >>= 1;
-  const int h = (int)(id % c.n_kv);
-  const int64_t slot = id / c.n_kv;
+  // which block: sequence b, its j-th touched one; which head
+  const bool is_key = !(id & 1);
+  const int slot = a.by_kv.div(id >> 1), h = (id >> 1) - slot * c.n_kv;
   int b, j;
   if (off) {
-    // sequence i's slots begin at off[i] / 16 + 2 i: n tokens touch at most n / 16 + 2 blocks
-    b = last_not_above(c.n_seq, slot, [&](int i) { return (int64_t)off[i] / kCacheBlock + 2 * i; });
-    j = (int)(slot - off[b] / kCacheBlock - 2 * b);
+    b = sequence(slot);
+    j = slot - off[b] / kCacheBlock - 2 * b;
   } else {
-    b = (int)(slot / a.per_seq);
-    j = (int)(slot - (int64_t)b * a.per_seq);
+    b = a.by_slots.div(slot);
+    j = slot - b * a.per_seq;
   }
   int64_t first;
   int n;
   seq_rows(a.rows, b, &first, &n, a.err);
-  if (n == 0 || j < 0) return;
   const int len = seq_len(c, b, a.err);
+  if (n == 0 || j < 0) return;
   const int held = len - n;
   if (held < 0) {
     raise_error(a.err, ERRBIT_INDEX);
     return;
   }
-  const int64_t p0 = ((int64_t)held / kCacheBlock + j) * kCacheBlock;
-  if (p0 >= len) return;
-  const int64_t page = seq_page(c, b, (int)(p0 / c.page), a.err);
-  if (page < 0) return;
-  const int in_page = (int)(p0 % c.page);
-  uint8_t* codes = (values ? c.V : c.K) + page * c.page_stride + ((int64_t)h * c.page + in_page + r) * D;
-  float* scale = (values ? c.vs : c.ks) + (page * c.n_kv + h) * (c.page / kCacheBlock) + in_page / kCacheBlock;
-  const int p = (int)p0 + r;
+  const int64_t first_at = ((int64_t)held / kCacheBlock + j) * kCacheBlock;
+  if (first_at >= len) return;
+  const int p0 = (int)first_at, in_table = a.by_page.div(p0), in_page = p0 - in_table * c.page;
+  // the page's number is on its way while the new rows are loaded and turned
+  const int32_t page_id = __ldg(c.pages + b * c.ld_pages + in_table);
+  const int p = p0 + r;
   const bool is_old = p < held, is_new = !is_old && p < len;
-  const float s0 = p0 < held ? *scale : 0.f;
-  uint32_t w[4] = {0, 0, 0, 0};
-  if (is_old) {
-    const uint2 u0 = *reinterpret_cast<const uint2*>(codes + channel<D>(col, 0, split));
-    const uint2 u1 = *reinterpret_cast<const uint2*>(codes + channel<D>(col, 8, split));
-    w[0] = u0.x; w[1] = u0.y; w[2] = u1.x; w[3] = u1.y;
-  }
   float x[16];
   uint32_t top = 0;
   if (is_new) {
     const int64_t t = first + (p - held);
-    if (values)
-      load_rotated<D>(a, a.v, a.vec_v, t, h, col, split, -1, x);
-    else
-      load_rotated<D>(a, a.k, a.vec_k, t, h, col, split, rot_row(a, t, p), x);
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      if (!finite(x[e])) {
-        x[e] = 0.f;
-        bad = true;
-      }
-      top = max(top, __float_as_uint(fabsf(x[e])));
+    if (is_key) {
+      load_row<D>(a.k, a.vec_k, t, h, col, x);
+      rotate_row<D>(a, a.k, t, h, col, rot_row(a, t, p), x);
+    } else {
+      load_row<D>(a.v, a.vec_v, t, h, col, x);
     }
-    if (bad) raise_error(a.err, ERRBIT_NUMERIC);
+    top = top_of(x, a.err);
   }
+  if (page_id < 0 || page_id >= c.n_pages) {  // (the same for the whole block)
+    raise_error(a.err, ERRBIT_INDEX);
+    return;
+  }
+  const int64_t page = page_id;
+  const int64_t at = page * c.page_stride + ((int64_t)h * c.page + in_page + r) * D;
+  const int64_t at_s = (page * c.n_kv + h) * ((unsigned)c.page / kCacheBlock) + in_page / kCacheBlock;
+  uint8_t* codes = (is_key ? c.K : c.V) + at;
+  float* scale = (is_key ? c.ks : c.vs) + at_s;
+  const float s0 = p0 < held ? *scale : 0.f;
   top = __reduce_max_sync(0xffffffffu, top);
   if ((tid & 31) == 0) top_s[tid >> 5] = top;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) top = max(top, top_s[i]);
-  constexpr float kInv = (float)(1.0 / (FMT == CRVQ_KV_INT8 ? 127.0 : 448.0));
-  const float s = fmaxf(__fmul_rn(__uint_as_float(top), kInv), s0);
-  const float ratio = s > 0.f ? __fdiv_rn(s0, s) : 0.f;
-  if (is_new) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = s > 0.f ? __fdiv_rn(x[e], s) : 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = encode4<FMT>(x + 4 * e);
-  } else if (is_old && ratio != 1.f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float v[4];
-      decode4<FMT>(w[e], v);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], ratio);
-      w[e] = encode4<FMT>(v);
-    }
-  }
-  if (is_new || (is_old && ratio != 1.f)) {
-    *reinterpret_cast<uint2*>(codes + channel<D>(col, 0, split)) = make_uint2(w[0], w[1]);
-    *reinterpret_cast<uint2*>(codes + channel<D>(col, 8, split)) = make_uint2(w[2], w[3]);
-  }
-  if (tid == 0) *scale = s;  // (s0 was read by every thread before the barrier)
+  encode_block<D, FMT>(x, is_new, is_old, s0, top, codes, scale, col);
 }
 
-// A thread turns 16 / sizeof(type) codes of K and of V into one 16-byte store each.
+// A warp takes up to kReadCodes codes of one token's keys and of its values (heads side by side): each lane four
+// (fp32) or eight codes at a time to one 16-byte store, the token's place looked up once.
+constexpr int kReadCodes = 1024;
+
 template <int FMT, int TYPE>
 __global__ void __launch_bounds__(256)
-read_kernel(const __grid_constant__ CacheView c, int D, const int32_t* __restrict__ start,
-            const int32_t* __restrict__ off_g, int64_t n_tok, void* K_out, void* V_out, unsigned* err) {
-  constexpr int kVec = TYPE == CRVQ_F32 ? 4 : 8;
-  __shared__ int32_t off_s[kOffShared + 1];
+read_kernel(const __grid_constant__ CacheView c, int log_d, Divisor by_parts, Divisor by_page, const int32_t* __restrict__ start,
+            const int32_t* __restrict__ off, int64_t n_tok, void* K_out, void* V_out, unsigned* err) {
+  constexpr int kVec = TYPE == CRVQ_F32 ? 4 : 8, kStep = 32 * kVec, kBatch = 4;
   pdl_trigger();
   pdl_wait();
-  const int32_t* off = off_g;
-  if (c.n_seq <= kOffShared) {
-    for (int i = threadIdx.x; i <= c.n_seq; i += 256) off_s[i] = __ldg(off_g + i);
-    __syncthreads();
-    off = off_s;
+  const int lane = threadIdx.x & 31, all = c.n_kv << log_d;
+  const int w = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t t = by_parts.div(w);
+  if (t >= n_tok) return;
+  const int e0 = (w - (int)t * (int)by_parts.d) * kReadCodes, e1 = min(all, e0 + kReadCodes);
+  int b;
+  if (c.n_seq <= 32) {
+    const int64_t mine = lane < c.n_seq ? __ldg(off + lane) : t + 1;
+    b = 31 - __clz(max(1u, __ballot_sync(0xffffffffu, mine <= t)));
+  } else {
+    b = last_not_above(c.n_seq, t, [&](int i) { return (int64_t)__ldg(off + i); });
   }
-  const int per_head = D / kVec;
-  const int64_t per_tok = (int64_t)c.n_kv * per_head;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= n_tok * per_tok) return;
-  const int64_t t = at / per_tok;
-  const int rest = (int)(at - t * per_tok), h = rest / per_head, ch = (rest - h * per_head) * kVec;
-  const int b = last_not_above(c.n_seq, t, [&](int i) { return (int64_t)off[i]; });
-  const int64_t i = t - off[b];
+  const int64_t i = t - __ldg(off + b);
   const int64_t p = (int64_t)__ldg(start + b) + i;
   const int len = seq_len(c, b, err);
   int64_t page = -1;
-  if (i < 0 || t >= off[b + 1] || p < 0 || p >= len)
+  if (i < 0 || t >= __ldg(off + b + 1) || p < 0 || p >= len)
     raise_error(err, ERRBIT_INDEX);
   else
-    page = seq_page(c, b, (int)(p / c.page), err);
-  float k[8], v[8];
+    page = seq_page(c, b, by_page.div((int)p), err);
+  const int in = page >= 0 ? (int)p - by_page.div((int)p) * c.page : 0, blocks = (unsigned)c.page / kCacheBlock;
+  const int64_t at = page * c.page_stride + ((int64_t)in << log_d);
+  const int64_t at_s = page * c.n_kv * blocks + (unsigned)in / kCacheBlock;
+  for (int x0 = e0 + lane * kVec; x0 < e1; x0 += kStep * kBatch) {
+    uint32_t wk[kBatch][kVec / 4], wv[kBatch][kVec / 4];
+    float sk[kBatch], sv[kBatch];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) k[e] = v[e] = 0.f;
-  if (page >= 0) {
-    const int in = (int)(p % c.page);
-    const int64_t at_c = page * c.page_stride + ((int64_t)h * c.page + in) * D + ch;
-    const int64_t at_s = (page * c.n_kv + h) * (c.page / kCacheBlock) + in / kCacheBlock;
-    const float sk = c.ks[at_s], sv = c.vs[at_s];
+    for (int u = 0; u < kBatch; ++u) {
+      const int x = x0 + u * kStep, h = x >> log_d;
+      sk[u] = sv[u] = 0.f;
 #pragma unroll
-    for (int e = 0; e < kVec / 4; ++e) {
-      decode4<FMT>(reinterpret_cast<const uint32_t*>(c.K + at_c)[e], k + 4 * e);
-      decode4<FMT>(reinterpret_cast<const uint32_t*>(c.V + at_c)[e], v + 4 * e);
+      for (int e = 0; e < kVec / 4; ++e) wk[u][e] = wv[u][e] = 0;
+      if (x < e1 && page >= 0) {
+        const int64_t src = at + ((int64_t)h * c.page << log_d) + (x - (h << log_d));
+#pragma unroll
+        for (int e = 0; e < kVec / 4; ++e) {
+          wk[u][e] = __ldg(reinterpret_cast<const uint32_t*>(c.K + src) + e);
+          wv[u][e] = __ldg(reinterpret_cast<const uint32_t*>(c.V + src) + e);
+        }
+        sk[u] = __ldg(c.ks + at_s + h * blocks);
+        sv[u] = __ldg(c.vs + at_s + h * blocks);
+      }
     }
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      k[e] *= sk;
-      v[e] *= sv;
+    for (int u = 0; u < kBatch; ++u) {
+      const int x = x0 + u * kStep;
+      if (x >= e1) break;
+      float k[8], v[8];
+#pragma unroll
+      for (int e = 0; e < kVec / 4; ++e) {
+        decode4<FMT>(wk[u][e], k + 4 * e);
+        decode4<FMT>(wv[u][e], v + 4 * e);
+      }
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        k[e] = page >= 0 ? k[e] * sk[u] : 0.f;
+        v[e] = page >= 0 ? v[e] * sv[u] : 0.f;
+      }
+      const int64_t dst = t * all + x;
+      if constexpr (TYPE == CRVQ_F32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(K_out) + dst) = make_float4(k[0], k[1], k[2], k[3]);
+        *reinterpret_cast<float4*>(static_cast<float*>(V_out) + dst) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+        store8(K_out, dst, TYPE, true, k);
+        store8(V_out, dst, TYPE, true, v);
+      }
     }
-  }
-  if constexpr (TYPE == CRVQ_F32) {
-    static_cast<float4*>(K_out)[at] = make_float4(k[0], k[1], k[2], k[3]);
-    static_cast<float4*>(V_out)[at] = make_float4(v[0], v[1], v[2], v[3]);
-  } else {
-    store8(K_out, at * 8, TYPE, true, k);
-    store8(V_out, at * 8, TYPE, true, v);
   }
 }
 
@@ -379,15 +516,16 @@ crvq_status append(const crvq_kv_cache* cache, const crvq_heads* k, const crvq_h
     a.half = rot->half;
     a.vec_rot = (((uintptr_t)rot->cos | (uintptr_t)rot->sin) & 15u) == 0 && rot->ld % 4 == 0;
   }
-  a.pair_regs = a.interleaved || a.half == 0 || 2 * a.half == D;
-  int64_t n_q = 0;
+  a.pair_regs = a.interleaved || a.half == 0 || 2 * a.half == D;  // (else a partner is another thread's)
+  int64_t n_rows = 0;
   if (q) {
     CRVQ_TRY(make_heads(q, "q", D, n_tok, &a.q));
     CRVQ_TRY(make_heads(q_out, "q_out", D, n_tok, &a.qo));
     CRVQ_CHECK_ARG(a.q.heads == a.qo.heads && a.q.type == a.qo.type, "q and q_out differ in heads or type");
     a.vec_q = vec_ok(a.q);
     a.vec_qo = vec_ok(a.qo);
-    n_q = ceil_div(n_tok * a.q.heads, 16);
+    n_rows = n_tok * a.q.heads;
+    a.by_heads = Divisor(a.q.heads);
   }
   a.vec_k = vec_ok(a.k);
   a.vec_v = vec_ok(a.v);
@@ -395,9 +533,17 @@ crvq_status append(const crvq_kv_cache* cache, const crvq_heads* k, const crvq_h
   // blocks that n tokens can touch: ceil((n - 1) / 16) + 1
   a.per_seq = (a.rows.per + 14) / kCacheBlock + 1;
   a.slots = new_off ? n_tok / kCacheBlock + 2 * (int64_t)a.c.n_seq : (int64_t)a.c.n_seq * a.per_seq;
-  a.n_append = a.slots * a.c.n_kv * 2;
-  const int64_t grid = a.n_append + n_q;
-  if (grid >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many new tokens in one call");
+  const int64_t n_append = a.slots * a.c.n_kv * 2, grid = n_append + ceil_div(n_rows, 16);
+  if (grid >= (int64_t)1 << 31 || n_rows >= (int64_t)1 << 31)
+    return fail(CRVQ_ERR_UNSUPPORTED, "too many new tokens in one call");
+  a.n_append = (int)n_append;
+  a.n_rows = (int)n_rows;
+  a.by_kv = Divisor(a.c.n_kv);
+  a.by_page = Divisor(a.c.page);
+  if (!new_off) {
+    a.by_per = Divisor(a.rows.per);
+    a.by_slots = Divisor(a.per_seq);
+  }
   CRVQ_TRY(device_error_word(&a.err));
   ProfScope ps("cache_append", stream, (double)n_tok * D * (2.0 * a.c.n_kv + (q ? a.q.heads : 0)));
   return cache->format == CRVQ_KV_INT8 ? launch_append<CRVQ_KV_INT8>(a, D, grid, stream)
@@ -409,17 +555,18 @@ crvq_status launch_read(const CacheView& c, int D, const int32_t* start, const i
                         int type, void* K_out, void* V_out, cudaStream_t stream) {
   unsigned* err = nullptr;
   CRVQ_TRY(device_error_word(&err));
-  const int64_t threads = n_tok * c.n_kv * (D / (type == CRVQ_F32 ? 4 : 8));
-  const int64_t grid = ceil_div(threads, 256);
-  if (grid >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many tokens in one call");
+  const int64_t parts = ceil_div((int64_t)c.n_kv * D, kReadCodes), grid = ceil_div(n_tok * parts, 8);
+  if (8 * grid >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many tokens in one call");
   ProfScope ps("cache_read", stream, (double)n_tok * c.n_kv * D * 2 * (1 + type_bytes(type)));
   const dim3 g((unsigned)grid), t(256);
+  const Divisor by_parts(parts), by_page(c.page);
+  const int log_d = D == 64 ? 6 : D == 128 ? 7 : 8;
   if (type == CRVQ_F32)
-    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_F32>, g, t, 0, stream, c, D, start, off, n_tok, K_out, V_out, err));
+    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_F32>, g, t, 0, stream, c, log_d, by_parts, by_page, start, off, n_tok, K_out, V_out, err));
   else if (type == CRVQ_BF16)
-    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_BF16>, g, t, 0, stream, c, D, start, off, n_tok, K_out, V_out, err));
+    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_BF16>, g, t, 0, stream, c, log_d, by_parts, by_page, start, off, n_tok, K_out, V_out, err));
   else
-    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_F16>, g, t, 0, stream, c, D, start, off, n_tok, K_out, V_out, err));
+    CRVQ_CUDA(launch_pdl(read_kernel<FMT, CRVQ_F16>, g, t, 0, stream, c, log_d, by_parts, by_page, start, off, n_tok, K_out, V_out, err));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }

@@ -36,6 +36,22 @@ struct RowsView {
   int per;
 };
 
+// Division of n in [0, 2^31) by a divisor d in [1, 2^31) known before the launch, as a product: with
+// l = ceil(log2 d) and mul = ceil(2^(31 + l) / d), floor(n mul / 2^(31 + l)) is exact (Granlund & Montgomery
+// 1994, for 31-bit n: mul then fits 32 bits).
+struct Divisor {
+  uint32_t d = 1, mul = 0, shift = 0;
+  Divisor() = default;
+  explicit Divisor(int64_t div) : d((uint32_t)div) {
+    int l = 0;
+    while (((int64_t)1 << l) < div) ++l;
+    if (l == 0) return;  // (d = 1: mul would be 2^31 with a shift of -1)
+    mul = (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d);
+    shift = (uint32_t)(l - 1);
+  }
+  __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift); }
+};
+
 // Checks of the arguments (cache.cu): each sets the last error on refusal.
 crvq_status make_cache(const crvq_kv_cache* c, CacheView* out);
 crvq_status make_heads(const crvq_heads* h, const char* name, int head_dim, int64_t n_tok,
