@@ -75,6 +75,26 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
       : "memory");
 }
 
+// Two fp32 numbers at once.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void halves(uint64_t v, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Bounded wait; false once any wait of the CTA has run out. (Out of line but for the first look: the roles' code
 // together overflowed the instruction caches.)
 __device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile int* dead, unsigned* err) {
@@ -278,7 +298,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
         tc::fence_async_smem();
         tc::mbar_arrive(tc::smem_u32(&q_full[X]));
       }
-      float m = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f;
+      float m = -INFINITY, top = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f;  // (m: the reference, top: the maximum)
       for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
         const int buf = tile_no & 1;
         if (active) {
@@ -328,6 +348,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
                 if (seen >> e & 1) mt = fmaxf(mt, v[e] * (e < 16 ? s0 : s1));
             }
           }
+          top = fmaxf(top, mt);
           float up = ref;
           if (sv_top > ref || i == 0)
             up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u, 0x7f000000u)),
@@ -340,9 +361,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc::tc_fence_after();
-            const float mn = need ? fmaxf(m, mt) : m;
-            const float back = m == mn ? 1.f : pow2(m - mn), fac = back * (ref / up);
-            m = mn;
+            const float back = m == top ? 1.f : pow2(m - top), fac = back * (ref / up);
+            m = top;  // (every row's: the warp's other rows will need it later)
             l *= back;
 #pragma unroll 1
             for (int ch = 0; ch < D / 32; ++ch) {
@@ -370,15 +390,20 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
               for (int b = 0; b < 4; ++b) {
                 const float lw = fmaxf(lg_s[buf][4 * half + b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
                 const float g = sk_s[buf][4 * half + b] * f;
-                float sum[4];
+                const uint64_t gg = pair(g, g), bb = pair(bias, bias);
+                uint64_t sum[4];
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                  const float x = pow2(fmaf(__uint_as_float(u[16 * b + e]), g, bias));
-                  const float y = pow2(fmaf(__uint_as_float(u[16 * b + e + 1]), g, bias));
-                  sum[e / 2 & 3] = e < 8 ? x + y : sum[e / 2 & 3] + (x + y);
+                  float x, y;
+                  halves(fma2(pair(__uint_as_float(u[16 * b + e]), __uint_as_float(u[16 * b + e + 1])), gg, bb), x, y);
+                  x = pow2(x);
+                  y = pow2(y);
+                  sum[e / 2 & 3] = e < 8 ? pair(x, y) : add2(sum[e / 2 & 3], pair(x, y));
                   packed[8 * b + e / 2] = half2_bits(x, y);
                 }
-                l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), pow2(-lw), l);
+                float s0, s1;
+                halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+                l = fmaf(s0 + s1, pow2(-lw), l);
               }
               tmem_st16(s_at + half * 32, packed);
               tmem_st16(s_at + half * 32 + 16, packed + 16);
