@@ -1,23 +1,31 @@
 // Attention over the paged 8-bit cache: o = sum_j p_j V_j / sum_j p_j with p_j = exp(scale q . K_j - max),
 // K_j = c_j s^k, V_j = c'_j s^v (one scale per 16 tokens and head).
 //
-// Form. A warp takes one block of 16 tokens at a time: S^T (16 tokens x 8 columns) = K Q^T on
-// mma.sync.m16n8k16 with the codes as the A operand, O^T += V^T P^T with V^T as A and the weights as
-// B. A column is one (query token, query head) pair; a unit is up to 8 NT columns of one kv head, so
-// query heads that share a kv head (and a few drafted tokens) share every code that is read. The
-// contraction index of either product may be taken in any order, so each lane's operand pieces are
-// chosen as 16 consecutive codes of one token row: the codes come straight from global memory in
-// 16-byte loads, one block ahead, and become fp16 by byte permutes (int8: 1024 + code + 128, less
-// 1152; exact) or by one conversion per pair (e4m3; exact).
+// Form. A warp takes two blocks of 16 tokens at a time (one for 256 channels): S^T (16 tokens x 8 columns) =
+// K Q^T on mma.sync.m16n8k16 with the codes as the A operand, O^T += V^T P^T with V^T as A and the weights as
+// B. A column is one (query token, query head) pair; a unit is up to 8 NT columns of one kv head, so query
+// heads that share a kv head (and a few drafted tokens) share every code that is read: the rows are far too
+// few to fill a tcgen05 tile (128), and the products are small beside the codes' way from memory. The
+// contraction index of either product may be taken in any order, so each lane's operand pieces are chosen as
+// 16 consecutive codes of one token row. Blocks are copied to shared memory by a warp's 32 lanes 512
+// consecutive bytes at a time, two steps ahead, and their codes become fp16 by byte permutes (int8:
+// 1024 + code + 128, less 1152; exact) or by one conversion per pair (e4m3; exact).
 //   The key scale multiplies the block's scores in fp32. The value scale multiplies the weights,
-// relative to the largest scale so far (a power of two), so that a weight in fp16 is at most 2^14
-// whatever the scales are; weights below 2^-38 of that vanish. Running maxima and sums are fp32. From
-// fp32 queries both q and the weights are two fp16 operands each.
+// relative to the largest scale so far (a power of two), so that a weight is at most 2^14 whatever the
+// scales are; weights below 2^-38 of that vanish. A weight is two fp16 operands (22 bits: one operand's 11
+// were the largest error of the result), as q is from fp32. Running maxima and sums are fp32.
 //
-// Split. The work is every (sequence, kv head, column group)'s tiles of 64 tokens in one line, of which
-// each CTA takes an equal share, whatever the lengths are: they are read on the device. A unit that
-// lies within a share is written at once; the others' parts (maximum, sum, unnormalised output) go to
-// scratch and are joined in order by a second kernel, so results do not depend on timing.
+// Split, by whether the sequences could be long (their lengths are on the device, the page table's width is not):
+//   Line. The work is every (sequence, kv head, column group)'s tiles of 128 tokens (64 for 256 channels) in
+// one line, of which each CTA takes an equal share, whatever the lengths are. A unit that lies within a share
+// is written at once; the others' parts (maximum, sum, unnormalised output) go to scratch and are joined in
+// order by a second kernel, so results do not depend on timing.
+//   Clusters. A unit's tiles are dealt out to the 2, 4 or 8 CTAs of a cluster, which join their parts through
+// each other's shared memory: no second launch, no scratch.
+//
+// What bounds it: the bytes of the cache. 64 sequences of up to 4096 tokens, 32 kv heads: 181 us, 6.2 TB/s; 4
+// of up to 131072 tokens, 8 kv heads: 164 us, 6.0 TB/s (91 and 88 % of a copy's rate). One sequence of 1001
+// tokens: 9.6 us, latency (12.5 by the line); 16 of up to 3001 with up to 5 drafted tokens, fp32: 23 us.
 #include "attend.cuh"
 
 namespace crvq {
@@ -90,6 +98,56 @@ __device__ __forceinline__ void start_block(const uint8_t* src, uint32_t dst, in
   }
 }
 
+__device__ __forceinline__ float load_remote(const float* p, int rank) {
+  uint32_t at;
+  float v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Joins a unit that its cluster's CTAs hold parts of (outputs [COLS][D] at `ring`, maxima, sums): each takes every
+// cluster-th column, the parts in the order of the ranks.
+template <int D, int COLS>
+__device__ __forceinline__ void join_cluster(const AttendArgs& a, const Unit& u, int col0, int n_cols, const char* ring,
+                                             const float* m_s, const float* l_s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x % a.cluster;
+  const float* o_s = reinterpret_cast<const float*>(ring);
+  cluster_sync();
+  for (int col = rank + warp * a.cluster; col < n_cols; col += kWarps * a.cluster) {
+    const float mine = lane < a.cluster ? load_remote(m_s + col, lane) : -INFINITY;
+    const float sum = lane < a.cluster ? load_remote(l_s + col, lane) : 0.f;
+    float M = mine;
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+    M = __shfl_sync(0xffffffffu, M, 0);
+    const float f = pow2(mine - (M == -INFINITY ? 0.f : M));
+    float L = 0.f, o[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      if (r >= a.cluster) break;
+      const float fr = __shfl_sync(0xffffffffu, f, r);
+      L += __shfl_sync(0xffffffffu, sum, r) * fr;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] += load_remote(o_s + col * D + lane + 32 * e, r) * fr;
+    }
+    const int j = (col0 + col) / a.group, h = u.h * a.group + (col0 + col) % a.group;
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+      store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + lane + 32 * e, a.o.type, o[e] * inv);
+    if (lane == 0 && a.lse)
+      a.lse[(u.s.first + j) * a.q.heads + h] = L > 0.f ? (M + log2f(L)) / kLog2e : (L == 0.f ? -INFINITY : L);
+  }
+  cluster_sync();  // (no CTA leaves while its memory is read)
+}
+
 template <int D, int NT, int FMT, bool SPLIT>
 struct Shape {
   static constexpr int kCols = 8 * NT;
@@ -122,23 +180,38 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
   float* r_s = l_s + kWarps * COLS;                                  // value reference of a warp
   pdl_wait();  // (no early trigger: waiting blocks of the next kernels would take this one's places)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-  const Line<D, COLS> line(a);
-  const int64_t total = line.total;
-  const int shares = (int)min((int64_t)a.shares, total);
-  if ((int)blockIdx.x >= shares) return;
-  const int64_t w1 = share_begin(total, blockIdx.x + 1, shares);
+  const bool cluster = a.cluster > 0;
+  Line<D, COLS> line;
+  int64_t w = 0, w1 = 1;
+  if (!cluster) {
+    line = Line<D, COLS>(a);
+    const int shares = (int)min((int64_t)a.shares, line.total);
+    if ((int)blockIdx.x >= shares) return;
+    w = share_begin(line.total, blockIdx.x, shares);
+    w1 = share_begin(line.total, blockIdx.x + 1, shares);
+  }
   char* mine = ring + warp * S::kRing;
   const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
   const uint32_t key_at = Tile<D>::at(gid, tig);
   const uint32_t val_at[2] = {D == 64 ? Tile<D>::at(2 * tig, gid >> 1) + (gid & 1) * 8 : Tile<D>::at(2 * tig, gid),
                               D == 64 ? Tile<D>::at(2 * tig + 1, gid >> 1) + (gid & 1) * 8 : Tile<D>::at(2 * tig + 1, gid)};
 
-  for (int64_t w = share_begin(total, blockIdx.x, shares); w < w1;) {
-    const Unit u = line.locate(a, w);
-    const int64_t tile0 = u.begin + kStart, unit_end = tile0 + u.s.tiles;
-    const int t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
-    w = min(unit_end, w1);
-    if (u.tile >= t_end) continue;  // (this share ends before the unit's first tile)
+  while (w < w1) {
+    Unit u;
+    int t_end;
+    if (cluster) {
+      if (!Line<D, COLS>::unit(a, blockIdx.x / a.cluster, &u)) return;  // (with its whole cluster)
+      const int rank = blockIdx.x % a.cluster;
+      u.tile = (int)((int64_t)u.s.tiles * rank / a.cluster);
+      t_end = (int)((int64_t)u.s.tiles * (rank + 1) / a.cluster);
+      w = w1;
+    } else {
+      u = line.locate(a, w);
+      const int64_t tile0 = u.begin + kStart, unit_end = tile0 + u.s.tiles;
+      t_end = (int)max((int64_t)0, min(unit_end, w1) - tile0);
+      w = min(unit_end, w1);
+      if (u.tile >= t_end) continue;  // (this share ends before the unit's first tile)
+    }
     const int len = u.s.len, group = a.group;
     const int col0 = u.cg * COLS, n_cols = min(COLS, u.s.n * group - col0);
     __syncthreads();  // the previous unit's shared memory has been read
@@ -494,7 +567,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         }
       }
     __syncthreads();
-    const bool complete = u.tile == 0 && t_end == u.s.tiles;
+    const bool complete = !cluster && u.tile == 0 && t_end == u.s.tiles;
     float* part = a.part + (int64_t)(2 * blockIdx.x + (u.tile == 0 ? 1 : 0)) * S::kSlot;
     for (int col = warp; col < n_cols; col += kWarps) {
       float M = -INFINITY, L = 0.f;
@@ -518,11 +591,17 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         for (int i = 0; i < kWarps; ++i) v += reinterpret_cast<const float*>(ring + i * S::kRing)[col * D + d] * fac[i];
         if (complete)
           store_elem(a.o.data, (u.s.first + j) * a.o.ld_tok + h * a.o.ld_head + d, a.o.type, v * inv);
+        else if (cluster)  // (over warp 0's outputs, of which this lane alone reads this one)
+          reinterpret_cast<float*>(ring)[col * D + d] = v;
         else
           part[col * D + d] = v;
       }
+      __syncwarp();
       if (lane == 0) {
-        if (!complete) {
+        if (cluster) {
+          m_s[col] = M;
+          l_s[col] = L;
+        } else if (!complete) {
           part[COLS * D + col] = M;
           part[COLS * D + COLS + col] = L;
         } else if (a.lse) {
@@ -530,25 +609,65 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         }
       }
     }
+    if (cluster) join_cluster<D, COLS>(a, u, col0, n_cols, ring, m_s, l_s);
   }
+}
+
+// Clusters where a CTA then has no more than this many tiles, whatever the lengths are. Line against clusters, us,
+// for (units, tiles per CTA): (8, 1) 12.5, 9.6; (8, 4) 16.9, 13.3; (32, 2) 17.8, 12.8; (96, 1) 15.0, 11.0;
+// (96, 5) 20.8, 21.9; (130, 8, of 64 channels) 24.6, 23.0; (32, 8) 23.5, 26.0; (8, 16) 24.8, 26.6; (8, 32) 28.5, 44.7.
+constexpr int kClusterTiles = 8;
+
+crvq_status launch_clusters(void (*kernel)(AttendArgs), dim3 grid, int size, size_t smem, cudaStream_t stream,
+                            const AttendArgs& a) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  CRVQ_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+  CRVQ_LAUNCHED();
+  return CRVQ_OK;
 }
 
 template <int D, int NT, int FMT, bool SPLIT>
 crvq_status launch_attend(AttendArgs& a, cudaStream_t stream) {
   using S = Shape<D, NT, FMT, SPLIT>;
+  constexpr int COLS = S::kCols;
   auto kernel = attend_kernel<D, NT, FMT, SPLIT>;
   CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
   a.shares = sm_count() * S::kPerSm;
+  ProfScope ps("cache_attention", stream, (double)a.rows.n_tok * a.q.heads * D);
+  // the most tokens that a unit's columns see, in tiles
+  const int64_t held = (int64_t)a.c.max_pages * a.c.page, seen = a.window > 0 ? min(held, a.window + a.rows.n_tok) : held;
+  const int64_t units = most_units<COLS>(a), most = seen / kTile<D>;
+  for (int size = 8; size >= 2; size /= 2) {
+    if (units * size > a.shares) continue;
+    if (most > kClusterTiles * size) break;
+    a.cluster = size;
+    return launch_clusters(kernel, dim3((unsigned)(units * size)), size, S::kSmem, stream, a);
+  }
   Scratch mem;
   CRVQ_TRY(mem.alloc((size_t)2 * a.shares * S::kSlot * sizeof(float), stream));
   a.part = mem.as<float>();
-  ProfScope ps("cache_attention", stream, (double)a.rows.n_tok * a.q.heads * D);
   CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)a.shares), dim3(kThreads), S::kSmem, stream, a));
   CRVQ_LAUNCHED();
   return launch_join<D, S::kCols>(a, stream);
 }
 
-constexpr int64_t kManyColumns = 128;
+// Columns per sequence, on average, from which tiles of 128 rows (attend_tc.cu) are taken. This form against that, us,
+// for (sequences of up to 4096 tokens x kv heads, columns): (64 x 32, 32) 604, 774; (16 x 8, 32) 51, 61; (16 x 8, 48)
+// 68, 63; (8 x 8, 64) 51, 41; (1 x 8, 64) 22, 27; (64 x 32, 64) 1188, 781; (1 x 8, 128) 30, 31; (1 x 8, 256) 50, 41.
+constexpr int64_t kManyColumns = 64;
 
 template <int D, int FMT, bool SPLIT>
 crvq_status pick_columns(AttendArgs& a, cudaStream_t stream) {
@@ -597,7 +716,6 @@ crvq_status attention(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n
   a.vec_q = vec_ok(a.q);
   a.vec_o = vec_ok(a.o);
   CRVQ_TRY(device_error_word(&a.err));
-  // many columns per sequence on average: tensor-core tiles of 128 rows
   if (D != 256 && a.q.type != CRVQ_F32 && n_tok * a.group >= kManyColumns * (int64_t)a.c.n_seq)
     return launch_attend_many(a, D, cache->format, stream);
   if (D == 64) return pick_format<64>(a, cache->format, stream);

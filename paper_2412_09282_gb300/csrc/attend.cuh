@@ -1,6 +1,7 @@
 // Attention over the paged 8-bit cache: what the kernels share (attend.cu: few queries per sequence on
 // mma.sync; attend_tc.cu: many on tcgen05). Arguments, the split of the work into equal shares of one
-// line, code conversion, and the joining of units that lie in several shares.
+// line, code conversion, and the joining of units that lie in several shares (8.3 us of 24.6 for 16 sequences with
+// up to five queries: latency; the parts are in L2).
 #pragma once
 
 #include "cache.cuh"
@@ -20,6 +21,7 @@ struct AttendArgs {
   float* lse;
   float* part;      // 2 slots per CTA: [cols][D] outputs, [cols] maxima, [cols] sums
   int shares;
+  int cluster;      // CTAs of a unit that join it among themselves (0: shares of the line)
   unsigned* err;
 };
 
@@ -91,6 +93,7 @@ struct Line {
   int64_t cost, end;  // of sequence `lane`
   int64_t total;
 
+  Line() = default;
   static __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b) {
     if (b >= a.c.n_seq) return 0;
     const Seq s = load_seq<D, COLS>(a, b);
@@ -114,7 +117,7 @@ struct Line {
     if (a.c.n_seq > 32) total += __shfl_sync(0xffffffffu, scan(more), 31);
   }
   // Unit number i (sequence by sequence, head by head); false past the last.
-  __device__ bool unit(const AttendArgs& a, int64_t i, Unit* u) const {
+  static __device__ bool unit(const AttendArgs& a, int64_t i, Unit* u) {
     const int lane = threadIdx.x & 31;
     int64_t base = 0;
     for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
@@ -213,7 +216,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs a) {
   Unit u;
   int i0;  // the share that holds the unit's first tile
   if constexpr (BY_UNIT) {
-    if (!line.unit(a, blockIdx.x, &u)) return;
+    if (!Line<D, COLS>::unit(a, blockIdx.x, &u)) return;
     const int64_t first = u.begin + kStart;
     i0 = (int)min((int64_t)shares - 1, divide(first * shares, total));  // within one of it
     while (i0 + 1 < shares && share_begin(total, i0 + 1, shares) <= first) ++i0;
@@ -315,17 +318,26 @@ attend_join_kernel(const __grid_constant__ AttendArgs a) {
   }
 }
 
+// An upper bound of the units: every sequence's columns, rounded up to whole groups.
+template <int COLS>
+int64_t most_units(const AttendArgs& a) {
+  return (a.rows.n_tok * a.group / COLS + a.c.n_seq) * a.c.n_kv;
+}
+
 template <int D, int COLS>
 crvq_status launch_join(const AttendArgs& a, cudaStream_t stream) {
-  // an upper bound of the units: every sequence's columns, rounded up to whole groups
-  const int64_t units = (a.rows.n_tok * a.group / COLS + a.c.n_seq) * a.c.n_kv;
+  const int64_t units = most_units<COLS>(a);
   const dim3 threads(32 * kJoinWarps);
-  // (8 units of 40 parts: 24 us by boundaries, 18 by units; 64 units of 7 parts: 16.5 and 20.5)
-  if (units * kJoinWarps <= a.shares)
-    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, true>, dim3((unsigned)units, COLS), threads, 0, stream, a));
-  else
-    CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, false>, dim3((unsigned)a.shares - 1, COLS > 32 ? 8 : COLS / kJoinWarps),
-                         threads, 0, stream, a));
+  // 8 units of 40 parts, 8 columns: 24 us by boundaries, 18 by units; 64 units of 7 parts: 16.5 and 20.5; 16 units of
+  // 9 parts, 256 columns: 41 and 58.
+  if constexpr (COLS <= 16)
+    if (units * kJoinWarps <= a.shares) {
+      CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, true>, dim3((unsigned)units, COLS), threads, 0, stream, a));
+      CRVQ_LAUNCHED();
+      return CRVQ_OK;
+    }
+  CRVQ_CUDA(launch_pdl(attend_join_kernel<D, COLS, false>, dim3((unsigned)a.shares - 1, COLS > 32 ? 8 : COLS / kJoinWarps),
+                       threads, 0, stream, a));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
 }
