@@ -135,8 +135,9 @@ def crvq_cache_append(cache, k, v, new_off=None, cos=None, sin=None, positions=N
             _device(positions, torch.int32, "positions")
             if positions.shape != (n_tok,) or not positions.is_contiguous():
                 raise ValueError("positions must be contiguous with one entry per token")
-        rot = _lib.crvq_rotary(cos.data_ptr(), sin.data_ptr(), None if positions is None else positions.data_ptr(), cos.shape[0],
-                               max(cos.stride(0), cos.shape[1]), cos.shape[1], int(bool(interleaved)))
+        n_pos, half = cos.shape
+        rot = _lib.crvq_rotary(cos.data_ptr(), sin.data_ptr(), None if positions is None else positions.data_ptr(),
+                               n_pos, max(cos.stride(0), half), half, 1 if interleaved else 0)
     qc = oc = None
     if q is not None:
         if q.shape[0] != n_tok:
