@@ -553,7 +553,7 @@ crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, co
  * Scores, maxima and sums are fp32, products run on the tensor cores with fp32 accumulation. q is
  * taken relative to a power of two per row in one fp16 operand (exact for 16-bit types but for
  * elements below 2^-14 of the row's largest) or, from fp32, in two. The weights p_j are held to 22 bits
- * (two fp16 operands); for 16-bit types of 64 or 128 channels with 64 or more (query, head) pairs per
+ * (two fp16 operands); for bf16 of 64 or 128 channels with 64 or more (query, head) pairs per
  * kv head and sequence on average, which take tiles of 128 rows, to fp16's 11. Work is split over the
  * cached tokens by the lengths on the device and joined in a fixed order: results are identical run to run.
  * Requires q->heads to be a multiple of n_kv.

@@ -47,12 +47,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-// a - fp16(a) for the pair, as fp16
-__device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t hi) {
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-  return half2_bits(a - f.x, b - f.y);
-}
-
 __device__ __forceinline__ int word(const uint4& u, int i) {
   return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
 }

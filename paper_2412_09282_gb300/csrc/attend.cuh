@@ -196,6 +196,12 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// a - fp16(a) for the pair, as fp16
+__device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t hi) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  return half2_bits(a - f.x, b - f.y);
+}
+
 // Joins the parts of units that lie in several shares, in the order of the shares. Two forms:
 //   BY_UNIT (few units, so many parts each): a block per unit (x) and column (y), whose warps take every
 //     eighth part;

@@ -182,7 +182,8 @@ __device__ __noinline__ bool find_part(const AttendArgs& a, const Line<D, kUnit>
   return false;
 }
 
-template <int D, int FMT>
+// TWO: weights in two fp16 pieces (22 bits), for outputs that a single piece's 11 bits would show in.
+template <int D, int FMT, bool TWO>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   using S = TcShape<D>;
@@ -378,58 +379,69 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
             ref = up;
             lref = (float)((int)(__float_as_uint(ref) >> 23) - 127);
           }
-          // weights, over S's own columns (a chunk's scores are in registers before they are overwritten)
+          // weights, over S's own columns (a half's scores are in registers before they are overwritten): in 32
+          // columns each half's, second pieces in the next 32 where there are any
           const float mm = m == -INFINITY ? 0.f : m;
-          if (whole) {
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-              uint32_t u[64];
-              tc::tmem_ld64_wait(s_at + half * 64, u);
-              uint32_t packed[32];
+          for (int half = 0; half < 2; ++half) {
+            uint32_t u[64];
+            tc::tmem_ld64_wait(s_at + half * 64, u);
+            const uint32_t p_at = s_at + (TWO ? 64 : 32) * half;
+            float lw[4], g[4];
 #pragma unroll
-              for (int b = 0; b < 4; ++b) {
-                const float lw = fmaxf(lg_s[buf][4 * half + b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
-                const float g = sk_s[buf][4 * half + b] * f;
-                const uint64_t gg = pair(g, g), bb = pair(bias, bias);
-                uint64_t sum[4];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                  float x, y;
-                  halves(fma2(pair(__uint_as_float(u[16 * b + e]), __uint_as_float(u[16 * b + e + 1])), gg, bb), x, y);
-                  x = pow2(x);
-                  y = pow2(y);
-                  sum[e / 2 & 3] = e < 8 ? pair(x, y) : add2(sum[e / 2 & 3], pair(x, y));
-                  packed[8 * b + e / 2] = half2_bits(x, y);
-                }
-                float s0, s1;
-                halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
-                l = fmaf(s0 + s1, pow2(-lw), l);
-              }
-              tmem_st16(s_at + half * 32, packed);
-              tmem_st16(s_at + half * 32 + 16, packed + 16);
+            for (int b = 0; b < 4; ++b) {
+              lw[b] = fmaxf(lg_s[buf][4 * half + b] - lref, -60.f) + kTcLogWeight;
+              g[b] = sk_s[buf][4 * half + b] * f;
             }
-          } else {
-#pragma unroll 1
-            for (int ch = 0; ch < 4; ++ch) {
-              float v[32];
-              tc::tmem_ld32(s_at + ch * 32, v);
-              uint32_t packed[16];
-              const uint32_t seen = seen32(tok + 32 * ch, &live_s[buf][2 * ch], kb, ke);
+            if (whole) {
 #pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                const float lw = fmaxf(lg_s[buf][2 * ch + b] - lref, -60.f) + kTcLogWeight, bias = lw - mm;
-                const float g = sk_s[buf][2 * ch + b] * f;
-                float sum = 0.f;
+              for (int b = 0; b < 4; b += 2) {
+                uint32_t hi[16], lo[TWO ? 16 : 1];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  float& x = v[16 * b + e];
-                  x = seen >> (16 * b + e) & 1 ? pow2(fmaf(x, g, bias)) : 0.f;
-                  sum += x;
-                  if (e & 1) packed[8 * b + e / 2] = half2_bits(v[16 * b + e - 1], x);
+                for (int e0 = 0; e0 < 32; e0 += 16) {
+                  const int bb = b + e0 / 16;
+                  const uint64_t gg = pair(g[bb], g[bb]), bias = pair(lw[bb] - mm, lw[bb] - mm);
+                  uint64_t sum[4];
+#pragma unroll
+                  for (int e = 0; e < 16; e += 2) {
+                    float x, y;
+                    halves(fma2(pair(__uint_as_float(u[16 * bb + e]), __uint_as_float(u[16 * bb + e + 1])), gg, bias), x, y);
+                    x = pow2(x);
+                    y = pow2(y);
+                    sum[e / 2 & 3] = e < 8 ? pair(x, y) : add2(sum[e / 2 & 3], pair(x, y));
+                    hi[(e0 + e) / 2] = half2_bits(x, y);
+                    if constexpr (TWO) lo[(e0 + e) / 2] = half2_rest(x, y, hi[(e0 + e) / 2]);
+                  }
+                  float s0, s1;
+                  halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+                  l = fmaf(s0 + s1, pow2(-lw[bb]), l);
                 }
-                l = fmaf(sum, pow2(-lw), l);
+                tmem_st16(p_at + b * 8, hi);
+                if constexpr (TWO) tmem_st16(p_at + 32 + b * 8, lo);
               }
-              tmem_st16(s_at + ch * 16, packed);
+            } else {
+#pragma unroll
+              for (int b = 0; b < 4; b += 2) {
+                uint32_t hi[16], lo[TWO ? 16 : 1];
+                const uint32_t seen = seen32(tok + 64 * half + 16 * b, &live_s[buf][4 * half + b], kb, ke);
+#pragma unroll
+                for (int e0 = 0; e0 < 32; e0 += 16) {
+                  const int bb = b + e0 / 16;
+                  const float bias = lw[bb] - mm;
+                  float sum = 0.f;
+#pragma unroll
+                  for (int e = 0; e < 16; e += 2) {
+                    const float x = seen >> (e0 + e) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e]), g[bb], bias)) : 0.f;
+                    const float y = seen >> (e0 + e + 1) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e + 1]), g[bb], bias)) : 0.f;
+                    sum += x + y;
+                    hi[(e0 + e) / 2] = half2_bits(x, y);
+                    if constexpr (TWO) lo[(e0 + e) / 2] = half2_rest(x, y, hi[(e0 + e) / 2]);
+                  }
+                  l = fmaf(sum, pow2(-lw[bb]), l);
+                }
+                tmem_st16(p_at + b * 8, hi);
+                if constexpr (TWO) tmem_st16(p_at + 32 + b * 8, lo);
+              }
             }
           }
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -637,8 +649,10 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           tc::tc_fence_after();
 #pragma unroll
           for (int ks = 0; ks < kKeys / 16; ++ks)
-            mma_ts(tmem + 256 + X * 128, tmem + X * 128 + ks * 8, v_desc + (buf * S::kSide + ks * 2 * (int)S::kBand) / 16, kPv,
-                   i > 0 || ks > 0);
+#pragma unroll
+            for (int z = 0; z < (TWO ? 2 : 1); ++z)
+              mma_ts(tmem + 256 + X * 128, tmem + X * 128 + (TWO ? (ks >> 2) * 64 + z * 32 + (ks & 3) * 8 : ks * 8),
+                     v_desc + (buf * S::kSide + ks * 2 * (int)S::kBand) / 16, kPv, i > 0 || ks > 0 || z > 0);
           commit(&pv_done[X]);
           if (X == groups - 1) commit(&v_empty[buf]);
           if (i + 1 < p.n) {
@@ -664,10 +678,10 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   if (warp == 12) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool TWO>
 crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
   using S = TcShape<D>;
-  auto kernel = attend_tc_kernel<D, FMT>;
+  auto kernel = attend_tc_kernel<D, FMT, TWO>;
   CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
   a.shares = sm_count();
   Scratch mem;
@@ -679,12 +693,20 @@ crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
   return launch_join<D, kUnit>(a, stream);
 }
 
+// (bf16 outputs' own rounding is 8 times a single piece's error. fp16 outputs with a single piece were 1.4 to 1.5 times as
+// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 404 to 502 us.)
+template <int D>
+crvq_status pick_tc(AttendArgs& a, int format, cudaStream_t stream) {
+  const bool two = a.q.type == CRVQ_F16;
+  if (format == CRVQ_KV_INT8)
+    return two ? launch_tc<D, CRVQ_KV_INT8, true>(a, stream) : launch_tc<D, CRVQ_KV_INT8, false>(a, stream);
+  return two ? launch_tc<D, CRVQ_KV_E4M3, true>(a, stream) : launch_tc<D, CRVQ_KV_E4M3, false>(a, stream);
+}
+
 }  // namespace
 
 crvq_status launch_attend_many(AttendArgs& a, int D, int format, cudaStream_t stream) {
-  if (D == 64)
-    return format == CRVQ_KV_INT8 ? launch_tc<64, CRVQ_KV_INT8>(a, stream) : launch_tc<64, CRVQ_KV_E4M3>(a, stream);
-  return format == CRVQ_KV_INT8 ? launch_tc<128, CRVQ_KV_INT8>(a, stream) : launch_tc<128, CRVQ_KV_E4M3>(a, stream);
+  return D == 64 ? pick_tc<64>(a, format, stream) : pick_tc<128>(a, format, stream);
 }
 
 }  // namespace crvq

@@ -212,3 +212,18 @@ def test_chunks_report_bad_pages_and_skip_them():
         w = np.exp(z - z.max())
         ref = (w / w.sum()) @ V[:, 0]
         assert np.abs(out[j, 0] - ref).max() <= 2.0 ** -7 * np.abs(V).max()
+
+
+@pytest.mark.parametrize("d,counts", [(128, [40, 100]), (64, [64, 128])])
+def test_fp16_chunks_are_as_exact_as_their_rounding(d, counts):
+    """fp16 queries are exact operands, weights hold 22 bits: the outputs' rounding is all of the error that shows.
+    Root mean squares over all outputs; 1.05 leaves room for the weights' 2^-21 and the sums' 2^-20."""
+    import paper_2412_09282_gb300 as P
+    host, gpu = U.make(44, [300, 900], 64, 2, d, "int8")
+    q = _queries(45, sum(counts), 16, d, "f16", 2.5)
+    ref, _, _, _ = D.attention(host, q, counts, float(np.float32(1.0 / math.sqrt(d))), True, 0)
+    out = P.crvq_cache_attention(gpu, U.heads(q, "f16"), q_off=U.offsets(counts))
+    P.crvq_sync()
+    err = U.exactly(out).astype(np.float64) - ref
+    rounding = ref.astype(np.float16).astype(np.float64) - ref
+    assert np.sqrt(np.mean(err ** 2)) <= 1.05 * np.sqrt(np.mean(rounding ** 2))
