@@ -302,20 +302,23 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
       float m = -INFINITY, top = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f;  // (m: the reference, top: the maximum)
       for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
         const int buf = tile_no & 1;
+        ok = wait_for(&k_full[buf], (tile_no >> 1) & 1, dead, a.err);
         if (active) {
-          ok = wait_for(&s_full[X], mine_no & 1, dead, a.err);
-          tc::tc_fence_after();
-        }
-        ok = ok && wait_for(&k_full[buf], (tile_no >> 1) & 1, dead, a.err);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (active) {
+          // (while the scores are on their way: what the blocks' scales say)
           const int tok = p.first + i * kKeys;
           const float4 sv0 = *reinterpret_cast<const float4*>(&sv_s[buf][0]), sv1 = *reinterpret_cast<const float4*>(&sv_s[buf][4]);
           const int4 lv0 = *reinterpret_cast<const int4*>(&live_s[buf][0]), lv1 = *reinterpret_cast<const int4*>(&live_s[buf][4]);
           const float sv_top = fmaxf(fmaxf(fmaxf(sv0.x, sv0.y), fmaxf(sv0.z, sv0.w)), fmaxf(fmaxf(sv1.x, sv1.y), fmaxf(sv1.z, sv1.w)));
           const bool whole = (lv0.x & lv0.y & lv0.z & lv0.w & lv1.x & lv1.y & lv1.z & lv1.w) != 0 && tok >= p.every_b &&
                              tok + kKeys <= p.every_e;
+          float up = ref;
+          if (sv_top > ref || i == 0)
+            up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u, 0x7f000000u)),
+                       7.7037197775489434e-34f);
+          ok = ok && wait_for(&s_full[X], mine_no & 1, dead, a.err);
+          tc::tc_fence_after();
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
           // The row's maximum over the tile, then (after the rescale) its weights, 32 columns at a time, in rolled
           // loops: unrolled, the warps' different code overflowed the instruction caches.
           float mt = -INFINITY;
@@ -350,10 +353,6 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
             }
           }
           top = fmaxf(top, mt);
-          float up = ref;
-          if (sv_top > ref || i == 0)
-            up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u, 0x7f000000u)),
-                       7.7037197775489434e-34f);
           const bool need = mt > m + kLazy || (m == -INFINITY && mt > m) || up > ref;
           if (i == 0) {
             m = mt;
@@ -449,7 +448,8 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           tc::mbar_arrive(tc::smem_u32(&p_full[X]));
           ++mine_no;
         }
-        __syncwarp();
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
         if (lane == 0) tc::mbar_arrive(tc::smem_u32(&k_empty[buf]));
       }
       if (!ok) break;
@@ -694,7 +694,7 @@ crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
 }
 
 // (bf16 outputs' own rounding is 8 times a single piece's error. fp16 outputs with a single piece were 1.4 to 1.5 times as
-// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 404 to 502 us.)
+// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 410 to 493 us.)
 template <int D>
 crvq_status pick_tc(AttendArgs& a, int format, cudaStream_t stream) {
   const bool two = a.q.type == CRVQ_F16;
