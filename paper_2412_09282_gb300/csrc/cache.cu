@@ -204,15 +204,6 @@ __device__ __forceinline__ void decode4(uint32_t w, float v[4]) {
   }
 }
 
-// x / s rounded once, for inv = 1 / s rounded once: the first correction brings the product within one unit in the
-// last place, and then the remainder is exact and the second one rounds correctly (Markstein 1990). For s
-// in (2^-80, 2^80) no step that a code depends on leaves the normal numbers.
-__device__ __forceinline__ float quotient(float x, float s, float inv) {
-  float q = __fmul_rn(x, inv);
-  q = __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
-  return __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
-}
-
 // One head's keys or values of a block: this thread's new values x (is_new) or old codes to new codes, with
 // the block's scale, from the largest new magnitude (bits) and the old scale.
 template <int D, int FMT>
@@ -222,7 +213,7 @@ __device__ __forceinline__ void encode_block(float x[16], bool is_new, bool is_o
   const float s = fmaxf(__fmul_rn(__uint_as_float(top), kInv), s0);
   uint32_t w[4];
   if (is_new) {
-    if (s > 0x1p-80f && s < 0x1p80f) {
+    if (plain_divisor(s)) {
       const float inv = __frcp_rn(s);
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = quotient(x[e], s, inv);

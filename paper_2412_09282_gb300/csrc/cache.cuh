@@ -111,6 +111,16 @@ __device__ __forceinline__ int last_not_above(int n, int64_t v, Key key) {
   return lo;
 }
 
+// x / s rounded once, for inv = 1 / s rounded once: the first correction brings the product within one unit in the
+// last place, and then the remainder is exact and the second one rounds correctly (Markstein 1990). For s
+// in (2^-80, 2^80) no step that a code depends on leaves the normal numbers.
+__device__ __forceinline__ float quotient(float x, float s, float inv) {
+  float q = __fmul_rn(x, inv);
+  q = __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
+  return __fmaf_rn(__fmaf_rn(-q, s, x), inv, q);
+}
+__device__ __forceinline__ bool plain_divisor(float s) { return s > 0x1p-80f && s < 0x1p80f; }
+
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, int type) {
   if (type == CRVQ_F32) return static_cast<const float*>(p)[i];
   const uint16_t u = static_cast<const uint16_t*>(p)[i];

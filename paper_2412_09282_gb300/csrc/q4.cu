@@ -552,7 +552,7 @@ struct QuantizeArgs {
   int type;
   bool vec_w, vec_c, vec_h;
   float* W_hat;
-  int64_t threads_row;  // threads per row, whole groups
+  Divisor by_row;  // threads per row, whole groups
   unsigned* err;
 };
 
@@ -561,9 +561,8 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const __grid_constant_
   constexpr int kLanes = GROUP / 8;
   pdl_trigger();
   pdl_wait();
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = at / a.threads_row;
-  const int64_t j0 = (at - row * a.threads_row) * 8, g = j0 / GROUP;
+  const int at = (int)blockIdx.x * 256 + threadIdx.x, row_i = a.by_row.div(at);
+  const int64_t row = row_i, j0 = (int64_t)(at - row_i * (int)a.by_row.d) * 8, g = j0 / GROUP;
   const bool live = row < a.m.M;  // whole groups of lanes
   const int64_t N = a.m.N;
   const int n = live ? (int)max((int64_t)0, min((int64_t)8, N - j0)) : 0;
@@ -574,18 +573,21 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const __grid_constant_
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = e < n ? load_elem(a.W, row * a.ldw + j0 + e, a.type) : 0.f;
   }
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(w[e]) & 0x7fffffffu);
+  if (top >= 0x7f800000u) {
+    raise_error(a.err, ERRBIT_NUMERIC);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(fabsf(w[e]) <= 3.402823466e38f)) w[e] = 0.f;
+  }
   float lo = 0.f, hi = 0.f;
-  bool bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if (!(fabsf(w[e]) <= 3.402823466e38f)) {
-      w[e] = 0.f;
-      bad = true;
-    }
     lo = fminf(lo, w[e]);
     hi = fmaxf(hi, w[e]);
   }
-  if (bad) raise_error(a.err, ERRBIT_NUMERIC);
 #pragma unroll
   for (int d = kLanes / 2; d > 0; d >>= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
@@ -597,13 +599,24 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const __grid_constant_
   const float s = __bfloat162float(s16);
   float z = 8.f;
   if (a.m.zeros) z = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 0.f;
+  if (plain_divisor(s)) {
+    const float inv = __frcp_rn(s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = quotient(w[e], s, inv);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = s > 0.f ? __fdiv_rn(w[e], s) : 0.f;
+  }
+  // Adding 1.5 * 2^23 rounds to an integer (of quotients up to 2^8; others end at the clamps), which the sum's low
+  // bits are.
+  constexpr float kRound = 12582912.f;
   float v[8];
   uint32_t codes = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float q = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(w[e], s)) + z, 0.f), 15.f) : z;
+    const float q = fminf(fmaxf(__fsub_rn(__fadd_rn(fminf(fmaxf(w[e], -64.f), 64.f), kRound), kRound) + z, 0.f), 15.f);
     v[e] = (q - z) * s;
-    if (e < n) codes |= (uint32_t)q << (4 * e);
+    if (e < n) codes |= (__float_as_uint(__fadd_rn(q, kRound)) & 15u) << (4 * e);
   }
   if (n == 0) return;
   uint8_t* c = a.m.codes + row * a.m.ld_codes + j0 / 2;
@@ -757,18 +770,27 @@ crvq_status quantize(const void* W, int64_t ldw, int type, const crvq_q4_matrix*
   a.vec_c = ((uintptr_t)m->codes & 3u) == 0 && m->ld_codes % 4 == 0;
   a.vec_h = ((uintptr_t)W_hat & 15u) == 0 && m->N % 4 == 0;
   a.W_hat = W_hat;
-  a.threads_row = ceil_div(m->N, m->group) * (m->group / 8);
-  const int64_t grid = ceil_div(m->M * a.threads_row, 256);
-  if (grid >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "matrix too large");
+  const int64_t per_row = ceil_div(m->N, m->group) * (m->group / 8), most = ((int64_t)1 << 31) - 256;
+  if (per_row > most) return fail(CRVQ_ERR_UNSUPPORTED, "rows of %lld inputs are too long", (long long)m->N);
+  a.by_row = Divisor(per_row);
   ProfScope ps("q4_quantize", stream, (double)m->M * m->N);
-  const dim3 g((unsigned)grid), t(256);
-  if (m->group == 32)
-    CRVQ_CUDA(launch_pdl(q4_quantize_kernel<32>, g, t, 0, stream, a));
-  else if (m->group == 64)
-    CRVQ_CUDA(launch_pdl(q4_quantize_kernel<64>, g, t, 0, stream, a));
-  else
-    CRVQ_CUDA(launch_pdl(q4_quantize_kernel<128>, g, t, 0, stream, a));
-  CRVQ_LAUNCHED();
+  const int64_t rows = most / per_row;  // of a launch: thread indices have 31 bits
+  for (int64_t r0 = 0; r0 < m->M; r0 += rows) {
+    a.m.M = std::min(rows, m->M - r0);
+    const dim3 g((unsigned)ceil_div(a.m.M * per_row, 256)), t(256);
+    if (m->group == 32)
+      CRVQ_CUDA(launch_pdl(q4_quantize_kernel<32>, g, t, 0, stream, a));
+    else if (m->group == 64)
+      CRVQ_CUDA(launch_pdl(q4_quantize_kernel<64>, g, t, 0, stream, a));
+    else
+      CRVQ_CUDA(launch_pdl(q4_quantize_kernel<128>, g, t, 0, stream, a));
+    CRVQ_LAUNCHED();
+    a.W = static_cast<const char*>(a.W) + rows * ldw * (int64_t)wide;
+    a.m.codes += rows * m->ld_codes;
+    a.m.scales += rows * m->ld_scales;
+    if (a.m.zeros) a.m.zeros += rows * m->ld_scales;
+    if (a.W_hat) a.W_hat += rows * m->N;
+  }
   return CRVQ_OK;
 }
 
