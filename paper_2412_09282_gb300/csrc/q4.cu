@@ -18,6 +18,11 @@
 // order. Where there are fewer tiles than SMs the inputs are sliced over a cluster, whose sums meet in
 // distributed shared memory. One launch, no scratch, sums in a fixed order. (A CTA per tile spent
 // most of its time on laying out inputs and on its own start: 28672 x 8192, one input, 73 us.)
+//
+// What bounds it: instructions. A step of 16 rows takes about 390 (9 per word of 8 codes into operands; the rest
+// products, input reads, scales and places), 0.6 per cycle and scheduler, and a call starts and ends with some 6000 cycles of code
+// that runs once (places, layout, joins). One input: 28672 x 8192 28.3 us, 4.3 TB/s; 11008 x 4096 9.5 us; 512 x 512 3.8 us.
+// 16 inputs, 28672 x 8192: 45.8 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -53,6 +58,8 @@ struct MatvecQ4 {
   int cols;           // columns laid out: b, or 8 NT
   int chunk;          // steps laid out at a time
   int group;          // tiles whose sums are held at a time
+  int log_slices;     // slices of the inputs: CTAs of a cluster
+  int tiles_each, tiles_more, steps_each, steps_more;  // of a cluster and of a slice; the first `more` have one more
 };
 
 __device__ __forceinline__ void mma16(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
@@ -182,7 +189,8 @@ template <int TYPE, int GROUP, int NT, int RT>
 struct MatvecShape {
   static constexpr int kPieces = TYPE == CRVQ_F32 ? 2 : 1;
   static constexpr bool kScaled = TYPE != CRVQ_F16;           // inputs relative to a power of two per group
-  static constexpr int kWarps = NT == 4 ? 8 : 12;
+  // (32 fp32 inputs need 203 to 255 registers; 8, 14 and 16 warps elsewhere: 10, 4 and 0 to 10 % slower)
+  static constexpr int kWarps = NT == 4 && TYPE == CRVQ_F32 ? 8 : 12;
   static constexpr int kStages = NT == 1 ? 3 : 2;             // (more leave less room for inputs)
 
   static constexpr int kGroups = kStep / GROUP;               // groups in a step
@@ -212,17 +220,13 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
   pdl_trigger();
   pdl_wait();
   cg::cluster_group cluster = cg::this_cluster();
-  const int slices = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int slices = 1 << a.log_slices, rank = blockIdx.x & (slices - 1), me = blockIdx.x >> a.log_slices;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
   const Q4View& m = a.m;
   // this CTA's tiles and steps
-  const int64_t tiles = (m.M + R - 1) / R, ctas = gridDim.x / slices, me = blockIdx.x / slices;
-  const int64_t tile0 = tiles * me / ctas;
-  const int n_tiles = (int)(tiles * (me + 1) / ctas - tile0);
-  const int all_steps = (int)((m.N + kStep - 1) / kStep);
-  const int step0 = (int)((int64_t)all_steps * rank / slices);
-  const int n_steps = (int)((int64_t)all_steps * (rank + 1) / slices) - step0;
-  const int n_chunks = (n_steps + a.chunk - 1) / a.chunk;
+  const int tile0 = me * a.tiles_each + min(me, a.tiles_more);
+  const int n_tiles = a.tiles_each + (me < a.tiles_more);
+  const int step0 = rank * a.steps_each + min(rank, a.steps_more), n_steps = a.steps_each + (rank < a.steps_more);
 
   const int ring = warp * S::kRing;  // (offsets from sm: 32-bit shared-memory addresses)
   float* slots = reinterpret_cast<float*>(sm + W * S::kRing);  // [W][COLS][R]
@@ -284,7 +288,7 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
   const __nv_bfloat16* scales = nullptr;
   int64_t zeros = 0;               // (the zero points' offset)
   auto point = [&]() {             // after a tile's or a chunk's first place
-    const int64_t k = (int64_t)(step0 + ahead.c0 + ahead.st) * kStep, row0 = (tile0 + ahead.t0 + ahead.tile) * R;
+    const int64_t k = (int64_t)(step0 + ahead.c0 + ahead.st) * kStep, row0 = (int64_t)(tile0 + ahead.t0 + ahead.tile) * R;
     inside = a.vec_w && row0 + R <= m.M;
     codes = m.codes + (row0 + (lane >> 3)) * m.ld_codes + k / 2 + (lane & 7) * 16;
     zeros = (row0 + (lane >> 1)) * m.ld_scales + k / GROUP + (lane & 1) * kMine;
@@ -325,7 +329,7 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
             held[t][e] = s << 16 | (m.zeros ? __ldg(m.zeros + zeros + t * ld16 + e) & 15u : 8u);
           }
       } else {
-        const int64_t k = (int64_t)step * kStep, row0 = (tile0 + ahead.t0 + ahead.tile) * R;
+        const int64_t k = (int64_t)step * kStep, row0 = (int64_t)(tile0 + ahead.t0 + ahead.tile) * R;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           start_tile_edge(a, row0 + 16 * t, k, sm + ring + slot * S::kStage + t * kTileBytes);
@@ -358,10 +362,10 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
     const int nt = min(a.group, n_tiles - t0);
     if (t0) __syncthreads();  // the previous group's sums have been read
     for (int e = tid; e < nt * S::kSums; e += kThreads) sums[e] = 0.f;
-    for (int ch = 0; ch < n_chunks; ++ch) {
-      Place p = {t0, ch * a.chunk, 0, 0, 0, 0, 0};
+    for (int c0 = 0; c0 < n_steps; c0 += a.chunk) {
+      Place p = {t0, c0, 0, 0, 0, 0, 0};
       enter(p);
-      if (n_chunks > 1 || t0 == 0) {
+      if (n_steps > a.chunk || t0 == 0) {
         __syncthreads();  // the inputs before these have been read
         const int cn = p.nst * (kStep / 8);  // eights of inputs
         const int all = cn * cols;
@@ -519,11 +523,20 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
         }
       }
       __syncthreads();
-      for (int e = tid; e < S::kSums; e += kThreads)
+      for (int e = tid; e < S::kSums; e += kThreads) {
+        float v[W];
+        int t[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          t[i] = slot_tile[i];
+          v[i] = t[i] >= 0 ? slots[i * S::kSums + e] : 0.f;
+        }
+#pragma unroll
         for (int i = 0; i < W; ++i)
-          if (slot_tile[i] >= 0) sums[slot_tile[i] * S::kSums + e] += slots[i * S::kSums + e];
+          if (t[i] >= 0) sums[t[i] * S::kSums + e] += v[i];
+      }
     }
-    const int64_t r0 = (tile0 + t0) * R;
+    const int64_t r0 = (int64_t)(tile0 + t0) * R;
     if (slices == 1) {
       for (int e = tid; e < S::kSums; e += kThreads) {
         const int col = e / R, r = e - col * R;
@@ -533,11 +546,23 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
       }
     } else {
       cluster.sync();
-      for (int e = rank * kThreads + tid; e < nt * S::kSums; e += slices * kThreads) {
-        const int t = e / S::kSums, col = (e - t * S::kSums) / R, r = e % R;
-        float v = 0.f;
-        for (int i = 0; i < slices; ++i) v += cluster.map_shared_rank(sums, i)[e];
-        if (col < a.b && r0 + t * R + r < m.M) store_elem(a.Y, col * a.ldy + r0 + t * R + r, TYPE, v);
+      constexpr int kJoin = 4;  // outputs whose parts are on their way together
+      for (int e0 = rank * kThreads + tid; e0 < nt * S::kSums; e0 += kJoin * slices * kThreads) {
+        float v[kJoin] = {};
+#pragma unroll 2
+        for (int i = 0; i < slices; ++i) {
+          const float* part = cluster.map_shared_rank(sums, i);
+#pragma unroll
+          for (int u = 0; u < kJoin; ++u) {
+            const int e = e0 + u * slices * kThreads;
+            if (e < nt * S::kSums) v[u] += part[e];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kJoin; ++u) {
+          const int e = e0 + u * slices * kThreads, t = e / S::kSums, col = (e - t * S::kSums) / R, r = e % R;
+          if (t < nt && col < a.b && r0 + t * R + r < m.M) store_elem(a.Y, col * a.ldy + r0 + t * R + r, TYPE, v[u]);
+        }
       }
       cluster.sync();  // nobody's sums are read any more
     }
@@ -663,6 +688,7 @@ crvq_status launch_matvec(MatvecQ4& a, cudaStream_t stream) {
   a.cols = a.b <= 8 ? a.b : 8 * NT;
   const int64_t tiles = ceil_div(a.m.M, 16 * RT), sms = sm_count();
   const int64_t steps = ceil_div(a.m.N, kStep);
+  if (tiles >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "M = %lld is too large", (long long)a.m.M);
   if (steps > (1 << 24)) return fail(CRVQ_ERR_UNSUPPORTED, "N = %lld is too large", (long long)a.m.N);
   // Slices, and the tiles whose sums are held at a time: the choice with the least (tile, step) pairs of one row
   // tile on the busiest SM, with what else costs time in such pairs (about 50 ns): laying out inputs a
@@ -691,6 +717,11 @@ crvq_status launch_matvec(MatvecQ4& a, cudaStream_t stream) {
     }
   }
   if (clusters == 0) return fail(CRVQ_ERR_UNSUPPORTED, "matrix too large");
+  a.log_slices = slices == 8 ? 3 : slices == 4 ? 2 : slices == 2 ? 1 : 0;
+  a.tiles_each = (int)(tiles / clusters);
+  a.tiles_more = (int)(tiles % clusters);
+  a.steps_each = (int)(steps / slices);
+  a.steps_more = (int)(steps % slices);
   const size_t smem = S::smem(a.chunk, a.group, a.cols);
   CRVQ_TRY(smem_limit((const void*)kernel, smem));
   ProfScope ps("q4_matvec", stream, (double)a.m.M * a.m.N * a.b);
@@ -715,10 +746,12 @@ crvq_status launch_matvec(MatvecQ4& a, cudaStream_t stream) {
 
 template <int TYPE, int GROUP>
 crvq_status pick_inputs(MatvecQ4& a, cudaStream_t stream) {
-  // more inputs take more of shared memory's bandwidth: two row tiles then share what is read of them
+  // Row tiles of a step: 2 share what is read of the inputs; with more than 8 of those one leaves registers for the
+  // products of a group on their way (28672 x 8192, us with 2 and 1: 16 bf16 inputs 48.5, 45.8; 32 97.5, 77.3; 32 fp32
+  // 155, 126; one input 28.3, 30.9)
   if (a.b <= 8) return launch_matvec<TYPE, GROUP, 1, 2>(a, stream);
-  if (a.b <= 16) return launch_matvec<TYPE, GROUP, 2, 2>(a, stream);
-  return launch_matvec<TYPE, GROUP, 4, 2>(a, stream);
+  if (a.b <= 16) return launch_matvec<TYPE, GROUP, 2, 1>(a, stream);
+  return launch_matvec<TYPE, GROUP, 4, 1>(a, stream);
 }
 
 template <int TYPE>
