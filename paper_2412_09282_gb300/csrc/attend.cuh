@@ -1,5 +1,5 @@
-// Attention over the paged 8-bit cache: what the kernels share (attend.cu: few queries per sequence on
-// mma.sync; attend_tc.cu: many on tcgen05). Arguments, the split of the work into equal shares of one
+// Attention over the paged 8-bit cache: what the kernels share (attend_mma.cuh: few queries per sequence
+// on mma.sync; attend_tc.cu: many on tcgen05). Arguments, the split of the work into equal shares of one
 // line, code conversion, and the joining of units that lie in several shares (8.3 us of 24.6 for 16 sequences with
 // up to five queries: latency; the parts are in L2).
 #pragma once
@@ -21,10 +21,14 @@ struct AttendArgs {
   float* lse;
   float* part;      // 2 slots per CTA: [cols][D] outputs, [cols] maxima, [cols] sums
   int shares;
-  int cluster;      // CTAs of a unit that join it among themselves (0: shares of the line)
+  int cluster;      // CTAs of a unit that join it among themselves, a power of two (0: shares of the line)
+  int log_cluster;
   unsigned* err;
 };
 
+// Few queries, short sequences (attend_cluster.cu): `size` CTAs (2, 4 or 8) per unit of 8 NT columns.
+crvq_status launch_attend_clusters(AttendArgs& a, int D, int NT, int format, int64_t units, int size,
+                                   cudaStream_t stream);
 // Many queries per sequence (attend_tc.cu): 16-bit queries, 64 or 128 channels.
 crvq_status launch_attend_many(AttendArgs& a, int D, int format, cudaStream_t stream);
 
@@ -142,6 +146,34 @@ struct Line {
       }
       i -= __shfl_sync(0xffffffffu, e, 31);
       base += __shfl_sync(0xffffffffu, pe, 31);
+    }
+    return false;
+  }
+  // The same for counts below 2^31, without the unit's places on the line.
+  static __device__ bool unit_only(const AttendArgs& a, int i, Unit* u) {
+    const int lane = threadIdx.x & 31;
+    for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
+      Seq s;
+      s.groups = 0;
+      if (b0 + lane < a.c.n_seq) s = load_seq<D, COLS>(a, b0 + lane);
+      const int units = s.groups * a.c.n_kv;
+      int e = units;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, e, d);
+        if (lane >= d) e += x;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, e > i);
+      if (hit) {
+        const int src = __ffs(hit) - 1;
+        i -= __shfl_sync(0xffffffffu, e - units, src);
+        u->b = b0 + src;
+        u->s = load_seq<D, COLS>(a, u->b);
+        u->h = i / u->s.groups;
+        u->cg = i - u->h * u->s.groups;
+        return true;
+      }
+      i -= __shfl_sync(0xffffffffu, e, 31);
     }
     return false;
   }

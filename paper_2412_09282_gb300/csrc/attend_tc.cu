@@ -12,7 +12,7 @@
 //   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
 // exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
 // only when a row's maximum grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows.
-// Work is split like attend.cu's: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
+// Work is split like attend_mma.cuh's line: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
 #include "attend.cuh"
 #include "tc_ops.cuh"
 
