@@ -7,8 +7,9 @@ namespace crvq {
 namespace {
 
 // Clusters where a CTA then has no more than this many tiles, whatever the lengths are. Line against clusters, us,
-// for (units, tiles per CTA): (8, 1) 12.5, 9.6; (8, 4) 16.9, 13.3; (32, 2) 17.8, 12.8; (96, 1) 15.0, 11.0;
-// (96, 5) 20.8, 21.9; (130, 8, of 64 channels) 24.6, 23.0; (32, 8) 23.5, 26.0; (8, 16) 24.8, 26.6; (8, 32) 28.5, 44.7.
+// for (units, tiles per CTA): (8, 1) 12.1, 8.1; (8, 4) 16.1, 11.4; (32, 2) 17.3, 11.0; (96, 1) 15.0, 9.6;
+// (96, 5) 20.5, 19.6; (130, 8, of 64 channels) 24.7, 20.2; (32, 8) 23.1, 22.7; (8, 16) 24.4, 23.2; (96, 12) 32.6, 38.8;
+// (8, 32) 28.2, 38.8.
 constexpr int kClusterTiles = 8;
 
 template <int D, int NT, int FMT, bool SPLIT>

@@ -23,9 +23,10 @@
 //   Clusters. A unit's tiles are dealt out to the 2, 4 or 8 CTAs of a cluster, which join their parts through
 // each other's shared memory: no second launch, no scratch.
 //
-// What bounds it: the bytes of the cache. 64 sequences of up to 4096 tokens, 32 kv heads: 181 us, 6.2 TB/s; 4
-// of up to 131072 tokens, 8 kv heads: 164 us, 6.0 TB/s (91 and 88 % of a copy's rate). One sequence of 1001
-// tokens: 9.6 us, latency (12.5 by the line); 16 of up to 3001 with up to 5 drafted tokens, fp32: 23 us.
+// What bounds it: the bytes of the cache. 64 sequences of up to 4096 tokens, 32 kv heads: 183 us, 6.2 TB/s; 4
+// of up to 131072 tokens, 8 kv heads: 163 us, 6.0 TB/s (91 and 89 % of a copy's rate). Short calls: the chain of
+// lookups, copies, products and joins of a few tiles. One sequence of 1001 tokens: 8.1 us (12.1 by the line); 16 of up to
+// 3001 with up to 5 drafted tokens, fp32: 20 us (24.7).
 #pragma once
 
 #include "attend.cuh"

@@ -6,13 +6,20 @@
 //   S_X's own columns, O_X += P_X V (P_X read from tensor memory).
 // Twelve warps and one: two softmax groups of four warps (thread = row), four warps that turn the tile's codes into
 // fp16 operands (exact), one that issues the products. While one group's softmax runs, the other group's
-// products do: the tensor core and the softmax each take about half of the time of a tile.
+// products do.
 //   Keys and values have one layout, core matrices of 8 tokens x 8 channels: K-major for Q K^T, and
 // MN-major (channels along N) for P V, so values need no transposition.
 //   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
 // exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
 // only when a row's maximum grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows.
 // Work is split like attend_mma.cuh's line: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
+//
+// What bounds it: a chain of about 5000 cycles per tile and group (waits, row maxima, weights, products), which two
+// groups do not hide: the tensor pipe is active 35 % of the time, 0.44 instructions issue per cycle and scheduler, and
+// no one of maxima, exponentials, operand stores and products takes more than a sixth of the time when left out.
+// Two prompts of up to 1024 tokens over 8192, 64 heads on 8: 410 us, 760 TFLOP/s (39 % of the measured bf16 rate).
+// Steps of 64 keys with scores two steps ahead were slower (520), as were an issuing warp per group (413) and 16
+// softmax warps (spills).
 #include "attend.cuh"
 #include "tc_ops.cuh"
 

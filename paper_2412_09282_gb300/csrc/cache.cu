@@ -12,6 +12,11 @@
 // The grid has a slot for every block that could be touched (the lengths are on the device); the ones
 // that are not leave at once. Each product, difference and quotient is rounded to fp32 by itself (no
 // fused multiply-add): codes do not depend on how the compiler contracts.
+//
+// What bounds it: memory, with the lookups' latency between a CTA's start and its loads. Three fp32 prompts of up to
+// 4091 tokens, 32 heads, queries rotated: 104 us for 544 MB (5.2 TB/s; 30000 CTAs of one block and head each, 12 per
+// SM). Reading them back: 47 us, 302 MB (6.4 TB/s). One thread for K and V both took 179 us (registers); 64-bit
+// divisions for the places and CUDA's division per element, 145.
 #include "cache.cuh"
 
 #include "kernels.h"
