@@ -232,3 +232,26 @@ def test_offsets_beyond_32_bits():
         p = np.exp(z - z.max(1, keepdims=True))
         ref = np.einsum("hn,nhd->hd", p / p.sum(1, keepdims=True), U.exactly(V)[rows].astype(np.float64))
         assert np.abs(U.exactly(out)[b] - ref).max() <= 1e-5
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_append_wide_ranges(fmt):
+    """Blocks whose scales run from subnormal to 2^110 (quotients by corrected products and by division), new and
+    joined by larger and smaller values of a later call: equal to the oracle's codes and scales."""
+    import paper_2412_09282_gb300 as P
+    rng = np.random.default_rng(60)
+    exps = [-140, -126, -110, -80, -74, -72, -71, -40, 0, 50, 84, 86, 87, 88, 89, 110]
+    host, _ = U.make(61, [0] * 16, 16, 1, 64, fmt, wide=1, spare=16)
+    host["pages"] = np.arange(16, dtype=np.int32)[:, None].copy()
+    host["lens"] = np.full(16, 9, np.int32)
+    gpu = U.on_gpu(host, fmt)
+    for step, (n, by) in enumerate(((9, 0), (3, 6), (2, -9))):
+        if step:
+            host["lens"] = host["lens"] + np.int32(n)
+            gpu.lens.add_(n)
+        x = {name: np.ldexp(rng.standard_normal((16 * n, 1, 64)), np.repeat(exps, n)[:, None, None] + by).astype(np.float32)
+             for name in ("K", "V")}
+        D.append(host, x, [n] * 16, fmt)
+        P.crvq_cache_append(gpu, U.heads(x["K"], "f32"), U.heads(x["V"], "f32"))
+        P.crvq_sync()
+        _same_cache(gpu, host, None, None)

@@ -136,3 +136,24 @@ def test_quantize_reports_what_is_not_finite_and_refusals():
     with pytest.raises(P.CrvqError) as e:
         P.crvq_q4_quantize(W, 96)
     assert e.value.status == -2
+
+
+@pytest.mark.parametrize("symmetric", [True, False])
+def test_quantize_wide_ranges_and_ties(symmetric):
+    """Rows from subnormal to 2^120 (quotients by corrected products and by division), and weights halfway between
+    two levels: codes, scales and values equal to the oracle's."""
+    import paper_2412_09282_gb300 as P
+    rng = np.random.default_rng(48)
+    exps = np.array([-147, -140, -128, -120, -100, -82, -81, -80, -79, -78, -77, -76, -60, -3, 0, 5, 60, 76, 77, 78, 79, 80,
+                     81, 82, 83, 84, 100, 120])
+    W = np.ldexp(rng.standard_normal((len(exps), 128)), exps[:, None]).astype(np.float32)
+    ties = np.tile((np.arange(128) % 15 - 7.5).astype(np.float32), (2, 1))    # scale 7.5 / 7 or 1, both rounded to bf16
+    ties[1] = np.clip(ties[1], -7, 7)
+    ties[1, 0] = 7                                                            # scale 1: halves are ties
+    W = np.concatenate([W, ties])
+    codes, scales, zeros = D.q4_quantize(W, 64, symmetric)
+    m, W_hat = P.crvq_q4_quantize(torch.from_numpy(W).cuda(), 64, symmetric, want_W_hat=True)
+    P.crvq_sync()
+    assert np.array_equal(U.exactly(m.scales), scales)
+    assert np.array_equal(D.unpack(m.codes.cpu().numpy(), 128), codes)
+    assert np.array_equal(U.exactly(W_hat), D.q4_values(codes, scales, zeros, 64).astype(np.float32))
