@@ -52,6 +52,8 @@ def append(cache, x, counts, fmt):
     for b, n in enumerate(counts):
         length = int(cache["lens"][b])
         held = length - n
+        if n == 0:
+            continue
         for p0 in range(held // BLOCK * BLOCK, length, BLOCK):
             pg, at = place(cache["pages"], page, b, p0)
             end = min(p0 + BLOCK, length)

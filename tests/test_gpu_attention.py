@@ -227,3 +227,20 @@ def test_fp16_chunks_are_as_exact_as_their_rounding(d, counts):
     err = U.exactly(out).astype(np.float64) - ref
     rounding = ref.astype(np.float16).astype(np.float64) - ref
     assert np.sqrt(np.mean(err ** 2)) <= 1.05 * np.sqrt(np.mean(rounding ** 2))
+
+
+@pytest.mark.parametrize("n_seq,n_kv,group,most", [
+    (40, 1, 3, 2),       # clusters of CTAs
+    (300, 2, 4, 2),      # shares of a line
+    (40, 1, 2, 70),      # tiles of 128 rows
+])
+def test_many_sequences(n_seq, n_kv, group, most):
+    """More sequences than a warp's lanes, of which some are empty or ask nothing."""
+    rng = np.random.default_rng(46)
+    lens = rng.integers(0, 90, n_seq).tolist()
+    counts = [int(rng.integers(min(n, most) // 2, min(n, most) + 1)) if i % 5 else 0 for i, n in enumerate(lens)]
+    if most > 2:
+        lens, counts = [n + 70 for n in lens], [most if i % 5 else 0 for i in range(n_seq)]
+    host, gpu = U.make(47, lens, 16, n_kv, 64, "e4m3")
+    q = _queries(48, sum(counts), n_kv * group, 64, "bf16")
+    _check(host, gpu, q, counts, "bf16")

@@ -255,3 +255,11 @@ def test_append_wide_ranges(fmt):
         P.crvq_cache_append(gpu, U.heads(x["K"], "f32"), U.heads(x["V"], "f32"))
         P.crvq_sync()
         _same_cache(gpu, host, None, None)
+
+
+@pytest.mark.parametrize("n_seq", [33, 70, 1100])
+def test_append_many_sequences(n_seq):
+    """More sequences than a warp's lanes, and than offsets fit beside the kernel's data; many without new tokens."""
+    rng = np.random.default_rng(62)
+    held, new = rng.integers(0, 40, n_seq).tolist(), rng.choice([0, 0, 1, 1, 2, 19], n_seq).tolist()
+    test_append_ragged("int8", "bf16", 64, 16, 1, held, new)
