@@ -47,11 +47,13 @@ def _type(t, name):
 
 def _heads(t, name, head_dim):
     """crvq_heads of a tokens x heads x head_dim view with unit stride in the last dimension."""
-    code = _type(t, name)
-    stride = t.stride()
-    if len(stride) != 3 or stride[2] != 1 or t.shape[2] != head_dim:
+    code = _TYPES.get(t.dtype)
+    if code is None or not t.is_cuda:
+        _type(t, name)                                           # (raises)
+    shape, stride = t.shape, t.stride()
+    if len(stride) != 3 or stride[2] != 1 or shape[2] != head_dim:
         raise ValueError(f"{name} must be tokens x heads x {head_dim} with unit stride in the last dimension")
-    return _lib.crvq_heads(t.data_ptr(), stride[0], stride[1], t.shape[1], code)
+    return _lib.crvq_heads(t.data_ptr(), stride[0], stride[1], shape[1], code)
 
 
 def _offsets(off, n_seq, name):
