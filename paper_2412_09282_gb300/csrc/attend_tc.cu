@@ -11,8 +11,9 @@
 // MN-major (channels along N) for P V, so values need no transposition.
 //   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
 // exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
-// only when a row's maximum grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows.
-// Work is split like attend_mma.cuh's line: equal shares of one line, a CTA per SM; units that lie in two shares are joined.
+// only when a maximum of a warp's rows grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows,
+// and then to every row's maximum. fp16 outputs take the weights in two pieces, side by side over S's columns.
+// Work is split like attend_mma.cuh's line: equal shares, a CTA per SM; units that lie in two shares are joined.
 //
 // What bounds it: a chain of about 5000 cycles per tile and group (waits, row maxima, weights, products), which two
 // groups do not hide: the tensor pipe is active 35 % of the time, 0.44 instructions issue per cycle and scheduler, and
@@ -326,7 +327,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           tc::tc_fence_after();
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          // The row's maximum over the tile, then (after the rescale) its weights, 32 columns at a time, in rolled
+          // The row's maximum over the tile, then (after the rescale) its weights, half a tile at a time, in rolled
           // loops: unrolled, the warps' different code overflowed the instruction caches.
           float mt = -INFINITY;
           if (whole) {
