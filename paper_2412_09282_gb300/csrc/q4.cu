@@ -21,7 +21,7 @@
 //
 // What bounds it: instructions. A step of 16 rows takes about 390 (9 per word of 8 codes into operands; the rest
 // products, input reads, scales and places), 0.6 per cycle and scheduler, and a call starts and ends with some 6000 cycles of code
-// that runs once (places, layout, joins). One input: 28672 x 8192 28.3 us, 4.3 TB/s; 11008 x 4096 9.5 us; 512 x 512 3.8 us.
+// that runs once (places, layout, joins). One input: 28672 x 8192 27.5 us, 4.4 TB/s; 11008 x 4096 9.0 us; 512 x 512 3.5 us.
 // 16 inputs, 28672 x 8192: 45.8 us.
 #include <cooperative_groups.h>
 
@@ -191,7 +191,7 @@ struct MatvecShape {
   static constexpr bool kScaled = TYPE != CRVQ_F16;           // inputs relative to a power of two per group
   // (32 fp32 inputs need 203 to 255 registers; 8, 14 and 16 warps elsewhere: 10, 4 and 0 to 10 % slower)
   static constexpr int kWarps = NT == 4 && TYPE == CRVQ_F32 ? 8 : 12;
-  static constexpr int kStages = NT == 1 ? 3 : 2;             // (more leave less room for inputs)
+  static constexpr int kStages = 2;                           // (3: 3 % slower, and less room for inputs)
 
   static constexpr int kGroups = kStep / GROUP;               // groups in a step
   static constexpr int kScales = 16 * RT * kGroups;           // scales of a step's rows, with zero points, 4 bytes
@@ -369,7 +369,8 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
         __syncthreads();  // the inputs before these have been read
         const int cn = p.nst * (kStep / 8);  // eights of inputs
         const int all = cn * cols;
-        constexpr int kAhead = TYPE == CRVQ_F32 ? 2 : 4;  // loads on their way together
+        // loads on their way together (few inputs: what counts is that code that runs once is short; 4: 2 % slower)
+        constexpr int kAhead = NT == 1 ? 1 : TYPE == CRVQ_F32 ? 2 : 4;
         for (int e0 = 0; e0 < all; e0 += kThreads * kAhead) {  // (whole warps: 32 eights of one column)
           float xa[kAhead][8];
 #pragma unroll
@@ -750,7 +751,7 @@ template <int TYPE, int GROUP>
 crvq_status pick_inputs(MatvecQ4& a, cudaStream_t stream) {
   // Row tiles of a step: 2 share what is read of the inputs; with more than 8 of those one leaves registers for the
   // products of a group on their way (28672 x 8192, us with 2 and 1: 16 bf16 inputs 48.5, 45.8; 32 97.5, 77.3; 32 fp32
-  // 155, 126; one input 28.3, 30.9)
+  // 155, 126; one input 28.7, 30.9)
   if (a.b <= 8) return launch_matvec<TYPE, GROUP, 1, 2>(a, stream);
   if (a.b <= 16) return launch_matvec<TYPE, GROUP, 2, 1>(a, stream);
   return launch_matvec<TYPE, GROUP, 4, 1>(a, stream);
