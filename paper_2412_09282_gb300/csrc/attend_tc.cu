@@ -9,10 +9,13 @@
 // products do.
 //   Keys and values have one layout, core matrices of 8 tokens x 8 channels: K-major for Q K^T, and
 // MN-major (channels along N) for P V, so values need no transposition.
-//   The key scales multiply scores in the softmax. A value scale s is an addend log2(s / ref) in the weights'
-// exponent, ref the power of two at the largest scale so far; the sum takes it out again. O is rescaled
-// only when a maximum of a warp's rows grows by more than 2^8 (weights are at most 2^14 in fp16) or ref grows,
-// and then to every row's maximum. fp16 outputs take the weights in two pieces, side by side over S's columns.
+//   The key scales multiply scores in the softmax. A value scale s is an addend log2(s) in the weights' exponent,
+// from which the sum takes it out again. Weights are relative to a power of two of their row, at the largest p s of
+// the tokens that the row sees: fp16 has 2^-24 to 2^16, and a common reference (the largest scale of a tile, say) would
+// leave nothing of a row that does not see the token with that scale, or gives it no weight. O is rescaled
+// only when that of a warp's rows grows by more than 2^8 (weights are at most 2^14 in fp16), and then to every row's
+// present one; a score's maximum that grows rescales the sum alone. fp16 outputs take the weights in two pieces, side
+// by side over S's columns.
 // Work is split like attend_mma.cuh's line: equal shares, a CTA per SM; units that lie in two shares are joined.
 //
 // What bounds it: a chain of about 5000 cycles per tile and group (waits, row maxima, weights, products), which two
@@ -32,8 +35,7 @@ constexpr int kRows = 128;                // rows of a group
 constexpr int kUnit = 2 * kRows;          // columns of a unit
 constexpr int kKeys = 128;                // tokens of a tile
 constexpr int kTcThreads = 13 * 32;
-constexpr float kTcWeight = 64.f;         // weights are scaled by it, and up to 2^8 more before a rescale
-constexpr float kTcLogWeight = 6.f;
+constexpr float kTcLogWeight = 6.f;       // weights are scaled by 2^6, and up to 2^8 more before a rescale
 constexpr float kLazy = 8.f;
 constexpr uint32_t kTmemCols = 512;       // S_0, S_1 at 0, 128; O_0, O_1 at 256, 384
 
@@ -137,6 +139,9 @@ __device__ __forceinline__ void store_codes(char* dst, const uint4& u) {
   *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
 }
 
+__device__ __forceinline__ float4 four(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float of(const float4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
 // Which of the 32 tokens from t0 on (two blocks) a row sees, as bits.
 __device__ __forceinline__ uint32_t seen32(int t0, const int* live, int kb, int ke) {
   const int lo = min(max(kb - t0, 0), 32), hi = min(max(ke - t0, 0), 32);
@@ -198,7 +203,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(128) char sm[];
   __shared__ __align__(8) uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2],
       q_full[2], all_done;
-  __shared__ __align__(16) float sk_s[2][8], sv_s[2][8], lg_s[2][8];  // scales of a tile's blocks, log2 of the values'
+  __shared__ __align__(16) float sk_s[2][8], lg_s[2][8];  // key scales of a tile's blocks, log2 of the values'
   __shared__ __align__(16) int live_s[2][8];
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_s;
@@ -307,34 +312,31 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
         tc::fence_async_smem();
         tc::mbar_arrive(tc::smem_u32(&q_full[X]));
       }
-      float m = -INFINITY, top = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f;  // (m: the reference, top: the maximum)
+      // All in log2: the score that the sum l is relative to, a whole number at the maximum or above; the weights'
+      // reference and what it should be, the largest score + log2 s (whole numbers: rescales are exact).
+      float m = -INFINITY, l = 0.f, ref = -INFINITY, top = -INFINITY;
       for (int i = 0; i < p.n && ok; ++i, ++tile_no) {
         const int buf = tile_no & 1;
         ok = wait_for(&k_full[buf], (tile_no >> 1) & 1, dead, a.err);
         if (active) {
           // (while the scores are on their way: what the blocks' scales say)
           const int tok = p.first + i * kKeys;
-          const float4 sv0 = *reinterpret_cast<const float4*>(&sv_s[buf][0]), sv1 = *reinterpret_cast<const float4*>(&sv_s[buf][4]);
           const int4 lv0 = *reinterpret_cast<const int4*>(&live_s[buf][0]), lv1 = *reinterpret_cast<const int4*>(&live_s[buf][4]);
-          const float sv_top = fmaxf(fmaxf(fmaxf(sv0.x, sv0.y), fmaxf(sv0.z, sv0.w)), fmaxf(fmaxf(sv1.x, sv1.y), fmaxf(sv1.z, sv1.w)));
           const bool whole = (lv0.x & lv0.y & lv0.z & lv0.w & lv1.x & lv1.y & lv1.z & lv1.w) != 0 && tok >= p.every_b &&
                              tok + kKeys <= p.every_e;
-          float up = ref;
-          if (sv_top > ref || i == 0)
-            up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u, 0x7f000000u)),
-                       7.7037197775489434e-34f);
           ok = ok && wait_for(&s_full[X], mine_no & 1, dead, a.err);
           tc::tc_fence_after();
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          // The row's maximum over the tile, then (after the rescale) its weights, half a tile at a time, in rolled
+          // The row's maxima over the tile, then (after the rescale) its weights, half a tile at a time, in rolled
           // loops: unrolled, the warps' different code overflowed the instruction caches.
-          float mt = -INFINITY;
+          float mt = -INFINITY, rt = -INFINITY;
           if (whole) {
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
               uint32_t u[64];
               tc::tmem_ld64_wait(s_at + half * 64, u);
+              const float4 sk4 = four(&sk_s[buf][4 * half]), lg4 = four(&lg_s[buf][4 * half]);
 #pragma unroll
               for (int b = 0; b < 4; ++b) {
                 float t[8];
@@ -345,7 +347,9 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
                 for (int w2 = 4; w2 > 0; w2 >>= 1)
 #pragma unroll
                   for (int e = 0; e < w2; ++e) t[e] = fmaxf(t[e], t[e + w2]);
-                mt = fmaxf(mt, t[0] * (sk_s[buf][4 * half + b] * f));
+                const float best = t[0] * (of(sk4, b) * f);
+                mt = fmaxf(mt, best);
+                rt = fmaxf(rt, best + of(lg4, b));
               }
             }
           } else {
@@ -355,23 +359,28 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
               tc::tmem_ld32(s_at + ch * 32, v);
               const uint32_t seen = seen32(tok + 32 * ch, &live_s[buf][2 * ch], kb, ke);
               const float s0 = sk_s[buf][2 * ch] * f, s1 = sk_s[buf][2 * ch + 1] * f;
+              float best[2] = {-INFINITY, -INFINITY};
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (seen >> e & 1) mt = fmaxf(mt, v[e] * (e < 16 ? s0 : s1));
+                if (seen >> e & 1) best[e / 16] = fmaxf(best[e / 16], v[e] * (e < 16 ? s0 : s1));
+              mt = fmaxf(mt, fmaxf(best[0], best[1]));
+              rt = fmaxf(rt, fmaxf(best[0] + lg_s[buf][2 * ch], best[1] + lg_s[buf][2 * ch + 1]));
             }
           }
-          top = fmaxf(top, mt);
-          const bool need = mt > m + kLazy || (m == -INFINITY && mt > m) || up > ref;
+          const float mn = fmaxf(m, ceilf(mt));
+          if (mn != m) l *= pow2(m - mn);
+          m = mn;
+          top = fmaxf(top, ceilf(rt));
+          const bool need = top > ref + kLazy || (ref == -INFINITY && top > ref);
           if (i == 0) {
-            m = mt;
+            ref = top;
           } else if (__any_sync(0xffffffffu, need)) {
             ok = wait_for(&pv_done[X], (mine_no - 1) & 1, dead, a.err);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc::tc_fence_after();
-            const float back = m == top ? 1.f : pow2(m - top), fac = back * (ref / up);
-            m = top;  // (every row's: the warp's other rows will need it later)
-            l *= back;
+            const float fac = ref == top ? 1.f : pow2(ref - top);
+            ref = top;  // (every row's: the warp's other rows will need it later)
 #pragma unroll 1
             for (int ch = 0; ch < D / 32; ++ch) {
               float v[32];
@@ -382,23 +391,22 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
               tc::tmem_st32_wait(o_at + ch * 32, u);
             }
           }
-          if (up != ref) {
-            ref = up;
-            lref = (float)((int)(__float_as_uint(ref) >> 23) - 127);
-          }
           // weights, over S's own columns (a half's scores are in registers before they are overwritten): in 32
           // columns each half's, second pieces in the next 32 where there are any
-          const float mm = m == -INFINITY ? 0.f : m;
+          const float mm = m == -INFINITY ? 0.f : m, rr = (ref == -INFINITY ? 0.f : ref) - kTcLogWeight;
+          const float least = -54.f - mm;  // (2^-60 of the largest weight instead of less: the sum is taken from it, too)
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             uint32_t u[64];
             tc::tmem_ld64_wait(s_at + half * 64, u);
             const uint32_t p_at = s_at + (TWO ? 64 : 32) * half;
-            float lw[4], g[4];
+            const float4 sk4 = four(&sk_s[buf][4 * half]), lg4 = four(&lg_s[buf][4 * half]);
+            float bias[4], g[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-              lw[b] = fmaxf(lg_s[buf][4 * half + b] - lref, -60.f) + kTcLogWeight;
-              g[b] = sk_s[buf][4 * half + b] * f;
+              const float lw = of(lg4, b) - rr;
+              bias[b] = lw < least ? least : lw;  // (a scale that is no number stays one)
+              g[b] = of(sk4, b) * f;
             }
             if (whole) {
 #pragma unroll
@@ -407,12 +415,12 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                 for (int e0 = 0; e0 < 32; e0 += 16) {
                   const int bb = b + e0 / 16;
-                  const uint64_t gg = pair(g[bb], g[bb]), bias = pair(lw[bb] - mm, lw[bb] - mm);
+                  const uint64_t gg = pair(g[bb], g[bb]), bias2 = pair(bias[bb], bias[bb]);
                   uint64_t sum[4];
 #pragma unroll
                   for (int e = 0; e < 16; e += 2) {
                     float x, y;
-                    halves(fma2(pair(__uint_as_float(u[16 * bb + e]), __uint_as_float(u[16 * bb + e + 1])), gg, bias), x, y);
+                    halves(fma2(pair(__uint_as_float(u[16 * bb + e]), __uint_as_float(u[16 * bb + e + 1])), gg, bias2), x, y);
                     x = pow2(x);
                     y = pow2(y);
                     sum[e / 2 & 3] = e < 8 ? pair(x, y) : add2(sum[e / 2 & 3], pair(x, y));
@@ -421,7 +429,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
                   }
                   float s0, s1;
                   halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
-                  l = fmaf(s0 + s1, pow2(-lw[bb]), l);
+                  l = fmaf(s0 + s1, pow2(-mm - bias[bb]), l);
                 }
                 tmem_st16(p_at + b * 8, hi);
                 if constexpr (TWO) tmem_st16(p_at + 32 + b * 8, lo);
@@ -434,17 +442,16 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                 for (int e0 = 0; e0 < 32; e0 += 16) {
                   const int bb = b + e0 / 16;
-                  const float bias = lw[bb] - mm;
                   float sum = 0.f;
 #pragma unroll
                   for (int e = 0; e < 16; e += 2) {
-                    const float x = seen >> (e0 + e) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e]), g[bb], bias)) : 0.f;
-                    const float y = seen >> (e0 + e + 1) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e + 1]), g[bb], bias)) : 0.f;
+                    const float x = seen >> (e0 + e) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e]), g[bb], bias[bb])) : 0.f;
+                    const float y = seen >> (e0 + e + 1) & 1 ? pow2(fmaf(__uint_as_float(u[16 * bb + e + 1]), g[bb], bias[bb])) : 0.f;
                     sum += x + y;
                     hi[(e0 + e) / 2] = half2_bits(x, y);
                     if constexpr (TWO) lo[(e0 + e) / 2] = half2_rest(x, y, hi[(e0 + e) / 2]);
                   }
-                  l = fmaf(sum, pow2(-lw[bb]), l);
+                  if (sum != 0.f) l = fmaf(sum, pow2(-mm - bias[bb]), l);  // (an unseen scale may be anything)
                 }
                 tmem_st16(p_at + b * 8, hi);
                 if constexpr (TWO) tmem_st16(p_at + 32 + b * 8, lo);
@@ -470,7 +477,7 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
         tc::tc_fence_after();
       }
       const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-      const float fac = p.n > 0 ? ref * (1.f / kTcWeight) * (complete ? inv : 1.f) : 0.f;
+      const float fac = p.n > 0 ? pow2(ref - kTcLogWeight - (m == -INFINITY ? 0.f : m)) * (complete ? inv : 1.f) : 0.f;
       float* part = a.part + (int64_t)(2 * blockIdx.x + (p.u.tile == 0 ? 1 : 0)) * S::kSlot;
       if (active) {
         // 32 columns at a time through this warp's rows of Q's memory (read whole by now), then rows by neighbouring
@@ -595,7 +602,6 @@ attend_tc_kernel(const __grid_constant__ AttendArgs a) {
           if (!ok) break;
           if (lane < 2) {
             sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
-            sv_s[buf][2 * cw + lane] = lane ? sv[1] : sv[0];
             lg_s[buf][2 * cw + lane] = log2f(lane ? sv[1] : sv[0]);
             live_s[buf][2 * cw + lane] = (lane ? at[1] : at[0]) >= 0;
           }
