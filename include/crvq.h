@@ -554,7 +554,9 @@ crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, co
  * taken relative to a power of two per row in one fp16 operand (exact for 16-bit types but for
  * elements below 2^-14 of the row's largest) or, from fp32, in two. The weights p_j are held to 22 bits
  * (two fp16 operands); for bf16 of 64 or 128 channels with 64 or more (query, head) pairs per
- * kv head and sequence on average, which take tiles of 128 rows, to fp16's 11. Work is split over the
+ * kv head and sequence on average, which take tiles of 128 rows, to fp16's 11. They are held relative to the largest
+ * p_j * (value scale) of the keys that the query sees; from 2^-24 of it on (2^-16 for those tiles) smaller ones lose
+ * bits, and those below 2^-38 (2^-30) count as 0. Work is split over the
  * cached tokens by the lengths on the device and joined in a fixed order: results are identical run to run.
  * Requires q->heads to be a multiple of n_kv.
  */

@@ -41,7 +41,7 @@ template <int D>
 constexpr int kBlocks = D == 256 ? 1 : 2;
 template <int D>
 constexpr int kTile = kCacheBlock * kBlocks<D> * kWarps;  // tokens of a CTA at a time
-constexpr float kWeight = 16384.f;           // weights are scaled into fp16's range
+constexpr float kLogWeight = 14.f;           // weights are scaled by 2^14 into fp16's range
 constexpr float kLog2e = 1.4426950408889634f;
 
 // 2^x (within 2 ulp; results below 2^-126 are 0)

@@ -10,10 +10,12 @@
 // 16 consecutive codes of one token row. Blocks are copied to shared memory by a warp's 32 lanes 512
 // consecutive bytes at a time, two steps ahead, and their codes become fp16 by byte permutes (int8:
 // 1024 + code + 128, less 1152; exact) or by one conversion per pair (e4m3; exact).
-//   The key scale multiplies the block's scores in fp32. The value scale multiplies the weights,
-// relative to the largest scale so far (a power of two), so that a weight is at most 2^14 whatever the
-// scales are; weights below 2^-38 of that vanish. A weight is two fp16 operands (22 bits: one operand's 11
-// were the largest error of the result), as q is from fp32. Running maxima and sums are fp32.
+//   The key scale multiplies the block's scores in fp32. The value scale s multiplies the weights, which are
+// relative to a power of two of their column, at the largest p s of the tokens that the column sees: a weight is at
+// most 2^14, and those below 2^-38 of that vanish. (Relative to the largest scale instead, nothing is left of a column that
+// does not see the token with that scale, or gives it no weight.) A weight is two fp16 operands (22 bits: one
+// operand's 11 were the largest error of the result), as q is from fp32. Running maxima, rounded up to whole
+// numbers in log2 so that rescales are exact, and sums are fp32.
 //
 // Split, by whether the sequences could be long (their lengths are on the device, the page table's width is not):
 //   Line. The work is every (sequence, kv head, column group)'s tiles of 128 tokens (64 for 256 channels) in
@@ -26,7 +28,7 @@
 // What bounds it: the bytes of the cache. 64 sequences of up to 4096 tokens, 32 kv heads: 183 us, 6.2 TB/s; 4
 // of up to 131072 tokens, 8 kv heads: 163 us, 6.0 TB/s (91 and 89 % of a copy's rate). Short calls: the chain of
 // lookups, copies, products and joins of a few tiles. One sequence of 1001 tokens: 8.1 us (12.1 by the line); 16 of up to
-// 3001 with up to 5 drafted tokens, fp32: 20 us (24.7).
+// 3001 with up to 5 drafted tokens, fp32: 21 us (26 by the line).
 #pragma once
 
 #include "attend.cuh"
@@ -174,7 +176,7 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
   int* end_s = beg_s + COLS;
   float* m_s = reinterpret_cast<float*>(end_s + COLS);               // [kWarps][COLS]
   float* l_s = m_s + kWarps * COLS;
-  float* r_s = l_s + kWarps * COLS;                                  // value reference of a warp
+  float* r_s = l_s + kWarps * COLS;                                  // weights' reference
   pdl_wait();  // (no early trigger: waiting blocks of the next kernels would take this one's places)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
   Line<D, COLS> line;
@@ -333,7 +335,10 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
     const int every_b = beg_s[n_cols - 1], every_e = end_s[0];
 
     float o[D / 16][NT][4];
-    float m[NT][2], l[NT][2], ref = 0.f, inv_ref = 0.f;
+    // in log2, whole numbers: m at the largest score or above, and in shared memory (two reads a step, and registers are
+    // scarce) the weights' reference at the largest score + log2 s or above
+    float m[NT][2], l[NT][2];
+    float2* refs = reinterpret_cast<float2*>(r_s + warp * COLS) + tig;  // of this lane's columns: 4 further on for n + 1
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -347,6 +352,10 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         m[t][e] = -INFINITY;
         l[t][e] = 0.f;
       }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      if (gid == 0) refs[4 * t] = make_float2(-INFINITY, -INFINITY);
+    __syncwarp();
 
     // S^T of step i's keys (what lies there is masked later where no key does)
     auto scores = [&](int i, float s[NB][NT][4]) {
@@ -411,13 +420,15 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
 
       // scores in units of log2, masked (a block that no query sees: all of it); their maxima
       const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e && (live & kAll) == kAll;
-      float top[NT][2];
-      bool grew = false;
+      float lg[NB];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int b = 0; b < NB; ++b) lg[b] = __log2f(sv[b]);
+      bool grew = false;  // in this lane's tokens (the lanes' maxima are joined only when one has)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float2 r = refs[4 * n];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float v = -INFINITY;
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const float g = f[n][e] * sk[b];
@@ -429,55 +440,64 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
               if (!in || t0 < kb[n][e] || t0 >= ke[n][e]) s[b][n][e] = -INFINITY;
               if (!in || t0 + 8 < kb[n][e] || t0 + 8 >= ke[n][e]) s[b][n][e + 2] = -INFINITY;
             }
-            v = fmaxf(v, fmaxf(s[b][n][e], s[b][n][e + 2]));
+            const float v = fmaxf(s[b][n][e], s[b][n][e + 2]);
+            grew = grew || v > m[n][e] || v + lg[b] > (e ? r.y : r.x);
           }
+        }
+      }
+      if (__any_sync(0xffffffffu, grew)) {
+        auto over_lanes = [](float v) {
           v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
           v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-          top[n][e] = v;
-          grew = grew || v > m[n][e];
-        }
-      float sv_top = 0.f;
+          return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+        };
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-        if (live >> b & 1) sv_top = fmaxf(sv_top, sv[b]);
-      if (sv_top > ref || __any_sync(0xffffffffu, grew)) {
-        float r = 1.f;
-        if (sv_top > ref) {
-          // the power of two at or above, within 2^-110 .. 2^127 (its reciprocal times kWeight is finite)
-          const float up = fmaxf(__uint_as_float(min((__float_as_uint(sv_top) + 0x7fffffu) & 0x7f800000u,
-                                                     0x7f000000u)), 7.7037197775489434e-34f);
-          r = ref / up;
-          ref = up;
-          inv_ref = 1.f / up * kWeight;
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+          const float2 r2 = refs[4 * n];
+          float r[2] = {r2.x, r2.y};
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float mn = fmaxf(m[n][e], top[n][e]);
-            const float fac = m[n][e] == mn ? 1.f : pow2(m[n][e] - mn);
+            float v = -INFINITY, t = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) v = fmaxf(v, fmaxf(s[b][n][e], s[b][n][e + 2]));
+            const float mn = fmaxf(m[n][e], ceilf(over_lanes(v)));
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {  // (what is 0 as an fp32 weight has no say)
+              v = fmaxf(s[b][n][e], s[b][n][e + 2]);
+              if (v > mn - 126.f) t = fmaxf(t, v + lg[b]);
+            }
+            // (not below mn - 112: a weight's factor stays below 2^127)
+            const float rn = fmaxf(r[e], fmaxf(ceilf(over_lanes(t)), mn - 112.f));
+            const float fac = r[e] == rn ? 1.f : pow2(r[e] - rn);
+            if (m[n][e] != mn) l[n][e] *= pow2(m[n][e] - mn);
             m[n][e] = mn;
-            l[n][e] *= fac;
+            r[e] = rn;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
-              o[d][n][e] *= fac * r;
-              o[d][n][e + 2] *= fac * r;
+              o[d][n][e] *= fac;
+              o[d][n][e + 2] *= fac;
             }
           }
+          __syncwarp();  // every lane has read it
+          if (gid == 0) refs[4 * n] = make_float2(r[0], r[1]);
+        }
+        __syncwarp();
       }
       uint32_t pb[NB][2][NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const float m0 = m[n][0] == -INFINITY ? 0.f : m[n][0], m1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+        const float2 r = refs[4 * n];
+        const float g0 = pow2(m0 - r.x + kLogWeight), g1 = pow2(m1 - r.y + kLogWeight);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          const float wv = live >> b & 1 ? sv[b] * inv_ref : 0.f;
+          // (finite: the largest scale of all may be one that a column does not see)
+          const float w0 = live >> b & 1 ? fminf(sv[b] * g0, 0x1p126f) : 0.f, w1 = live >> b & 1 ? fminf(sv[b] * g1, 0x1p126f) : 0.f;
           float p0 = pow2(s[b][n][0] - m0), p1 = pow2(s[b][n][1] - m1);
           float p2 = pow2(s[b][n][2] - m0), p3 = pow2(s[b][n][3] - m1);
           l[n][0] += p0 + p2;
           l[n][1] += p1 + p3;
-          p0 *= wv; p1 *= wv; p2 *= wv; p3 *= wv;
+          p0 *= w0; p1 *= w1; p2 *= w0; p3 *= w1;
           const uint32_t h0 = half2_bits(p0, p1), h1 = half2_bits(p2, p3);
           pb[b][0][n][0] = transpose8(h0);
           pb[b][0][n][1] = transpose8(h1);
@@ -552,7 +572,6 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         if (gid == 0) {
           m_s[warp * COLS + col] = m[n][e];
           l_s[warp * COLS + col] = v;
-          r_s[warp * COLS + col] = ref;
         }
         float* row = o_s + col * D;
 #pragma unroll
@@ -573,9 +592,8 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
       float fac[kWarps];
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
-        const float x = pow2(m_s[i * COLS + col] - mm);
-        L += l_s[i * COLS + col] * x;
-        fac[i] = x * r_s[i * COLS + col] * (1.f / kWeight);
+        L += l_s[i * COLS + col] * pow2(m_s[i * COLS + col] - mm);
+        fac[i] = pow2(r_s[i * COLS + col] - mm - kLogWeight);
       }
       const int j = (col0 + col) / group, h = u.h * group + (col0 + col) % group;
       const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);

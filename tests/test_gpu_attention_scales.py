@@ -117,3 +117,66 @@ def test_chunks_with_a_scale_that_is_not_a_number(dtype):
     out = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, dtype)))
     P.crvq_sync()
     assert np.array_equal(out[:80], ref[:80]) and not np.isfinite(out[80:]).any()
+
+
+@pytest.mark.parametrize("wide", [None, 800])                        # clusters of CTAs, shares of a line
+@pytest.mark.parametrize("dtype,by", APART)
+@pytest.mark.parametrize("d,group,count", [(128, 2, 20), (64, 1, 30), (64, 1, 5), (128, 8, 1), (256, 1, 6), (256, 3, 20)])
+def test_few_queries_large_scales_that_other_queries_see(dtype, by, d, group, count, wide):
+    """Blocks that only some of a unit's queries see, by causality and by the window."""
+    for fmt, length in (("int8", 60), ("e4m3", 52)):
+        host, _ = U.make(78, [length], 16, 1, d, fmt, wide=wide)
+        _apart(host, 16, fmt, [0, 3], by)
+        gpu = U.on_gpu(host, fmt)
+        q = T._queries(79, count, group, d, dtype)
+        _check(host, gpu, q, [count], dtype)
+        _check(host, gpu, q, [count], dtype, window=34)
+
+
+@pytest.mark.parametrize("wide", [None, 800])
+@pytest.mark.parametrize("dtype,by", APART)
+@pytest.mark.parametrize("d,group", [(128, 8), (64, 1), (256, 4)])
+def test_few_queries_large_scales_that_weigh_nothing(dtype, by, d, group, wide):
+    """A block that every query sees and that none gives weight: first, between others, last."""
+    for fmt in ("int8", "e4m3"):
+        for at in (0, 1, 6, 20, 31):
+            host, _ = U.make(80, [500], 16, 1, d, fmt, wide=wide)
+            _apart(host, 16, fmt, [at], by)
+            _away(host, 16, [at])
+            _check(host, U.on_gpu(host, fmt), _ask(81, 1, group, d, dtype), [1], dtype, ragged=False)
+
+
+@pytest.mark.parametrize("wide", [None, 800])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_queries_and_values_with_scale_zero(dtype, wide):
+    """Blocks whose value scale is zero, alone and beside others: their tokens count in the sum alone."""
+    for lens, zero in (([300], (0, 1, 2, 11)), ([40], (0, 1, 2))):
+        host, _ = U.make(82, lens, 16, 1, 64, "int8", wide=wide)
+        for i in zero:
+            host["v_scale"][host["pages"][0][i]] = 0.0
+        gpu = U.on_gpu(host, "int8")
+        _check(host, gpu, T._queries(83, 1, 4, 64, dtype), [1], dtype)
+
+
+@pytest.mark.parametrize("wide", [None, 800])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_few_queries_and_the_smallest_and_largest_scales(d, wide):
+    """Scales from fp32's smallest normal number to near its largest, in sequences of their own and within one."""
+    for exps in ([-126] * 8, [118] * 8, [-126, 118, -60, 0, 60, -126, 100, -100]):
+        host, _ = U.make(84, [128], 16, 1, d, "int8", wide=wide)
+        for i, e in enumerate(exps):
+            host["v_scale"][host["pages"][0][i]] = np.ldexp(np.float32(1), e)
+        _check(host, U.on_gpu(host, "int8"), T._queries(85, 1, 3, d, "f32"), [1], "f32")
+
+
+@pytest.mark.parametrize("wide", [None, 800])
+def test_few_queries_with_a_scale_that_is_not_a_number(wide):
+    """Rows that see the block are not finite, the others are as without it."""
+    import paper_2412_09282_gb300 as P
+    host, gpu = U.make(86, [60], 16, 1, 64, "int8", wide=wide)
+    q = T._queries(87, 30, 1, 64, "f32")
+    ref = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f32")))
+    gpu.v_scale[int(host["pages"][0][3])] = float("nan")             # tokens 48 .. 59
+    out = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f32")))
+    P.crvq_sync()
+    assert np.array_equal(out[:18], ref[:18]) and not np.isfinite(out[18:]).any()
