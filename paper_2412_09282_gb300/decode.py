@@ -139,7 +139,7 @@ def crvq_cache_append(cache, k, v, new_off=None, cos=None, sin=None, positions=N
                 raise ValueError("positions must be contiguous with one entry per token")
         n_pos, half = cos.shape
         rot = _lib.crvq_rotary(cos.data_ptr(), sin.data_ptr(), None if positions is None else positions.data_ptr(),
-                               n_pos, max(cos.stride(0), half), half, 1 if interleaved else 0)
+                               n_pos, cos.stride(0) if n_pos > 1 else half, half, 1 if interleaved else 0)
     qc = oc = None
     if q is not None:
         if q.shape[0] != n_tok:
