@@ -128,6 +128,10 @@ def crvq_cache_append(cache, k, v, new_off=None, cos=None, sin=None, positions=N
     if v.shape[0] != n_tok:
         raise ValueError("k and v differ in tokens")
     rot = None
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin: give both or neither")
+    if positions is not None and cos is None:
+        raise ValueError("positions are rows of cos and sin, which are missing")
     if cos is not None:
         _device(cos, torch.float32, "cos")
         _device(sin, torch.float32, "sin")

@@ -31,3 +31,10 @@ def test_a_table_of_one_row_may_have_any_stride():
     zero = torch.zeros(2, dtype=torch.int32, device="cuda")
     _call(cos=tab, sin=tab, positions=zero)
     P.crvq_sync()
+
+
+def test_half_of_the_tables_and_positions_without_them_are_refused():
+    tab = torch.ones((9, 32), device="cuda")
+    for kw in (dict(cos=tab), dict(sin=tab), dict(positions=torch.zeros(2, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            _call(**kw)
