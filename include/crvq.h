@@ -585,7 +585,8 @@ typedef struct crvq_q4_matrix {
  * W (M x N of `type`, row stride ldw) to 4 bits, by rounding to the nearest level. Without zeros the
  * scale of a group is bf16(max|w| * (1/7)), the code round(w / scale) + 8; with zeros, for lo = min(w, 0)
  * and hi = max(w, 0), scale = bf16((hi - lo) * (1/15)), zero = round(-lo / scale), code = round(w /
- * scale) + zero; ties to even, clamped to 0..15. A group of zeros gets scale 0.
+ * scale) + zero; ties to even, clamped to 0..15. A group of zeros gets scale 0. Where hi - lo is above fp32's largest
+ * number, scale = bf16(hi * (1/15) - lo * (1/15)), and a code whose value would be above it is the next one towards zero.
  *   W_hat [M x N] fp32 (contiguous) or NULL: the values that the codes stand for.
  * Values that are not finite count as 0 and are reported as CRVQ_ERR_NUMERIC by crvq_sync.
  */

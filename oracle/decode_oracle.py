@@ -135,12 +135,20 @@ def q4_quantize(W, group, symmetric):
     for g in range(G):
         w = W[:, g * group:(g + 1) * group]
         lo, hi = np.minimum(w.min(1), F(0)), np.maximum(w.max(1), F(0))
-        s = bf16((hi - lo) * F(1.0 / 15.0)) if not symmetric else bf16(np.maximum(hi, -lo) * F(1.0 / 7.0))
+        if symmetric:
+            s = np.maximum(hi, -lo) * F(1.0 / 7.0)
+        else:
+            with np.errstate(over="ignore"):
+                s = (hi - lo) * F(1.0 / 15.0)
+            s = np.where(np.isinf(s), hi * F(1.0 / 15.0) - lo * F(1.0 / 15.0), s)
+        s = bf16(s)
         safe = np.where(s > 0, s, F(1))
         if not symmetric:
             zeros[:, g] = np.where(s > 0, np.clip(np.rint(-lo / safe), 0, 15), 0)
-        q = np.where(s[:, None] > 0, np.rint(w / safe[:, None]), 0) + zeros[:, g:g + 1]
-        codes[:, g * group:(g + 1) * group] = np.clip(q, 0, 15).astype(np.int64)
+        q = np.clip(np.where(s[:, None] > 0, np.rint(w / safe[:, None]), 0) + zeros[:, g:g + 1], 0, 15)
+        level = q - zeros[:, g:g + 1]
+        above = np.abs(level.astype(np.float64) * s[:, None]) >= 2.0 ** 128 - 2.0 ** 103   # (rounds to infinity)
+        codes[:, g * group:(g + 1) * group] = (q - np.where(above, np.sign(level), 0)).astype(np.int64)
         scales[:, g] = s
     return codes, scales, zeros
 

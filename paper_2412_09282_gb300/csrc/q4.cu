@@ -622,8 +622,9 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const __grid_constant_
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
   }
   constexpr float k7 = (float)(1.0 / 7.0), k15 = (float)(1.0 / 15.0);
-  const __nv_bfloat16 s16 = __float2bfloat16_rn(a.m.zeros ? __fmul_rn(__fsub_rn(hi, lo), k15)
-                                                          : __fmul_rn(fmaxf(hi, -lo), k7));
+  float range = __fmul_rn(__fsub_rn(hi, lo), k15);
+  if (range == INFINITY) range = __fsub_rn(__fmul_rn(hi, k15), __fmul_rn(lo, k15));  // (hi - lo is above fp32's numbers)
+  const __nv_bfloat16 s16 = __float2bfloat16_rn(a.m.zeros ? range : __fmul_rn(fmaxf(hi, -lo), k7));
   const float s = __bfloat162float(s16);
   float z = 8.f;
   if (a.m.zeros) z = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 0.f;
@@ -644,6 +645,14 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const __grid_constant_
     const float q = fminf(fmaxf(__fsub_rn(__fadd_rn(w[e], kRound), kRound) + z, 0.f), 15.f);
     v[e] = (q - z) * s;
     codes |= (__float_as_uint(__fadd_rn(q, kRound)) & 15u) << (4 * e);
+  }
+  if (s > 0x1p120f) {  // a nearest level may be above fp32's numbers: then the one before it (rare: apart from the loop)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (fabsf(v[e]) == INFINITY) {
+        codes = v[e] > 0.f ? codes - (1u << 4 * e) : codes + (1u << 4 * e);
+        v[e] = ((float)(codes >> 4 * e & 15u) - z) * s;
+      }
   }
   if (n == 0) return;
   if (n < 8) codes &= (1u << (4 * n)) - 1u;
