@@ -548,6 +548,7 @@ crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, co
  * query at place t sees the key at place j when 0 <= j < lens[b], when j <= t (causal), and when
  * j > t - window (window > 0). A query that sees nothing gets 0.
  *   q_off   [n_seq + 1] int32, or NULL: n_tok / n_seq queries each.
+ *   scale   within -2^127 .. 2^127.
  *   out     [n_tok x q->heads x head_dim], the type of q.
  *   lse     [n_tok x q->heads] fp32 or NULL: log sum_j exp(scale * q . K_j), -inf where nothing is seen.
  * Scores, maxima and sums are fp32, products run on the tensor cores with fp32 accumulation. q is

@@ -71,7 +71,8 @@ crvq_status attention(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n
   CRVQ_CHECK_ARG(a.q.heads == a.o.heads && a.q.type == a.o.type, "q and out differ in heads or type");
   CRVQ_CHECK_ARG(a.q.heads % a.c.n_kv == 0, "q->heads (%d) must be a multiple of n_kv (%d)", a.q.heads, a.c.n_kv);
   CRVQ_CHECK_ARG(window >= 0, "window must be >= 0");
-  CRVQ_CHECK_ARG(scale == scale && fabsf(scale) <= 3.402823466e38f, "scale must be finite");
+  // (above, scale log2(e) is not finite, and a key of zeros would score 0 * infinity)
+  CRVQ_CHECK_ARG(fabsf(scale) <= 0x1p127f, "scale must be within -2^127 .. 2^127");
   CRVQ_CHECK_ARG(((uintptr_t)lse & 3u) == 0, "lse is not aligned");
   CRVQ_TRY(check_dev({{lse, "lse"}}));
   a.group = a.q.heads / a.c.n_kv;

@@ -180,3 +180,17 @@ def test_few_queries_with_a_scale_that_is_not_a_number(wide):
     out = U.exactly(P.crvq_cache_attention(gpu, U.heads(q, "f32")))
     P.crvq_sync()
     assert np.array_equal(out[:18], ref[:18]) and not np.isfinite(out[18:]).any()
+
+
+@pytest.mark.parametrize("count", [1, 40])                           # few queries, tiles of 128 rows
+def test_scores_of_the_largest_scale(count):
+    """Queries of zeros score 0 at any scale that is taken; a scale whose product with log2(e) is not finite is refused."""
+    import paper_2412_09282_gb300 as P
+    host, gpu = U.make(88, [60], 16, 1, 64, "int8")
+    q = torch.zeros((count, 2, 64), device="cuda", dtype=torch.bfloat16)
+    ref = P.crvq_cache_attention(gpu, q, scale=1.0)
+    assert torch.equal(P.crvq_cache_attention(gpu, q, scale=2.0 ** 127), ref) and bool(ref.isfinite().all())
+    for scale in (3e38, -3e38):
+        with pytest.raises(P.CrvqError) as e:
+            P.crvq_cache_attention(gpu, q, scale=scale)
+        assert e.value.status == -1
