@@ -48,6 +48,8 @@ def _values(m, r0, r1):
     (512, 28672, 128, False, 2, "bf16"),      # few tiles, many steps
     (238412, 1042, 128, True, 17, "f32"),     # tiles in several groups, several chunks in each
     (238412, 1042, 32, False, 3, "bf16"),
+    (60000, 4096, 64, False, 17, "bf16"),     # groups and clusters
+    (120000, 4090, 128, True, 8, "f32"),
 ])
 def test_long_ways(M, N, group, zeros, b, dtype):
     import paper_2412_09282_gb300 as P
