@@ -21,9 +21,10 @@ _addressof, _empty = C.addressof, torch.empty
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _foreign(stream, *outputs):
-    """The handle of a stream given by the caller, on which the outputs are then in use."""
-    for t in outputs:
+def _foreign(stream, *tensors):
+    """The handle of a stream given by the caller, on which the call's tensors are then in use: memory that a tensor gives
+    up meanwhile waits for it. (The caller's to order: that stream after the work that makes the inputs.)"""
+    for t in tensors:
         if t is not None:
             t.record_stream(stream)
     return stream.cuda_stream
@@ -108,6 +109,9 @@ class KVCache:
                                      pages.shape[1], page, n_kv, d, _FORMATS[K.dtype])
         self._addr = _addressof(self._c)
 
+    def tensors(self):
+        return self.K, self.V, self.k_scale, self.v_scale, self.pages, self.lens
+
     @staticmethod
     def empty(n_pages, n_kv, page, head_dim, pages, lens, dtype=torch.int8):
         """A cache over a new pool of pages (its codes are whatever the memory holds)."""
@@ -157,7 +161,8 @@ def crvq_cache_append(cache, k, v, new_off=None, cos=None, sin=None, positions=N
                                 _offsets(new_off, cache.n_seq, "new_off"),
                                 None if rot is None else _addressof(rot), None if qc is None else _addressof(qc),
                                 None if oc is None else _addressof(oc),
-                                _raw_stream(cache.index) if stream is None else _foreign(stream, q_out))
+                                _raw_stream(cache.index) if stream is None else
+                                _foreign(stream, k, v, q, q_out, new_off, cos, sin, positions, *cache.tensors()))
     if st:
         _check(st)
     return q_out
@@ -180,7 +185,8 @@ def crvq_cache_read(cache, start, off, n_tok, dtype=torch.float32, K_out=None, V
         raise ValueError(f"V_out must be contiguous n_tok x n_kv x head_dim of {dtype}")
     st = _L().crvq_cache_read(cache._addr, start.data_ptr(), _offsets(off, cache.n_seq, "off"), n_tok,
                               _type(K_out, "K_out"), K_out.data_ptr(), V_out.data_ptr(),
-                              _raw_stream(cache.index) if stream is None else _foreign(stream, K_out, V_out))
+                              _raw_stream(cache.index) if stream is None else
+                              _foreign(stream, K_out, V_out, start, off, *cache.tensors()))
     if st:
         _check(st)
     return K_out, V_out
@@ -201,7 +207,8 @@ def crvq_cache_attention(cache, q, q_off=None, scale=None, causal=True, window=0
     st = _L().crvq_cache_attention(cache._addr, _addressof(qc), q.shape[0], _offsets(q_off, cache.n_seq, "q_off"),
                                    1.0 / math.sqrt(d) if scale is None else scale, causal, window,
                                    _addressof(oc), None if lse is None else lse.data_ptr(),
-                                   _raw_stream(cache.index) if stream is None else _foreign(stream, out, lse))
+                                   _raw_stream(cache.index) if stream is None else
+                                   _foreign(stream, q, out, lse, q_off, *cache.tensors()))
     if st:
         _check(st)
     return (out, lse) if want_lse else out
@@ -264,8 +271,8 @@ def crvq_q4_quantize(W, group=128, symmetric=True, want_W_hat=False, out=None, s
     W_hat = _empty((M, N), device=W.device, dtype=torch.float32) if want_W_hat else None
     st = _L().crvq_q4_quantize(W.data_ptr(), stride[0] if M > 1 else N, t, out._addr,
                                None if W_hat is None else W_hat.data_ptr(),
-                               _raw_stream(out.index) if stream is None else _foreign(stream, W_hat, out.codes,
-                                                                                      out.scales, out.zeros))
+                               _raw_stream(out.index) if stream is None else
+                               _foreign(stream, W, W_hat, out.codes, out.scales, out.zeros))
     if st:
         _check(st)
     return out, W_hat
@@ -287,7 +294,8 @@ def crvq_q4_matvec(X, matrix, Y=None, stream=None):
             raise ValueError("Y must be b x M of X's type with unit column stride")
         ldy = Y.stride(0) if b > 1 else M
     st = _L().crvq_q4_matvec(matrix._addr, X.data_ptr(), stride[0] if b > 1 else shape[1], b, t, Y.data_ptr(), ldy,
-                             _raw_stream(matrix.index) if stream is None else _foreign(stream, Y))
+                             _raw_stream(matrix.index) if stream is None else
+                             _foreign(stream, X, Y, matrix.codes, matrix.scales, matrix.zeros))
     if st:
         _check(st)
     return Y
