@@ -519,7 +519,8 @@ typedef struct crvq_rotary {
  * lens[b] - (new_off[b + 1] - new_off[b]) .. lens[b].
  *   new_off  [n_seq + 1] int32, or NULL: n_tok / n_seq tokens each.
  *   rot      NULL: no rotation.
- *   q, q_out NULL, or the step's queries and where their rotated values go (may be the same memory).
+ *   q, q_out NULL, or the step's queries and where their rotated values go (may be the same memory; rows that are no
+ *            sequence's stay as they are where they turn by their place in the cache).
  * A block's scale is the largest of its new values' magnitudes times 1/127 (1/448 for e4m3), or the
  * present scale where that is larger and the block holds earlier tokens; their codes c then become
  * round(c * (old scale / new scale)), the new ones round(x / scale), ties to even, all in fp32. The
@@ -551,6 +552,7 @@ crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, co
  *   scale   within -2^127 .. 2^127.
  *   out     [n_tok x q->heads x head_dim], the type of q.
  *   lse     [n_tok x q->heads] fp32 or NULL: log sum_j exp(scale * q . K_j), -inf where nothing is seen.
+ * Rows of out and lse that are no sequence's stay as they are.
  * Scores, maxima and sums are fp32, products run on the tensor cores with fp32 accumulation. q is
  * taken relative to a power of two per row in one fp16 operand (exact for 16-bit types but for
  * elements below 2^-14 of the row's largest) or, from fp32, in two. The weights p_j are held to 22 bits
@@ -558,7 +560,8 @@ crvq_status crvq_cache_read(const crvq_kv_cache* cache, const int32_t* start, co
  * kv head and sequence on average, which take tiles of 128 rows, to fp16's 11. They are held relative to the largest
  * p_j * (value scale) of the keys that the query sees; from 2^-24 of it on (2^-16 for those tiles) smaller ones lose
  * bits, and those below 2^-38 (2^-30) count as 0. Work is split over the
- * cached tokens by the lengths on the device and joined in a fixed order: results are identical run to run.
+ * cached tokens by the lengths on the device and joined in a fixed order: results are identical run to run. (Which
+ * form a call takes depends on all of it: a sequence's last bits may differ beside other sequences.)
  * Requires q->heads to be a multiple of n_kv.
  */
 crvq_status crvq_cache_attention(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok,

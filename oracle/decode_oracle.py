@@ -86,7 +86,7 @@ def values(cache, name, b, first, last):
     return out
 
 
-def attention(cache, q, counts, scale, causal=True, window=0, q_bits=24):
+def attention(cache, q, counts, scale, causal=True, window=0):
     """(out, lse, bound pieces): out [tokens, heads, d] fp64; mass = sum_j p_j |V_j| and shake = the largest
     error of a score per unit roundoff, (d + 16) scale sum |q||k|, for tolerances."""
     n_kv = cache["K"].shape[1]

@@ -6,10 +6,10 @@ namespace crvq {
 
 namespace {
 
-// Clusters where a CTA then has no more than this many tiles, whatever the lengths are. Line against clusters, us,
-// for (units, tiles per CTA): (8, 1) 12.1, 8.1; (8, 4) 16.1, 11.4; (32, 2) 17.3, 11.0; (96, 1) 15.0, 9.6;
-// (96, 5) 20.5, 19.6; (130, 8, of 64 channels) 24.7, 20.2; (32, 8) 23.1, 22.7; (8, 16) 24.4, 23.2; (96, 12) 32.6, 38.8;
-// (8, 32) 28.2, 38.8.
+// Clusters where a CTA then has no more than this many tiles, whatever the lengths are: by the page table's width, so a
+// table for long contexts takes the line for short sequences, too. Line against clusters, us, for (units, tiles per
+// CTA): (8, 1) 12.3, 8.4; (8, 4) 16.4, 11.6; (32, 2) 14.2, 9.2; (96, 1) 15.5, 8.3; (96, 5) 18.6, 14.0; (130, 8, of 64
+// channels) 25.3, 21.4; (32, 8) 20.2, 15.5; (8, 16) 24.2, 24.0; (96, 12) 24.9, 25.5; (8, 32) 28.5, 39.6.
 constexpr int kClusterTiles = 8;
 
 template <int D, int NT, int FMT, bool SPLIT>
@@ -37,8 +37,8 @@ crvq_status launch_attend(AttendArgs& a, cudaStream_t stream) {
 }
 
 // Columns per sequence, on average, from which tiles of 128 rows (attend_tc.cu) are taken. This form against that, us,
-// for (sequences of up to 4096 tokens x kv heads, columns): (64 x 32, 32) 604, 774; (16 x 8, 32) 51, 61; (16 x 8, 48)
-// 68, 63; (8 x 8, 64) 51, 41; (1 x 8, 64) 22, 27; (64 x 32, 64) 1188, 781; (1 x 8, 128) 30, 31; (1 x 8, 256) 50, 41.
+// for (sequences of up to 4096 tokens x kv heads, columns): (64 x 32, 32) 691, 853; (16 x 8, 32) 61, 68; (16 x 8, 48)
+// 83, 69; (8 x 8, 64) 62, 44; (1 x 8, 64) 19, 28; (64 x 32, 64) 1359, 855; (1 x 8, 128) 27, 32; (1 x 8, 256) 52, 41.
 constexpr int64_t kManyColumns = 64;
 
 template <int D, int FMT, bool SPLIT>

@@ -26,9 +26,9 @@
 // each other's shared memory: no second launch, no scratch.
 //
 // What bounds it: the bytes of the cache. 64 sequences of up to 4096 tokens, 32 kv heads: 183 us, 6.2 TB/s; 4
-// of up to 131072 tokens, 8 kv heads: 163 us, 6.0 TB/s (91 and 89 % of a copy's rate). Short calls: the chain of
-// lookups, copies, products and joins of a few tiles. One sequence of 1001 tokens: 8.1 us (12.1 by the line); 16 of up to
-// 3001 with up to 5 drafted tokens, fp32: 21 us (26 by the line).
+// of up to 131072 tokens, 8 kv heads: 162 us, 6.1 TB/s (91 and 89 % of a copy's rate). Short calls: the chain of
+// lookups, copies, products and joins of a few tiles. One sequence of 1001 tokens: 8.3 us (12.1 by the line); 16 of up to
+// 3001 with up to 5 drafted tokens, fp32: 21 us (25 by the line).
 #pragma once
 
 #include "attend.cuh"

@@ -21,9 +21,9 @@
 // What bounds it: a chain of about 5000 cycles per tile and group (waits, row maxima, weights, products), which two
 // groups do not hide: the tensor pipe is active 35 % of the time, 0.44 instructions issue per cycle and scheduler, and
 // no one of maxima, exponentials, operand stores and products takes more than a sixth of the time when left out.
-// Two prompts of up to 1024 tokens over 8192, 64 heads on 8: 410 us, 760 TFLOP/s (39 % of the measured bf16 rate).
-// Steps of 64 keys with scores two steps ahead were slower (520), as were an issuing warp per group (413) and 16
-// softmax warps (spills).
+// Two prompts of up to 1024 tokens over 8192, 64 heads on 8: 414 us, 751 TFLOP/s (39 % of the measured bf16 rate).
+// Steps of 64 keys with scores two steps ahead were slower (520 when this form took 410), as were an issuing warp per
+// group (413) and 16 softmax warps (spills).
 #include "attend.cuh"
 #include "tc_ops.cuh"
 
@@ -708,7 +708,7 @@ crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
 }
 
 // (bf16 outputs' own rounding is 8 times a single piece's error. fp16 outputs with a single piece were 1.4 to 1.5 times as
-// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 410 to 493 us.)
+// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 414 to 487 us.)
 template <int D>
 crvq_status pick_tc(AttendArgs& a, int format, cudaStream_t stream) {
   const bool two = a.q.type == CRVQ_F16;

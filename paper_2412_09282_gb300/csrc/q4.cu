@@ -21,8 +21,8 @@
 //
 // What bounds it: instructions. A step of 16 rows takes about 390 (9 per word of 8 codes into operands; the rest
 // products, input reads, scales and places), 0.6 per cycle and scheduler, and a call starts and ends with some 6000 cycles of code
-// that runs once (places, layout, joins). One input: 28672 x 8192 27.5 us, 4.4 TB/s; 11008 x 4096 9.0 us; 512 x 512 3.5 us.
-// 16 inputs, 28672 x 8192: 45.8 us.
+// that runs once (places, layout, joins). One input, matrices that are not in L2: 28672 x 8192 28.0 us,
+// 4.3 TB/s; 11008 x 4096 9.9 us (9.0 from L2). From L2: 512 x 512 3.6 us. 16 inputs, 28672 x 8192: 45.8 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -571,7 +571,7 @@ q4_matvec_kernel(const __grid_constant__ MatvecQ4 a) {
 }
 
 // A thread takes eight consecutive weights; the GROUP / 8 threads of a group find its range by shuffles. 16.8 M fp32
-// weights with their values: 26.2 us, 5.5 TB/s; 40 instructions per weight issue 0.72 of the time (with CUDA's division
+// weights with their values: 26.5 us, 5.4 TB/s; 40 instructions per weight issue 0.72 of the time (with CUDA's division
 // and 64-bit places 54, 30.3 us).
 struct QuantizeArgs {
   Q4View m;
@@ -705,7 +705,10 @@ crvq_status launch_matvec(MatvecQ4& a, cudaStream_t stream) {
   // Slices, and the tiles whose sums are held at a time: the choice with the least (tile, step) pairs of one row
   // tile on the busiest SM, with what else costs time in such pairs (about 50 ns): laying out inputs a
   // third per step and column, ten per chunk and group, 20 per group of a cluster. Clusters that are resident
-  // at one CTA per SM: 152, 76, 36 and 15 (of 1, 2, 4 and 8).
+  // at one CTA per SM: 152, 76, 36 and 15 (of 1, 2, 4 and 8). Us with 1, 2, 4 and 8 slices, the choice in brackets: one
+  // bf16 input, 4096 x 4096 [5.5], 5.9, 6.0, 7.3; 11008 x 4096 [9.0], 8.9, 9.2, 10.8; 4096 x 11008 [9.6], 9.9, 9.2, 11.5;
+  // 28672 x 8192 [27.6], 27.8, 29.0, 36.0; 8192 x 28672 34.5, 32.1, [30.9], 34.1; 16 inputs, 4096 x 4096 16.6, 11.9, 9.9,
+  // [9.5]; 28672 x 8192 59.8, 49.1, [44.5], 53.1; 32 fp32 inputs of it 161, 131, [124], 151.
   int slices = 1;
   int64_t clusters = 0;
   double best = 0;
