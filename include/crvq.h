@@ -569,6 +569,39 @@ crvq_status crvq_cache_attention(const crvq_kv_cache* cache, const crvq_heads* q
                                  const crvq_heads* out, float* lse, crvq_stream_t stream);
 
 /*
+ * Which drafted tokens see which, from every tree's parents. The drafted tokens of sequence b are rows off[b] ..
+ * off[b + 1); parents[row] is the number, in its sequence's tree, of a token's parent, or -1 for a child of the last token
+ * before the tree. Parents come before their children (trees in the order in which their tokens were drafted).
+ *   off        [n_seq + 1] int32, or NULL: n_tok / n_seq tokens each.
+ *   mask       [n_tok x words]: bit j % 32 of word j / 32 of a token's row is 1 when j is the token itself or an ancestor
+ *              of it, less than `window` generations before it where window > 0.
+ *   words      32 * words >= the largest tree's tokens.
+ *   positions  [n_tok] int32 or NULL: the place that a token has on its path, lens[b] - n + depth in a tree of n
+ *              tokens (depth where lens is NULL; lens counts the tree): rows of rotation tables, and what a window
+ *              goes by.
+ * A parent that does not come before its child, and tokens that the words have no bits for, are reported as
+ * CRVQ_ERR_DEVICE by crvq_sync; the former count as roots, the latter are seen by none. Rows that are no sequence's stay
+ * as they are.
+ */
+crvq_status crvq_tree_mask(const int32_t* parents, int64_t n_tok, const int32_t* off, int32_t n_seq,
+                           const int32_t* lens, int32_t window, uint32_t* mask, int32_t words,
+                           int32_t* positions, crvq_stream_t stream);
+
+/*
+ * crvq_cache_attention for trees of drafted tokens: the queries of sequence b are its last n = q_off[b + 1] - q_off[b]
+ * tokens, in the order of its tree and of their places in the cache. Each sees the tokens before the tree (from place
+ * position - window + 1 on where window > 0) and the drafted ones whose bits are set in its row of mask; bits past
+ * the sequence's tokens have no meaning. A query that sees nothing gets 0, and -inf in lse.
+ *   mask       [n_tok x words], as crvq_tree_mask makes it or of the caller's own (any tokens, ancestors or not).
+ *   positions  [n_tok] int32, places lens[b] - n .. lens[b] - 1 (others count as the nearest); NULL without a window.
+ * The rest is as there: scales, precision, order of the sums, and what q and out may be.
+ */
+crvq_status crvq_cache_tree_attention(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok,
+                                      const int32_t* q_off, const uint32_t* mask, int32_t words,
+                                      const int32_t* positions, float scale, int32_t window,
+                                      const crvq_heads* out, float* lse, crvq_stream_t stream);
+
+/*
  * A matrix in 4 bits with a scale per group of inputs: W[i][j] = (code - zero) * scale, code of (i, j)
  * the low (j even) or high (j odd) four bits of codes[i * ld_codes + j / 2], scale and zero those of
  * group j / group of row i.

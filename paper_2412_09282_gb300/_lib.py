@@ -123,6 +123,10 @@ SIGNATURES = {
     "crvq_cache_read": (C.c_int32, [c_vp, c_vp, c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_cache_attention": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, C.c_float, C.c_int32,
                                          C.c_int32, c_vp, c_vp, c_vp]),
+    "crvq_tree_mask": (C.c_int32, [c_vp, C.c_int64, c_vp, C.c_int32, c_vp, C.c_int32, c_vp, C.c_int32,
+                                   c_vp, c_vp]),
+    "crvq_cache_tree_attention": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, c_vp, C.c_int32, c_vp,
+                                              C.c_float, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_q4_quantize": (C.c_int32, [c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_q4_matvec": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int32, c_vp, C.c_int64,
                                    c_vp]),

@@ -24,6 +24,9 @@ struct AttendArgs {
   int cluster;      // CTAs of a unit that join it among themselves, a power of two (0: shares of the line)
   int log_cluster;
   unsigned* err;
+  const uint32_t* tree;      // which drafted tokens a query sees: `words` words of bits a row
+  const int32_t* positions;  // of the queries (a window's; null without one)
+  int words;
 };
 
 // Few queries, short sequences (attend_cluster.cu): `size` CTAs (2, 4 or 8) per unit of 8 NT columns.
@@ -31,6 +34,13 @@ crvq_status launch_attend_clusters(AttendArgs& a, int D, int NT, int format, int
                                    cudaStream_t stream);
 // Many queries per sequence (attend_tc.cu): 16-bit queries, 64 or 128 channels.
 crvq_status launch_attend_many(AttendArgs& a, int D, int format, cudaStream_t stream);
+// The same two for trees of drafted tokens (attend_tree_cluster.cu, attend_tree_tc.cu).
+crvq_status launch_tree_clusters(AttendArgs& a, int D, int NT, int format, int64_t units, int size,
+                                 cudaStream_t stream);
+crvq_status launch_tree_many(AttendArgs& a, int D, int format, cudaStream_t stream);
+// Checks and the arguments of both calls (attend.cu).
+crvq_status attend_args(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok, const int32_t* q_off,
+                        float scale, int32_t window, const crvq_heads* out, float* lse, AttendArgs* args);
 
 namespace {
 
@@ -208,6 +218,30 @@ struct Line {
     return u;
   }
 };
+
+// Tokens t0 + i, 0 <= i < 32, with kb <= t0 + i < ke, as bits.
+__device__ __forceinline__ uint32_t range32(int t0, int kb, int ke) {
+  const int lo = min(max(kb - t0, 0), 32), hi = min(max(ke - t0, 0), 32);
+  const uint32_t below = hi == 32 ? 0xffffffffu : (1u << hi) - 1u, from = lo == 32 ? 0u : 0xffffffffu << lo;
+  return below & from;
+}
+
+// Trees of drafted tokens. The last n tokens of a sequence are the drafted ones, token `held` the first of them. A query
+// sees the cached tokens from kb on and those drafted ones that its row of bits names: tokens t0 + i as bits.
+__device__ __forceinline__ uint32_t tree32(const AttendArgs& a, int64_t row, int t0, int kb, int held, int len) {
+  uint32_t seen = range32(t0, kb, min(held, len));
+  if (t0 + 32 <= held || t0 >= len) return seen;
+  const int first = t0 - held, w = first >> 5;  // (before the first drafted token: words of zeros)
+  const uint32_t* bits = a.tree + row * a.words;
+  const uint32_t lo = w >= 0 && w < a.words ? __ldg(bits + w) : 0u, hi = w + 1 >= 0 && w + 1 < a.words ? __ldg(bits + w + 1) : 0u;
+  return seen | (__funnelshift_r(lo, hi, first & 31) & range32(t0, held, len));
+}
+
+// The first cached token that a drafted token sees (its position among the sequence's last n places).
+__device__ __forceinline__ int tree_begin(const AttendArgs& a, int64_t row, int held, int len) {
+  if (a.window <= 0) return 0;
+  return max(0, min(max(__ldg(a.positions + row), held), len - 1) - a.window + 1);
+}
 
 // Codes 0, 1 (half 0) or 2, 3 (half 1) of a word as fp16.
 template <int FMT, int HALF>

@@ -163,7 +163,8 @@ struct Shape {
   static constexpr int kSlot = kCols * (D + 2);  // floats of a part
 };
 
-template <int D, int NT, int FMT, bool SPLIT, bool CLUSTER>
+// TREE: the queries are trees of drafted tokens, each of which sees its ancestors among them (AttendArgs::tree).
+template <int D, int NT, int FMT, bool SPLIT, bool CLUSTER, bool TREE = false>
 __global__ void __launch_bounds__(kThreads, Shape<D, NT, FMT, SPLIT>::kPerSm)
 attend_kernel(const __grid_constant__ AttendArgs a) {
   using S = Shape<D, NT, FMT, SPLIT>;
@@ -218,8 +219,8 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
     // blocks NB i .. of the part; while it works on its values and on the next step's keys, the copies of
     // the next values and of the keys after those are on their way.
     const int reach = u.s.len - u.s.n + (col0 + n_cols - 1) / group + 1;  // past the last column's place
-    const int some_e = a.causal ? min(len, reach) : len;
-    const int some_b = a.window > 0 ? max(0, len - u.s.n + col0 / group - a.window + 1) : 0;
+    const int some_e = a.causal && !TREE ? min(len, reach) : len;
+    const int some_b = a.window > 0 ? max(0, len - u.s.n + (TREE ? 0 : col0 / group) - a.window + 1) : 0;
     constexpr int NB = kBlocks<D>;
     constexpr uint32_t kAll = (1u << NB) - 1;
     const int n_tiles = t_end - u.tile;
@@ -316,8 +317,13 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
       if (lane == 0) {
         f_s[col] = back * a.scale;
         const int pos = len - u.s.n + j;
-        beg_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-        end_s[col] = a.causal ? min(len, pos + 1) : len;
+        if constexpr (TREE) {
+          beg_s[col] = tree_begin(a, u.s.first + min(j, u.s.n - 1), len - u.s.n, len);
+          end_s[col] = min(len, len - u.s.n);
+        } else {
+          beg_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+          end_s[col] = a.causal ? min(len, pos + 1) : len;
+        }
       }
     }
     __syncthreads();
@@ -332,7 +338,11 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
         ke[t][e] = end_s[8 * t + 2 * tig + e];
       }
     // keys that every column sees (positions do not fall from column to column)
-    const int every_b = beg_s[n_cols - 1], every_e = end_s[0];
+    int every_b = beg_s[n_cols - 1];
+    const int every_e = end_s[0];
+    if constexpr (TREE)  // (positions in any order)
+      if (a.window > 0)
+        for (int col = 0; col < n_cols; ++col) every_b = max(every_b, beg_s[col]);
 
     float o[D / 16][NT][4];
     // in log2, whole numbers: m at the largest score or above, and in shared memory (two reads a step, and registers are
@@ -424,6 +434,17 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) lg[b] = __log2f(sv[b]);
       bool grew = false;  // in this lane's tokens (the lanes' maxima are joined only when one has)
+      uint32_t seen[NT][2];
+      if constexpr (TREE) {
+        if (!whole) {
+          static_assert(NB <= 2, "a warp's tokens are a word's bits");
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              seen[n][e] = tree32(a, u.s.first + (col0 + min(8 * n + 2 * tig + e, n_cols - 1)) / group, tok, kb[n][e], len - u.s.n, len) >> gid;
+        }
+      }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const float2 r = refs[4 * n];
@@ -437,8 +458,13 @@ attend_kernel(const __grid_constant__ AttendArgs a) {
             if (!whole) {
               const int t0 = tok + b * kCacheBlock + gid;
               const bool in = live >> b & 1;
-              if (!in || t0 < kb[n][e] || t0 >= ke[n][e]) s[b][n][e] = -INFINITY;
-              if (!in || t0 + 8 < kb[n][e] || t0 + 8 >= ke[n][e]) s[b][n][e + 2] = -INFINITY;
+              if constexpr (TREE) {
+                if (!in || !(seen[n][e] >> (b * kCacheBlock) & 1)) s[b][n][e] = -INFINITY;
+                if (!in || !(seen[n][e] >> (b * kCacheBlock + 8) & 1)) s[b][n][e + 2] = -INFINITY;
+              } else {
+                if (!in || t0 < kb[n][e] || t0 >= ke[n][e]) s[b][n][e] = -INFINITY;
+                if (!in || t0 + 8 < kb[n][e] || t0 + 8 >= ke[n][e]) s[b][n][e + 2] = -INFINITY;
+              }
             }
             const float v = fmaxf(s[b][n][e], s[b][n][e + 2]);
             grew = grew || v > m[n][e] || v + lg[b] > (e ? r.y : r.x);

@@ -176,39 +176,6 @@ __device__ __forceinline__ int64_t rot_row(const AppendArgs& a, int64_t t, int p
   return pos;
 }
 
-// Codes of four values (SMALL: magnitudes below Q + 1/2). int8: adding 1.5 * 2^23 rounds to an integer, which
-// the sum's low byte is in two's complement.
-template <int FMT, bool SMALL>
-__device__ __forceinline__ uint32_t encode4(const float v[4]) {
-  if constexpr (FMT == CRVQ_KV_INT8) {
-    uint32_t b[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      b[j] = __float_as_uint(__fadd_rn(SMALL ? v[j] : fminf(fmaxf(v[j], -127.f), 127.f), 12582912.f));
-    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-  } else {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
-    return lo | hi << 16;
-  }
-}
-
-template <int FMT>
-__device__ __forceinline__ void decode4(uint32_t w, float v[4]) {
-  if constexpr (FMT == CRVQ_KV_INT8) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (float)(int8_t)(w >> (8 * j));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * j)), __NV_E4M3);
-      const float2 f = __half22float2(__half2(r));
-      v[2 * j] = f.x;
-      v[2 * j + 1] = f.y;
-    }
-  }
-}
-
 // One head's keys or values of a block: this thread's new values x (is_new) or old codes to new codes, with
 // the block's scale, from the largest new magnitude (bits) and the old scale.
 template <int D, int FMT>

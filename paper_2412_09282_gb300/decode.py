@@ -214,6 +214,84 @@ def crvq_cache_attention(cache, q, q_off=None, scale=None, causal=True, window=0
     return (out, lse) if want_lse else out
 
 
+def crvq_tree_mask(parents, n_seq, off=None, lens=None, max_new=None, window=0, mask_out=None, positions_out=None,
+                   stream=None):
+    """(mask, positions) of trees of drafted tokens from their parents ([n_tok] int32: numbers within a sequence's tree,
+    -1 for roots; parents before children): mask [n_tok x ceil(max_new / 32)] int32, bit j of a row set for the token
+    itself and its ancestors (less than window generations before it), positions [n_tok] int32. max_new: the largest
+    tree's tokens (without off, n_tok / n_seq)."""
+    _device(parents, torch.int32, "parents")
+    if parents.dim() != 1 or not parents.is_contiguous():
+        raise ValueError("parents must be contiguous with one entry per drafted token")
+    n_tok = parents.shape[0]
+    if n_seq < 1:
+        raise ValueError("n_seq must be >= 1")
+    if lens is not None:
+        _device(lens, torch.int32, "lens")
+        if lens.shape != (n_seq,) or not lens.is_contiguous():
+            raise ValueError("lens must be contiguous with one entry per sequence")
+    if max_new is None:
+        if off is not None:
+            raise ValueError("max_new (the largest tree's tokens) is needed with off")
+        max_new = -(-n_tok // n_seq)
+    words = max(1, -(-max_new // 32))
+    if off is None and n_tok > 32 * words * n_seq:
+        raise ValueError(f"max_new ({max_new}) is less than a tree's tokens")
+    if mask_out is None:
+        mask_out = _empty((n_tok, words), device=parents.device, dtype=torch.int32)
+    else:
+        _device(mask_out, torch.int32, "mask_out")
+        if mask_out.shape != (n_tok, words) or not mask_out.is_contiguous():
+            raise ValueError(f"mask_out must be contiguous n_tok x {words}")
+    if positions_out is None:
+        positions_out = _empty((n_tok,), device=parents.device, dtype=torch.int32)
+    else:
+        _device(positions_out, torch.int32, "positions_out")
+        if positions_out.shape != (n_tok,) or not positions_out.is_contiguous():
+            raise ValueError("positions_out must be contiguous with one entry per drafted token")
+    st = _L().crvq_tree_mask(parents.data_ptr(), n_tok, _offsets(off, n_seq, "off"), n_seq,
+                             None if lens is None else lens.data_ptr(), window, mask_out.data_ptr(), words,
+                             positions_out.data_ptr(),
+                             _raw_stream(parents.get_device()) if stream is None else
+                             _foreign(stream, parents, off, lens, mask_out, positions_out))
+    if st:
+        _check(st)
+    return mask_out, positions_out
+
+
+def crvq_cache_tree_attention(cache, q, mask, q_off=None, positions=None, scale=None, window=0, out=None,
+                              want_lse=False, stream=None):
+    """Attention of trees of drafted tokens, a sequence's last ones, over the cache: every query (tokens x heads x
+    head_dim) sees the tokens before its tree and those of the tree whose bits its row of mask ([n_tok x words] int32) has;
+    a window needs the queries' positions. Returns out, or (out, lse) with want_lse."""
+    d = cache.head_dim
+    n_tok = q.shape[0]
+    qc = _heads(q, "q", d)
+    _device(mask, torch.int32, "mask")
+    if mask.dim() != 2 or mask.shape[0] != n_tok or mask.shape[1] < 1 or not mask.is_contiguous():
+        raise ValueError("mask must be contiguous n_tok x words")
+    if positions is not None:
+        _device(positions, torch.int32, "positions")
+        if positions.shape != (n_tok,) or not positions.is_contiguous():
+            raise ValueError("positions must be contiguous with one entry per token")
+    if out is None:
+        out = _empty(q.shape, device=q.device, dtype=q.dtype)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    oc = _heads(out, "out", d)
+    lse = _empty(q.shape[:2], device=q.device, dtype=torch.float32) if want_lse else None
+    st = _L().crvq_cache_tree_attention(cache._addr, _addressof(qc), n_tok, _offsets(q_off, cache.n_seq, "q_off"),
+                                        mask.data_ptr(), mask.shape[1],
+                                        None if positions is None else positions.data_ptr(),
+                                        1.0 / math.sqrt(d) if scale is None else scale, window, _addressof(oc),
+                                        None if lse is None else lse.data_ptr(),
+                                        _raw_stream(cache.index) if stream is None else
+                                        _foreign(stream, q, out, lse, q_off, mask, positions, *cache.tensors()))
+    if st:
+        _check(st)
+    return (out, lse) if want_lse else out
+
+
 class Q4Matrix:
     """A matrix with 4-bit weights (crvq_q4_matrix): codes [M x ceil(N / 2)] uint8 (two per byte, the even
     column in the low bits), scales [M x ceil(N / group)] bfloat16, zeros of that shape, uint8, or None (8).
