@@ -601,6 +601,31 @@ crvq_status crvq_cache_tree_attention(const crvq_kv_cache* cache, const crvq_hea
                                       const int32_t* positions, float scale, int32_t window,
                                       const crvq_heads* out, float* lse, crvq_stream_t stream);
 
+/* A number per cached token and kv head: data[b * ld_seq + h * ld_head + t] for token t of sequence b, 0 <= t < width
+ * (strides in elements; rows do not overlap). */
+typedef struct crvq_token_sums {
+  float* data;
+  int64_t ld_seq;
+  int64_t ld_head;
+  int64_t width;
+} crvq_token_sums;
+
+/*
+ * How much attention every cached token gets from a step's queries, added to what it had:
+ *   out[b][h][t] = decay * before[b][h][t] + sum exp(scale * q[i][g] . K_t - lse[i][g])
+ * over the queries i of sequence b that see the token t and the query heads g of kv head h: the softmax's weights, by the lse
+ * that crvq_cache_attention returned for the same queries, scale, causal and window. Tokens 0 .. lens[b] of every sequence
+ * get their sums (without queries: decay * before), the places behind them 0.
+ *   lse     [n_tok x q->heads] fp32; a query with an infinite lse (one that sees nothing) adds nothing.
+ *   before  or NULL: zeros. The same memory as out, or none that it shares. Finite decay.
+ * Both have the same width; tokens at or behind it have no sum and are reported as CRVQ_ERR_DEVICE by crvq_sync.
+ * Scores and sums are fp32 (products as in crvq_cache_attention), every sum in one fixed order.
+ */
+crvq_status crvq_cache_weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok,
+                               const int32_t* q_off, float scale, int32_t causal, int32_t window,
+                               const float* lse, const crvq_token_sums* before, float decay,
+                               const crvq_token_sums* out, crvq_stream_t stream);
+
 /*
  * A matrix in 4 bits with a scale per group of inputs: W[i][j] = (code - zero) * scale, code of (i, j)
  * the low (j even) or high (j odd) four bits of codes[i * ld_codes + j / 2], scale and zero those of

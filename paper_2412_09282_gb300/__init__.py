@@ -18,5 +18,5 @@ from .api import (  # noqa: F401
 )
 from .decode import (  # noqa: F401
     KVCache, Q4Matrix, crvq_cache_append, crvq_cache_attention, crvq_cache_read, crvq_cache_tree_attention,
-    crvq_q4_matvec, crvq_q4_quantize, crvq_tree_mask,
+    crvq_cache_weights, crvq_q4_matvec, crvq_q4_quantize, crvq_tree_mask,
 )

@@ -59,6 +59,10 @@ class crvq_kv_cache(C.Structure):
                 ("format", C.c_int32)]
 
 
+class crvq_token_sums(C.Structure):
+    _fields_ = [("data", c_vp), ("ld_seq", C.c_int64), ("ld_head", C.c_int64), ("width", C.c_int64)]
+
+
 class crvq_rotary(C.Structure):
     _fields_ = [("cos", c_vp), ("sin", c_vp), ("positions", c_vp), ("n_pos", C.c_int64),
                 ("ld", C.c_int64), ("half", C.c_int32), ("interleaved", C.c_int32)]
@@ -127,6 +131,8 @@ SIGNATURES = {
                                    c_vp, c_vp]),
     "crvq_cache_tree_attention": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, c_vp, C.c_int32, c_vp,
                                               C.c_float, C.c_int32, c_vp, c_vp, c_vp]),
+    "crvq_cache_weights": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, C.c_float, C.c_int32, C.c_int32,
+                                       c_vp, c_vp, C.c_float, c_vp, c_vp]),
     "crvq_q4_quantize": (C.c_int32, [c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_q4_matvec": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int32, c_vp, C.c_int64,
                                    c_vp]),

@@ -57,6 +57,8 @@ crvq_status make_cache(const crvq_kv_cache* c, CacheView* out);
 crvq_status make_heads(const crvq_heads* h, const char* name, int head_dim, int64_t n_tok,
                        HeadsView* out);
 crvq_status make_rows(const int32_t* off, int64_t n_tok, int n_seq, RowsView* out);
+// (weights.cu)
+crvq_status check_sums(const crvq_token_sums* s, const char* name, int n_seq, int n_kv);
 
 inline size_t type_bytes(int type) { return type == CRVQ_F32 ? 4 : 2; }
 

@@ -1,0 +1,329 @@
+// How much attention every cached token gets from a step's queries, added to what it had:
+//   out[b][h][t] = decay * before[b][h][t] + sum over the sequence's queries i and the query heads g of kv head h of
+//                  exp(scale q_ig . K_t - lse_ig).
+// The softmax's sum is known (lse), so tokens do not depend on one another: no maxima, no rescaling, nothing to join, and
+// every sum is one warp's, in a fixed order.
+//
+// Form. S^T (16 tokens x 8 columns, a column = a query token and head) = K Q^T on mma.sync.m16n8k16 with the codes as A
+// operand, as attention does for few queries (attend_mma.cuh), and the weights summed over the columns: in a lane's
+// registers, then over the four lanes that share a token. A warp takes two blocks of 16 tokens at a time (one of 256
+// channels), turns their codes into operands once and goes over all columns with them; up to `chunk` columns' queries lie
+// in shared memory as fp16 relative to a power of two each (two operands from fp32). Blocks are copied ahead into a ring
+// per warp, four steps deep: only keys are read, half of what attention reads.
+#include "weights.cuh"
+
+namespace crvq {
+
+namespace {
+
+template <int D>
+struct WShape {
+  static constexpr int kQRow = D + 8;  // halves per query row, padded against bank conflicts
+  static constexpr int kStages = 4;
+  static constexpr int kStage = Tile<D>::kBytes * kBlocks<D>;
+  static constexpr int kRing = kStage * kStages;
+  static constexpr int kMost = 256;    // columns at a time
+  static size_t smem(int chunk, bool split) {
+    return (size_t)kWarps * kRing + (size_t)chunk * (kQRow * 2 * (split ? 2 : 1) + 16);
+  }
+};
+
+template <int D, int FMT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, D == 256 ? 2 : 3)
+weights_kernel(const __grid_constant__ WeightArgs w) {
+  using S = WShape<D>;
+  constexpr int NB = kBlocks<D>;
+  const AttendArgs& a = w.a;
+  extern __shared__ __align__(16) char sm[];
+  char* ring = sm;                                                  // [kWarps][kStages][blocks] tiles
+  __half* q_s = reinterpret_cast<__half*>(sm + kWarps * S::kRing);  // [split][chunk][kQRow]
+  float4* col_s = reinterpret_cast<float4*>(q_s + (size_t)(SPLIT ? 2 : 1) * w.chunk * S::kQRow);  // factor, -lse, first, end
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+  const Line<D, kAllColumns> line(a);
+  const int shares = (int)min((int64_t)a.shares, line.total);
+  int64_t at = 0, at_end = 0;
+  if ((int)blockIdx.x < shares) {
+    at = share_begin(line.total, blockIdx.x, shares);
+    at_end = share_begin(line.total, blockIdx.x + 1, shares);
+  }
+  char* mine = ring + warp * S::kRing;
+  const uint32_t mine_u = (uint32_t)__cvta_generic_to_shared(mine);
+  const uint32_t key_at = Tile<D>::at(gid, tig);
+
+  while (at < at_end) {
+    const Unit u = line.locate(a, at);
+    const int64_t tile0 = u.begin + kStart, unit_end = tile0 + u.s.tiles;
+    const int t_end = (int)max((int64_t)0, min(unit_end, at_end) - tile0);
+    at = min(unit_end, at_end);
+    if (u.tile >= t_end) continue;
+    const int len = u.s.len, held = len - u.s.n, group = a.group;
+    const int64_t cols = (int64_t)u.s.n * group;
+    const int some_b = a.window > 0 ? max(0, held - a.window + 1) : 0;
+    const int n_tiles = t_end - u.tile;
+    float* out = w.out + u.b * w.out_seq + u.h * w.out_head;
+    const float* before = w.before ? w.before + u.b * w.before_seq + u.h * w.before_head : nullptr;
+
+    for (int64_t c0 = 0; c0 < cols; c0 += w.chunk) {
+      const int n_cols = (int)min((int64_t)w.chunk, cols - c0), groups = (n_cols + 7) / 8;
+      __syncthreads();  // the previous columns have been read
+      // places: a lane looks up every 32nd of this warp's blocks (as attend_kernel does)
+      int64_t at_l = -1, at_old = -1;
+      float sk_l = 0.f, sk_old = 0.f;
+      int batch = -1;
+      auto look_up = [&](int i) {
+        if (i >= n_tiles || (i * NB & 31) != 0) return;
+        at_old = at_l;
+        sk_old = sk_l;
+        batch = i * NB >> 5;
+        const int tl = u.tile + i + lane / NB;
+        const int tok = (u.s.lo + tl) * kTile<D> + (warp * NB + lane % NB) * kCacheBlock;
+        at_l = -1;
+        if (tl < t_end && tok < len && tok + kCacheBlock > some_b) {
+          const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
+          if (page >= 0) {
+            const int in = tok % a.c.page;
+            at_l = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
+            sk_l = __ldg(a.c.ks + (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock);
+          }
+        }
+      };
+      auto start = [&](int i) {
+        if (i < n_tiles) {
+          const bool old = (i * NB >> 5) != batch;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const int64_t src = __shfl_sync(0xffffffffu, old ? at_old : at_l, (i * NB + b) & 31);
+            if (src >= 0)
+              start_block<D, false>(a.c.K + src, mine_u + (i % S::kStages) * S::kStage + b * Tile<D>::kBytes, kCacheBlock);
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+#pragma unroll
+      for (int i = 0; i < S::kStages - 1; ++i) {
+        look_up(i);
+        start(i);
+      }
+      // queries: a warp per column, relative to the power of two at its largest element
+      for (int col = warp; col < 8 * groups; col += kWarps) {
+        const int64_t c = c0 + col;
+        const bool valid = col < n_cols;
+        const int j = valid ? (int)(c / group) : 0, h = u.h * group + (valid ? (int)(c % group) : 0);
+        const float lse = valid ? __ldg(w.lse + (u.s.first + j) * a.q.heads + h) : INFINITY;
+        const bool none = isinf(lse);  // (such a query has no weights)
+        float x[D / 32];
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          x[e] = none ? 0.f : load_elem(a.q.data, (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head + lane + 32 * e, a.q.type);
+          top = fmaxf(top, fabsf(x[e]));
+        }
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+        const uint32_t ex = __float_as_uint(top) >> 23;
+        const bool plain = ex == 0 || ex == 255;
+        const float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
+        const float back = plain ? 1.f : __uint_as_float(ex << 23);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          const float v = x[e] * inv;
+          const __half hi = __float2half_rn(v);
+          q_s[col * S::kQRow + lane + 32 * e] = hi;
+          if constexpr (SPLIT) q_s[(w.chunk + col) * S::kQRow + lane + 32 * e] = __float2half_rn(v - __half2float(hi));
+        }
+        if (lane == 0) {
+          const int pos = held + j;
+          col_s[col] = make_float4(none ? 0.f : back * a.scale, none ? -INFINITY : -lse * kLog2e,
+                                   __int_as_float(a.window > 0 ? max(0, pos - a.window + 1) : 0),
+                                   __int_as_float(a.causal ? min(len, pos + 1) : len));
+        }
+      }
+      __syncthreads();
+      // keys that every column sees (places do not fall from column to column)
+      const int every_b = __float_as_int(col_s[n_cols - 1].z), every_e = __float_as_int(col_s[0].w);
+
+      for (int i = 0; i < n_tiles; ++i) {
+        const bool old = (i * NB >> 5) != batch;
+        const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
+        float sk[NB];
+        bool live[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          sk[b] = __shfl_sync(0xffffffffu, old ? sk_old : sk_l, (i * NB + b) & 31);
+          live[b] = __shfl_sync(0xffffffffu, old ? at_old : at_l, (i * NB + b) & 31) >= 0;
+        }
+        // this lane's sum is that of one token: block tig / 2, row gid + 8 (tig % 2)
+        const int t_mine = tok + (tig >> 1) * kCacheBlock + (tig & 1) * 8 + gid;
+        const bool writes = (tig >> 1) < NB && t_mine < len && t_mine < w.width;
+        float base = 0.f;
+        if (writes) {
+          if (c0 > 0)
+            base = out[t_mine];
+          else if (before)
+            base = w.decay * __ldg(before + t_mine);
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+        __syncwarp();
+        const char* keys = mine + (i % S::kStages) * S::kStage;
+        uint32_t k[NB][D / 16][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int j = 0; j < D / 64; ++j) {
+            const char* p = keys + b * Tile<D>::kBytes + (j >> 1) * 128;
+            const uint4 k0 = *reinterpret_cast<const uint4*>(p + (key_at ^ (j & 1) * 64));
+            const uint4 k1 = *reinterpret_cast<const uint4*>(p + 8 * D + (key_at ^ (j & 1) * 64));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = word(k0, e), y = word(k1, e);
+              k[b][4 * j + e][0] = codes2<FMT, 0>(x);
+              k[b][4 * j + e][1] = codes2<FMT, 0>(y);
+              k[b][4 * j + e][2] = codes2<FMT, 1>(x);
+              k[b][4 * j + e][3] = codes2<FMT, 1>(y);
+            }
+          }
+        __syncwarp();  // every lane has read what these copies overwrite
+        look_up(i + S::kStages - 1);
+        start(i + S::kStages - 1);
+        const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e;
+        float sum[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sum[b][0] = sum[b][1] = 0.f;
+        for (int g = 0; g < groups; ++g) {
+          float s[NB][4];
+#pragma unroll
+          for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
+#pragma unroll
+          for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+            for (int z = 0; z < (SPLIT ? 2 : 1); ++z) {
+              const uint4* p = reinterpret_cast<const uint4*>(q_s + ((size_t)z * w.chunk + 8 * g + gid) * S::kQRow + 64 * j + 16 * tig);
+              const uint4 x = p[0], y = p[1];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                  mma_f16(s[b], k[b][4 * j + e][0], k[b][4 * j + e][1], k[b][4 * j + e][2], k[b][4 * j + e][3],
+                          e < 2 ? word(x, 2 * e) : word(y, 2 * e - 4), e < 2 ? word(x, 2 * e + 1) : word(y, 2 * e - 3));
+            }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float4 c = col_s[8 * g + 2 * tig + e];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              const float f = c.x * sk[b];
+              float p0 = pow2(fmaf(s[b][e], f, c.y)), p1 = pow2(fmaf(s[b][e + 2], f, c.y));
+              if (!whole) {
+                const int t0 = tok + b * kCacheBlock + gid, kb = __float_as_int(c.z), ke = __float_as_int(c.w);
+                if (t0 < kb || t0 >= ke) p0 = 0.f;
+                if (t0 + 8 < kb || t0 + 8 >= ke) p1 = 0.f;
+              }
+              sum[b][0] += p0;
+              sum[b][1] += p1;
+            }
+          }
+        }
+        float v = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = live[b] ? sum[b][e] : 0.f;
+            x += __shfl_xor_sync(0xffffffffu, x, 1);
+            x += __shfl_xor_sync(0xffffffffu, x, 2);
+            if (tig == 2 * b + e) v = x;
+          }
+        if (writes) out[t_mine] = base + v;
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+  }
+  unseen_places<D>(w);
+}
+
+template <int D, int FMT, bool SPLIT>
+crvq_status launch(WeightArgs& w, cudaStream_t stream) {
+  using S = WShape<D>;
+  auto kernel = weights_kernel<D, FMT, SPLIT>;
+  const AttendArgs& a = w.a;
+  // columns of a sequence, by the average where the rows' offsets are on the device
+  const int64_t cols = a.rows.off ? 2 * ceil_div(a.rows.n_tok * a.group, a.c.n_seq) : (int64_t)a.rows.per * a.group;
+  w.chunk = (int)min((int64_t)S::kMost, ceil_div(max(cols, (int64_t)1), 8) * 8);
+  const size_t smem = S::smem(w.chunk, SPLIT);
+  CRVQ_TRY(smem_limit((const void*)kernel, smem));
+  const int per_sm = max(1, min(D == 256 ? 2 : 3, (int)(233472 / (smem + 1024))));
+  w.a.shares = sm_count() * per_sm;
+  ProfScope ps("cache_weights", stream, (double)a.rows.n_tok * a.q.heads * D);
+  CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)w.a.shares), dim3(kThreads), smem, stream, w));
+  CRVQ_LAUNCHED();
+  return CRVQ_OK;
+}
+
+template <int D>
+crvq_status pick(WeightArgs& w, int format, cudaStream_t stream) {
+  const bool split = w.a.q.type == CRVQ_F32;
+  if (format == CRVQ_KV_INT8)
+    return split ? launch<D, CRVQ_KV_INT8, true>(w, stream) : launch<D, CRVQ_KV_INT8, false>(w, stream);
+  return split ? launch<D, CRVQ_KV_E4M3, true>(w, stream) : launch<D, CRVQ_KV_E4M3, false>(w, stream);
+}
+
+crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok, const int32_t* q_off, float scale,
+                    int32_t causal, int32_t window, const float* lse, const crvq_token_sums* before, float decay,
+                    const crvq_token_sums* out, cudaStream_t stream) {
+  WeightArgs w{};
+  CRVQ_TRY(attend_args(cache, q, n_tok, q_off, scale, window, q, nullptr, &w.a));
+  CRVQ_TRY(check_sums(out, "out", w.a.c.n_seq, w.a.c.n_kv));
+  CRVQ_CHECK_ARG(lse != nullptr || n_tok == 0, "lse is NULL");
+  CRVQ_CHECK_ARG(((uintptr_t)lse & 3u) == 0, "lse is not aligned");
+  CRVQ_TRY(check_dev({{lse, "lse"}}));
+  CRVQ_CHECK_ARG(fabsf(decay) <= 3.402823466e38f, "decay must be finite");
+  if (before) {
+    CRVQ_TRY(check_sums(before, "before", w.a.c.n_seq, w.a.c.n_kv));
+    CRVQ_CHECK_ARG(before->width == out->width, "before and out differ in width");
+    CRVQ_CHECK_ARG(before->data != out->data || (before->ld_seq == out->ld_seq && before->ld_head == out->ld_head),
+                   "before and out share memory with different strides");
+    w.before = before->data;
+    w.before_seq = before->ld_seq;
+    w.before_head = before->ld_head;
+  }
+  w.a.causal = causal != 0;
+  w.lse = lse;
+  w.out = out->data;
+  w.out_seq = out->ld_seq;
+  w.out_head = out->ld_head;
+  w.width = out->width;
+  w.decay = decay;
+  const int D = cache->head_dim;
+  if (D == 64) return pick<64>(w, cache->format, stream);
+  if (D == 128) return pick<128>(w, cache->format, stream);
+  return pick<256>(w, cache->format, stream);
+}
+
+}  // namespace
+
+crvq_status check_sums(const crvq_token_sums* s, const char* name, int n_seq, int n_kv) {
+  CRVQ_CHECK_ARG(s != nullptr && s->data != nullptr, "%s is NULL", name);
+  CRVQ_CHECK_ARG(((uintptr_t)s->data & 3u) == 0, "%s is not aligned", name);
+  CRVQ_CHECK_ARG(s->width >= 1 && s->width < (int64_t)1 << 31, "%s: width must be in [1, 2^31)", name);
+  // rows that do not overlap, in either order
+  const int64_t row = s->width, by_head = s->ld_head, by_seq = s->ld_seq;
+  const bool seq_outer = (n_kv == 1 || by_head >= row) && (n_seq == 1 || by_seq >= (n_kv == 1 ? row : by_head * (n_kv - 1) + row));
+  const bool head_outer = (n_seq == 1 || by_seq >= row) && (n_kv == 1 || by_head >= (n_seq == 1 ? row : by_seq * (n_seq - 1) + row));
+  CRVQ_CHECK_ARG(seq_outer || head_outer, "%s: rows overlap", name);
+  return check_dev({{s->data, name}});
+}
+
+}  // namespace crvq
+
+extern "C" {
+
+crvq_status crvq_cache_weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok, const int32_t* q_off,
+                               float scale, int32_t causal, int32_t window, const float* lse,
+                               const crvq_token_sums* before, float decay, const crvq_token_sums* out,
+                               crvq_stream_t stream) {
+  CRVQ_ENTRY({
+    return crvq::weights(cache, q, n_tok, q_off, scale, causal, window, lse, before, decay, out, (cudaStream_t)stream);
+  })
+}
+
+}  // extern "C"

@@ -292,6 +292,41 @@ def crvq_cache_tree_attention(cache, q, mask, q_off=None, positions=None, scale=
     return (out, lse) if want_lse else out
 
 
+def _sums(t, name, n_seq, n_kv):
+    """crvq_token_sums of an n_seq x n_kv x width view with unit stride in the last dimension."""
+    _device(t, torch.float32, name)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n_seq or shape[1] != n_kv or stride[2] != 1:
+        raise ValueError(f"{name} must be {n_seq} x {n_kv} x width with unit stride in the last dimension")
+    return _lib.crvq_token_sums(t.data_ptr(), stride[0], stride[1], shape[2])
+
+
+def crvq_cache_weights(cache, q, lse, q_off=None, scale=None, causal=True, window=0, weights=None, decay=1.0, out=None,
+                       stream=None):
+    """How much attention every cached token gets from the queries q whose attention returned lse (the same q_off, scale,
+    causal and window), added to decay * weights: [n_seq x n_kv x width] fp32, 0 behind every sequence's tokens. out may
+    be weights; a new one has room for every place of the page table."""
+    d = cache.head_dim
+    qc = _heads(q, "q", d)
+    _device(lse, torch.float32, "lse")
+    if lse.shape != q.shape[:2] or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous tokens x heads")
+    if weights is not None:
+        wc = _sums(weights, "weights", cache.n_seq, cache.n_kv)
+    if out is None:
+        width = cache.pages.shape[1] * cache.page if weights is None else weights.shape[2]
+        out = _empty((cache.n_seq, cache.n_kv, width), device=cache.device, dtype=torch.float32)
+    oc = _sums(out, "out", cache.n_seq, cache.n_kv)
+    st = _L().crvq_cache_weights(cache._addr, _addressof(qc), q.shape[0], _offsets(q_off, cache.n_seq, "q_off"),
+                                 1.0 / math.sqrt(d) if scale is None else scale, causal, window, lse.data_ptr(),
+                                 None if weights is None else _addressof(wc), decay, _addressof(oc),
+                                 _raw_stream(cache.index) if stream is None else
+                                 _foreign(stream, q, lse, q_off, weights, out, *cache.tensors()))
+    if st:
+        _check(st)
+    return out
+
+
 class Q4Matrix:
     """A matrix with 4-bit weights (crvq_q4_matrix): codes [M x ceil(N / 2)] uint8 (two per byte, the even
     column in the low bits), scales [M x ceil(N / group)] bfloat16, zeros of that shape, uint8, or None (8).
