@@ -627,6 +627,40 @@ crvq_status crvq_cache_weights(const crvq_kv_cache* cache, const crvq_heads* q, 
                                const crvq_token_sums* out, crvq_stream_t stream);
 
 /*
+ * Which tokens of every sequence and kv head stay when a cache is cut down to `keep` tokens: all of a sequence with no more;
+ * else its `first` first and `recent` last ones and, of those between, the ones with the largest weights, of equal ones
+ * those in front (-0 equals 0, NaN is above infinity).
+ *   lens    [n_seq] int32, tokens of every sequence, at most weights->width (others are reported, and count as 0).
+ *   keep    >= 1 and >= first + recent.
+ *   idx     [n_seq x n_kv x keep] int32: the places that stay, in order; -1 behind the last.
+ *   count   [n_seq] int32: min(lens[b], keep), the tokens that stay.
+ *   weights_out  or NULL: the weights of those tokens, in their order, and 0 behind them; at least min(keep,
+ *                weights->width) wide. Shares no memory with weights.
+ */
+crvq_status crvq_cache_select(const crvq_token_sums* weights, const int32_t* lens, int32_t n_seq, int32_t n_kv,
+                              int32_t keep, int32_t first, int32_t recent, int32_t* idx, int32_t* count,
+                              const crvq_token_sums* weights_out, crvq_stream_t stream);
+
+/*
+ * Moves tokens together: for r < count[b], place start[b] + r of sequence b of `out` gets, per kv head h, the keys and
+ * values of token idx[b * ld_seq + h * ld_head + r] of sequence b of cache (ld_head 0: the same tokens for all heads).
+ *   idx    places in [0, cache->lens[b]), `most` columns, of which count[b] are read.
+ *   start  [n_seq] int32 or NULL: 0. Tokens before it in its block stay where they are.
+ *   out    cache itself (the same arrays and page table), or a cache of the same n_seq, n_kv, head_dim and format whose
+ *          pages that are written are no page that is read: of another pool, or of the same one. Its lens are not read:
+ *          to be set to start[b] + count[b], by the caller, after the call. Sequences do not share a page that is written.
+ * A block's scale becomes the largest of its tokens' scales, codes c become round(c * (their scale / its scale)), ties to
+ * even, in fp32: codes that keep their scale keep their bits. The block of place start[b] - 1 is rescaled with the tokens
+ * that come into it; places behind the last moved token are not written (in its block they lose their scale).
+ * In place tokens move towards the front: idx >= start[b] + r, as places in ascending order do that begin at start[b] or
+ * behind it. Places that break these rules, a count outside [0, most], and pages out of range are reported as
+ * CRVQ_ERR_DEVICE by crvq_sync; such tokens are stored as 0, such a sequence's (page's) are not moved.
+ */
+crvq_status crvq_cache_keep(const crvq_kv_cache* cache, const int32_t* idx, int64_t ld_seq, int64_t ld_head,
+                            int32_t most, const int32_t* count, const int32_t* start,
+                            const crvq_kv_cache* out, crvq_stream_t stream);
+
+/*
  * A matrix in 4 bits with a scale per group of inputs: W[i][j] = (code - zero) * scale, code of (i, j)
  * the low (j even) or high (j odd) four bits of codes[i * ld_codes + j / 2], scale and zero those of
  * group j / group of row i.

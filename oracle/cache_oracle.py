@@ -123,7 +123,8 @@ def select(w, lens, keep, first, recent):
             if length > keep:
                 lo, hi = first, length - recent
                 x = w[b, h, lo:hi].astype(np.float64)
-                best = lo + np.argsort(-np.where(np.isnan(x), np.inf, x), kind="stable")[:keep - first - recent]
+                nan = np.isnan(x)                              # (above infinity)
+                best = lo + np.lexsort((-np.where(nan, 0.0, x), ~nan))[:keep - first - recent]
                 t = np.concatenate([t[:lo], np.sort(best), t[hi:]])
             idx[b, h, :len(t)] = t
             out[b, h, :len(t)] = w[b, h, t]

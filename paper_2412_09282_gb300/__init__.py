@@ -17,6 +17,6 @@ from .api import (  # noqa: F401
     IMPORTANCE_WA_INV, library_path,
 )
 from .decode import (  # noqa: F401
-    KVCache, Q4Matrix, crvq_cache_append, crvq_cache_attention, crvq_cache_read, crvq_cache_tree_attention,
-    crvq_cache_weights, crvq_q4_matvec, crvq_q4_quantize, crvq_tree_mask,
+    KVCache, Q4Matrix, crvq_cache_append, crvq_cache_attention, crvq_cache_keep, crvq_cache_read,
+    crvq_cache_select, crvq_cache_tree_attention, crvq_cache_weights, crvq_q4_matvec, crvq_q4_quantize, crvq_tree_mask,
 )

@@ -133,6 +133,10 @@ SIGNATURES = {
                                               C.c_float, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_cache_weights": (C.c_int32, [c_vp, c_vp, C.c_int64, c_vp, C.c_float, C.c_int32, C.c_int32,
                                        c_vp, c_vp, C.c_float, c_vp, c_vp]),
+    "crvq_cache_select": (C.c_int32, [c_vp, c_vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                      C.c_int32, c_vp, c_vp, c_vp, c_vp]),
+    "crvq_cache_keep": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int32, c_vp, c_vp, c_vp,
+                                    c_vp]),
     "crvq_q4_quantize": (C.c_int32, [c_vp, C.c_int64, C.c_int32, c_vp, c_vp, c_vp]),
     "crvq_q4_matvec": (C.c_int32, [c_vp, c_vp, C.c_int64, C.c_int64, C.c_int32, c_vp, C.c_int64,
                                    c_vp]),

@@ -1,0 +1,250 @@
+// Moving kept tokens together in a paged 8-bit cache: token idx[b][h][r] of the source goes to place start[b] + r of the
+// destination. Per block of 16 places of a head's keys or values that tokens c_i at scales s_i come to (with those tokens
+// before start[b] that the block holds already),
+//   s = max_i s_i,   c_i <- round(c_i * (s_i / s)),
+// each operation rounded to fp32: codes that keep their scale keep their bits.
+//
+// A CTA takes tiles of a few blocks of one head's keys or values: it looks up where every token of the tile lies (one thread a
+// token), then each thread moves 16 codes at a time, a block's scale found by every thread that writes to it.
+//   In place the tiles of a (sequence, head) are dealt out to the CTAs of a cluster, round by round: a round's codes and
+// scales are read by all of them before any is written. Tokens only move towards the front there (idx >= place), so what a
+// later round reads lies behind all that earlier ones have written.
+#include "cache.cuh"
+#include "kernels.h"
+
+namespace crvq {
+
+namespace {
+
+constexpr int kKeepThreads = 256;
+
+struct KeepArgs {
+  CacheView from, to;
+  const int32_t* idx;
+  const int32_t* count;
+  const int32_t* start;  // or null: 0
+  int64_t ld_seq, ld_head;
+  int most;              // columns of idx
+  int tiles;             // grid: CTAs per (sequence, head, keys or values)
+  bool same_pool;        // (then written pages must be others than those read at the same places)
+  Divisor from_page, to_page;
+  unsigned* err;
+};
+
+template <int D>
+struct KeepShape {
+  static constexpr int kRow = D / 16;                     // threads per token
+  static constexpr int kSlots = kKeepThreads / kRow;      // tokens at a time: 64, 32 or 16
+  static constexpr int kTimes = 4;
+  static constexpr int kTokens = kSlots * kTimes;         // of a tile
+};
+
+template <int D, int FMT, bool IN_PLACE>
+__global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ KeepArgs a) {
+  using S = KeepShape<D>;
+  __shared__ int64_t src_s[S::kTokens];                   // codes' places in the source (-1: none), dst per block
+  __shared__ int64_t dst_s[S::kTokens / kCacheBlock], dst_scale_s[S::kTokens / kCacheBlock];
+  __shared__ float scale_s[S::kTokens];
+  __shared__ bool old_s[S::kTokens];
+  pdl_wait();
+  const int tid = threadIdx.x;
+  const int unit = blockIdx.x / a.tiles, rank = blockIdx.x - unit * a.tiles;
+  const bool is_key = !(unit & 1);
+  const int b = (unit >> 1) / a.from.n_kv, h = (unit >> 1) - b * a.from.n_kv;
+  int n = __ldg(a.count + b);
+  const int start = a.start ? __ldg(a.start + b) : 0;
+  if (n < 0 || n > a.most || start < 0 || (int64_t)start + n > (int64_t)a.to.max_pages * a.to.page) {
+    raise_error(a.err, ERRBIT_INDEX);
+    n = 0;
+  }
+  if (n == 0) return;  // (with its whole cluster)
+  const int len = seq_len(a.from, b, a.err);
+  const int base = start / kCacheBlock * kCacheBlock, end = start + n;
+  const int n_tiles = (end - base + S::kTokens - 1) / S::kTokens;
+  const int rounds = IN_PLACE ? (n_tiles + a.tiles - 1) / a.tiles : (rank < n_tiles ? 1 : 0);
+  const int32_t* idx = a.idx + b * a.ld_seq + h * a.ld_head;
+  const uint8_t* from = is_key ? a.from.K : a.from.V;
+  uint8_t* to = is_key ? a.to.K : a.to.V;
+  const float* from_scale = is_key ? a.from.ks : a.from.vs;
+  float* to_scale = is_key ? a.to.ks : a.to.vs;
+  const int from_blocks = (unsigned)a.from.page / kCacheBlock, to_blocks = (unsigned)a.to.page / kCacheBlock;
+  const int col = tid % S::kRow, slot = tid / S::kRow;
+
+  for (int round = 0; round < rounds; ++round) {
+    const int p0 = base + (rank + round * a.tiles) * S::kTokens;
+    __syncthreads();  // the previous tile's places have been read
+    // places: p0 + tid, for the tile's first threads
+    if (tid < S::kTokens) {
+      const int p = p0 + tid;
+      int64_t src = -1, dst = -1;
+      float scale = 0.f;
+      bool old = false;
+      if (p < end) {
+        const int to_entry = a.to_page.div(p), to_in = p - to_entry * a.to.page;
+        const int64_t to_id = seq_page(a.to, b, to_entry, a.err);
+        if (to_id >= 0) {
+          dst = to_id * a.to.page_stride + ((int64_t)h * a.to.page + to_in) * D;
+          const int64_t at_scale = (to_id * a.to.n_kv + h) * to_blocks + to_in / kCacheBlock;
+          if (p < start) {
+            old = true;
+            src = dst;
+            scale = to_scale[at_scale];
+          } else {
+            const int t = __ldg(idx + (p - start));
+            if (t < 0 || t >= len || (IN_PLACE && t < p)) {
+              raise_error(a.err, ERRBIT_INDEX);
+            } else {
+              const int entry = a.from_page.div(t), in = t - entry * a.from.page;
+              const int64_t id = seq_page(a.from, b, entry, a.err);
+              if (id >= 0) {
+                src = id * a.from.page_stride + ((int64_t)h * a.from.page + in) * D;
+                scale = from_scale[(id * a.from.n_kv + h) * from_blocks + in / kCacheBlock];
+              }
+            }
+          }
+          if (tid % kCacheBlock == 0) dst_scale_s[tid / kCacheBlock] = at_scale;
+        }
+        if (!IN_PLACE && a.same_pool && to_id >= 0 && p < len && a.from.page == a.to.page &&
+            to_id == seq_page(a.from, b, to_entry, a.err)) {
+          raise_error(a.err, ERRBIT_INDEX);  // (in place, unsaid: the order of reads and writes would be open)
+          dst = -1;
+        }
+      }
+      if (tid % kCacheBlock == 0) dst_s[tid / kCacheBlock] = dst;
+      src_s[tid] = src;
+      scale_s[tid] = scale;
+      old_s[tid] = old;
+    }
+    __syncthreads();
+    uint4 codes[S::kTimes];
+#pragma unroll
+    for (int u = 0; u < S::kTimes; ++u) {
+      const int i = u * S::kSlots + slot;
+      const int64_t src = src_s[i];
+      codes[u] = make_uint4(0, 0, 0, 0);
+      if (src >= 0) codes[u] = *reinterpret_cast<const uint4*>((old_s[i] ? to : from) + src + 16 * col);
+    }
+    if (IN_PLACE && a.tiles > 1)
+      asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else if (IN_PLACE)
+      __syncthreads();
+#pragma unroll
+    for (int u = 0; u < S::kTimes; ++u) {
+      const int i = u * S::kSlots + slot, block = i / kCacheBlock;
+      if (p0 + i >= end || dst_s[block] < 0) continue;
+      float s = 0.f;
+      const float4* all = reinterpret_cast<const float4*>(scale_s + block * kCacheBlock);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 x = all[e];
+        s = fmaxf(s, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
+      }
+      const float mine = scale_s[i];
+      uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
+      if (mine != s || !(s > 0.f)) {
+        const float ratio = s > 0.f ? __fdiv_rn(mine, s) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v[4];
+          decode4<FMT>(w[e], v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = src_s[i] >= 0 && ratio > 0.f ? __fmul_rn(v[k], ratio) : 0.f;
+          w[e] = encode4<FMT, false>(v);
+        }
+      }
+      *reinterpret_cast<uint4*>(to + dst_s[block] + (i % kCacheBlock) * D + 16 * col) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (i % kCacheBlock == 0 && col == 0) to_scale[dst_scale_s[block]] = s;
+    }
+  }
+}
+
+template <int D, int FMT>
+crvq_status launch_keep(KeepArgs& a, bool in_place, cudaStream_t stream) {
+  // tiles that n tokens can touch, from any start
+  const int64_t tiles = ceil_div((int64_t)a.most + kCacheBlock - 1, KeepShape<D>::kTokens);
+  const int64_t units = (int64_t)a.from.n_seq * a.from.n_kv * 2;
+  int size = 1;
+  while (in_place && size < 8 && size < tiles) size *= 2;
+  a.tiles = in_place ? size : (int)tiles;
+  if (units * a.tiles >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many tokens in one call");
+  const dim3 grid((unsigned)(units * a.tiles)), threads(kKeepThreads);
+  if (!in_place) {
+    CRVQ_CUDA(launch_pdl(keep_kernel<D, FMT, false>, grid, threads, 0, stream, a));
+  } else {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = threads;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    CRVQ_CUDA(cudaLaunchKernelEx(&cfg, keep_kernel<D, FMT, true>, a));
+  }
+  CRVQ_LAUNCHED();
+  return CRVQ_OK;
+}
+
+template <int D>
+crvq_status pick_format(KeepArgs& a, int format, bool in_place, cudaStream_t stream) {
+  return format == CRVQ_KV_INT8 ? launch_keep<D, CRVQ_KV_INT8>(a, in_place, stream)
+                                : launch_keep<D, CRVQ_KV_E4M3>(a, in_place, stream);
+}
+
+crvq_status keep(const crvq_kv_cache* cache, const int32_t* idx, int64_t ld_seq, int64_t ld_head, int32_t most,
+                 const int32_t* count, const int32_t* start, const crvq_kv_cache* out, cudaStream_t stream) {
+  KeepArgs a{};
+  CRVQ_TRY(make_cache(cache, &a.from));
+  CRVQ_TRY(make_cache(out, &a.to));
+  CRVQ_CHECK_ARG(a.from.n_seq == a.to.n_seq && a.from.n_kv == a.to.n_kv && cache->head_dim == out->head_dim &&
+                     cache->format == out->format,
+                 "cache and out differ in sequences, kv heads, head_dim or format");
+  CRVQ_CHECK_ARG(most >= 0, "most must be >= 0");
+  CRVQ_CHECK_ARG(ld_head == 0 || ld_head >= most, "idx: rows of heads overlap");
+  CRVQ_CHECK_ARG(count != nullptr, "count is NULL");
+  CRVQ_CHECK_ARG((((uintptr_t)idx | (uintptr_t)count | (uintptr_t)start) & 3u) == 0, "idx, count or start is not aligned");
+  CRVQ_TRY(check_dev({{idx, "idx"}, {count, "count"}, {start, "start"}}));
+  if (most == 0) return CRVQ_OK;
+  CRVQ_CHECK_ARG(idx != nullptr, "idx is NULL");
+  CRVQ_CHECK_ARG((cache->K == out->K) == (cache->V == out->V) && (cache->K == out->K) == (cache->k_scale == out->k_scale) &&
+                     (cache->K == out->K) == (cache->v_scale == out->v_scale),
+                 "cache and out share some arrays of a pool, not all");
+  a.same_pool = cache->K == out->K;
+  const bool in_place = a.same_pool && cache->pages == out->pages && cache->ld_pages == out->ld_pages;
+  CRVQ_CHECK_ARG(!in_place || cache->page == out->page, "in place, cache and out differ in page");
+  CRVQ_CHECK_ARG(!a.same_pool || (cache->page == out->page && cache->page_stride == out->page_stride), "cache and out share a pool of different pages");
+  a.idx = idx;
+  a.ld_seq = ld_seq;
+  a.ld_head = ld_head;
+  a.most = most;
+  a.count = count;
+  a.start = start;
+  a.from_page = Divisor(a.from.page);
+  a.to_page = Divisor(a.to.page);
+  CRVQ_TRY(device_error_word(&a.err));
+  ProfScope ps("cache_keep", stream, (double)a.from.n_seq * a.from.n_kv * most * cache->head_dim * 4);
+  if (cache->head_dim == 64) return pick_format<64>(a, cache->format, in_place, stream);
+  if (cache->head_dim == 128) return pick_format<128>(a, cache->format, in_place, stream);
+  return pick_format<256>(a, cache->format, in_place, stream);
+}
+
+}  // namespace
+
+}  // namespace crvq
+
+extern "C" {
+
+crvq_status crvq_cache_keep(const crvq_kv_cache* cache, const int32_t* idx, int64_t ld_seq, int64_t ld_head, int32_t most,
+                            const int32_t* count, const int32_t* start, const crvq_kv_cache* out,
+                            crvq_stream_t stream) {
+  CRVQ_ENTRY({
+    return crvq::keep(cache, idx, ld_seq, ld_head, most, count, start, out, (cudaStream_t)stream);
+  })
+}
+
+}  // extern "C"

@@ -327,6 +327,64 @@ def crvq_cache_weights(cache, q, lse, q_off=None, scale=None, causal=True, windo
     return out
 
 
+def _per_seq(t, n_seq, name):
+    _device(t, torch.int32, name)
+    if t.shape != (n_seq,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with one entry per sequence")
+    return t.data_ptr()
+
+
+def crvq_cache_select(weights, lens, keep, first=0, recent=0, weights_out=None, idx_out=None, count_out=None, stream=None):
+    """(idx, count) of the tokens that stay when every sequence and kv head keeps `keep` of its lens[b] tokens: the first
+    ones, the most recent ones, and those between them with the largest weights ([n_seq x n_kv x width] fp32; ties to the
+    lowest place). idx [n_seq x n_kv x keep] int32, ascending, -1 behind the last; count [n_seq] int32. weights_out gets
+    the weights of those tokens in their order."""
+    if weights.dim() != 3:
+        raise ValueError("weights must be n_seq x n_kv x width")
+    n_seq, n_kv = weights.shape[:2]
+    wc = _sums(weights, "weights", n_seq, n_kv)
+    lens_at = _per_seq(lens, n_seq, "lens")
+    if weights_out is not None:
+        oc = _sums(weights_out, "weights_out", n_seq, n_kv)
+    if idx_out is None:
+        idx_out = _empty((n_seq, n_kv, max(keep, 0)), device=weights.device, dtype=torch.int32)
+    else:
+        _device(idx_out, torch.int32, "idx_out")
+        if idx_out.shape != (n_seq, n_kv, keep) or not idx_out.is_contiguous():
+            raise ValueError("idx_out must be contiguous n_seq x n_kv x keep")
+    if count_out is None:
+        count_out = _empty((n_seq,), device=weights.device, dtype=torch.int32)
+    count_at = _per_seq(count_out, n_seq, "count_out")
+    st = _L().crvq_cache_select(_addressof(wc), lens_at, n_seq, n_kv, keep, first, recent, idx_out.data_ptr(), count_at,
+                                None if weights_out is None else _addressof(oc),
+                                _raw_stream(weights.get_device()) if stream is None else
+                                _foreign(stream, weights, lens, weights_out, idx_out, count_out))
+    if st:
+        _check(st)
+    return idx_out, count_out
+
+
+def crvq_cache_keep(cache, idx, count, start=None, out=None, stream=None):
+    """Moves tokens idx[b, h, :count[b]] (or idx[b, :count[b]], the same for all heads) of every sequence of the cache to
+    the places start[b] (0 unless given) onwards of out: the cache itself unless given (then tokens only move towards the
+    front), or one with other pages. Set out.lens to start + count after it."""
+    out = cache if out is None else out
+    _device(idx, torch.int32, "idx")
+    shape, stride = idx.shape, idx.stride()
+    if (len(shape) not in (2, 3) or shape[0] != cache.n_seq or (len(shape) == 3 and shape[1] != cache.n_kv) or
+            (shape[-1] > 1 and stride[-1] != 1)):
+        raise ValueError("idx must be n_seq x n_kv x columns, or n_seq x columns, with unit stride in the last dimension")
+    by_head = 0 if len(shape) == 2 else max(shape[2], 1) if shape[1] == 1 else stride[1]
+    st = _L().crvq_cache_keep(cache._addr, idx.data_ptr(), stride[0], by_head, shape[-1],
+                              _per_seq(count, cache.n_seq, "count"),
+                              None if start is None else _per_seq(start, cache.n_seq, "start"), out._addr,
+                              _raw_stream(cache.index) if stream is None else
+                              _foreign(stream, idx, count, start, *cache.tensors(), *out.tensors()))
+    if st:
+        _check(st)
+    return out
+
+
 class Q4Matrix:
     """A matrix with 4-bit weights (crvq_q4_matrix): codes [M x ceil(N / 2)] uint8 (two per byte, the even
     column in the low bits), scales [M x ceil(N / group)] bfloat16, zeros of that shape, uint8, or None (8).
