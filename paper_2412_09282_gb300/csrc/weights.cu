@@ -133,7 +133,7 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
         }
         if (lane == 0) {
           const int pos = held + j;
-          col_s[col] = make_float4(none ? 0.f : back * a.scale, none ? -INFINITY : -lse * kLog2e,
+          col_s[col] = make_float4(none ? 0.f : back * w.scale, none ? -INFINITY : -lse,
                                    __int_as_float(a.window > 0 ? max(0, pos - a.window + 1) : 0),
                                    __int_as_float(a.causal ? min(len, pos + 1) : len));
         }
@@ -190,21 +190,29 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) sum[b][0] = sum[b][1] = 0.f;
         for (int g = 0; g < groups; ++g) {
+          // 64 channels' products at a time, second operands' apart, are added up in fp32: a tensor core's sums are cut off
+          // towards zero where they are long or a small product meets a large sum (16 of both kinds in a chain: weights
+          // 1e-6 too small on average; so, 2e-7)
           float s[NB][4];
-#pragma unroll
-          for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
 #pragma unroll
           for (int j = 0; j < D / 64; ++j)
 #pragma unroll
-            for (int z = 0; z < (SPLIT ? 2 : 1); ++z) {
+            for (int z = SPLIT ? 1 : 0; z >= 0; --z) {
               const uint4* p = reinterpret_cast<const uint4*>(q_s + ((size_t)z * w.chunk + 8 * g + gid) * S::kQRow + 64 * j + 16 * tig);
               const uint4 x = p[0], y = p[1];
+              float part[NB][4];
+#pragma unroll
+              for (int b = 0; b < NB; ++b) part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
 #pragma unroll
               for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
-                  mma_f16(s[b], k[b][4 * j + e][0], k[b][4 * j + e][1], k[b][4 * j + e][2], k[b][4 * j + e][3],
+                  mma_f16(part[b], k[b][4 * j + e][0], k[b][4 * j + e][1], k[b][4 * j + e][2], k[b][4 * j + e][3],
                           e < 2 ? word(x, 2 * e) : word(y, 2 * e - 4), e < 2 ? word(x, 2 * e + 1) : word(y, 2 * e - 3));
+#pragma unroll
+              for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][e] = j == 0 && z == (SPLIT ? 1 : 0) ? part[b][e] : s[b][e] + part[b][e];
             }
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
@@ -212,7 +220,7 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
               const float f = c.x * sk[b];
-              float p0 = pow2(fmaf(s[b][e], f, c.y)), p1 = pow2(fmaf(s[b][e + 2], f, c.y));
+              float p0 = pow2(fmaf(s[b][e], f, c.y) * kLog2e), p1 = pow2(fmaf(s[b][e + 2], f, c.y) * kLog2e);
               if (!whole) {
                 const int t0 = tok + b * kCacheBlock + gid, kb = __float_as_int(c.z), ke = __float_as_int(c.w);
                 if (t0 < kb || t0 >= ke) p0 = 0.f;
@@ -293,6 +301,7 @@ crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_t
   w.out_head = out->ld_head;
   w.width = out->width;
   w.decay = decay;
+  w.scale = scale;
   const int D = cache->head_dim;
   if (D == 64) return pick<64>(w, cache->format, stream);
   if (D == 128) return pick<128>(w, cache->format, stream);

@@ -13,6 +13,7 @@ struct WeightArgs {
   int64_t before_seq, before_head, out_seq, out_head;  // strides
   int64_t width;        // places in a row of before and out
   float decay;
+  float scale;          // (a's is in log2: there the difference of score and lse would be rounded at their size)
   int chunk;            // columns at a time
 };
 
