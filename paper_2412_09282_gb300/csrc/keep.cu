@@ -35,17 +35,27 @@ template <int D>
 struct KeepShape {
   static constexpr int kRow = D / 16;                     // threads per token
   static constexpr int kSlots = kKeepThreads / kRow;      // tokens at a time: 64, 32 or 16
-  static constexpr int kTimes = 4;
-  static constexpr int kTokens = kSlots * kTimes;         // of a tile
+  static constexpr int kTimes = D == 64 ? 4 : 8;
+  static constexpr int kTokens = kSlots * kTimes;         // of a tile: 256, 256 or 128
+  static_assert(kTokens <= kKeepThreads, "a thread looks up one token");
 };
 
+// Where a tile's tokens lie and go (dst -1: nowhere).
+template <int D>
+struct KeepTile {
+  static constexpr int kTokens = KeepShape<D>::kTokens;
+  int64_t src[kTokens];                   // of a token's codes (-1: none)
+  int64_t dst[kTokens / kCacheBlock], dst_scale[kTokens / kCacheBlock];
+  float scale[kTokens];
+  bool old[kTokens];                      // it lies in the destination already
+};
+
+// Looking a token up takes three loads one after another (its place, its page, its scale), so a tile's begin three rounds ahead:
+// in every round one step of three tiles is on its way beside the present tile's codes.
 template <int D, int FMT, bool IN_PLACE>
-__global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ KeepArgs a) {
+__global__ void __launch_bounds__(kKeepThreads, 3) keep_kernel(const __grid_constant__ KeepArgs a) {
   using S = KeepShape<D>;
-  __shared__ int64_t src_s[S::kTokens];                   // codes' places in the source (-1: none), dst per block
-  __shared__ int64_t dst_s[S::kTokens / kCacheBlock], dst_scale_s[S::kTokens / kCacheBlock];
-  __shared__ float scale_s[S::kTokens];
-  __shared__ bool old_s[S::kTokens];
+  __shared__ KeepTile<D> tile_s[2];
   pdl_wait();
   const int tid = threadIdx.x;
   const int unit = blockIdx.x / a.tiles, rank = blockIdx.x - unit * a.tiles;
@@ -61,7 +71,8 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
   const int len = seq_len(a.from, b, a.err);
   const int base = start / kCacheBlock * kCacheBlock, end = start + n;
   const int n_tiles = (end - base + S::kTokens - 1) / S::kTokens;
-  const int rounds = IN_PLACE ? (n_tiles + a.tiles - 1) / a.tiles : (rank < n_tiles ? 1 : 0);
+  // (in place, every CTA of a cluster takes part in every round)
+  const int rounds = IN_PLACE ? (n_tiles + a.tiles - 1) / a.tiles : max(0, n_tiles - rank + a.tiles - 1) / a.tiles;
   const int32_t* idx = a.idx + b * a.ld_seq + h * a.ld_head;
   const uint8_t* from = is_key ? a.from.K : a.from.V;
   uint8_t* to = is_key ? a.to.K : a.to.V;
@@ -69,77 +80,108 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
   float* to_scale = is_key ? a.to.ks : a.to.vs;
   const int from_blocks = (unsigned)a.from.page / kCacheBlock, to_blocks = (unsigned)a.to.page / kCacheBlock;
   const int col = tid % S::kRow, slot = tid / S::kRow;
+  auto place0 = [&](int round) { return base + (rank + round * a.tiles) * S::kTokens; };
+  // the place that this thread looks up for a round; `end` where there is none
+  auto place = [&](int round) { return tid < S::kTokens && round < rounds ? min(place0(round) + tid, end) : end; };
 
-  for (int round = 0; round < rounds; ++round) {
-    const int p0 = base + (rank + round * a.tiles) * S::kTokens;
-    __syncthreads();  // the previous tile's places have been read
-    // places: p0 + tid, for the tile's first threads
-    if (tid < S::kTokens) {
-      const int p = p0 + tid;
-      int64_t src = -1, dst = -1;
-      float scale = 0.f;
-      bool old = false;
-      if (p < end) {
-        const int to_entry = a.to_page.div(p), to_in = p - to_entry * a.to.page;
-        const int64_t to_id = seq_page(a.to, b, to_entry, a.err);
-        if (to_id >= 0) {
-          dst = to_id * a.to.page_stride + ((int64_t)h * a.to.page + to_in) * D;
-          const int64_t at_scale = (to_id * a.to.n_kv + h) * to_blocks + to_in / kCacheBlock;
-          if (p < start) {
-            old = true;
-            src = dst;
-            scale = to_scale[at_scale];
-          } else {
-            const int t = __ldg(idx + (p - start));
-            if (t < 0 || t >= len || (IN_PLACE && t < p)) {
-              raise_error(a.err, ERRBIT_INDEX);
-            } else {
-              const int entry = a.from_page.div(t), in = t - entry * a.from.page;
-              const int64_t id = seq_page(a.from, b, entry, a.err);
-              if (id >= 0) {
-                src = id * a.from.page_stride + ((int64_t)h * a.from.page + in) * D;
-                scale = from_scale[(id * a.from.n_kv + h) * from_blocks + in / kCacheBlock];
-              }
-            }
-          }
-          if (tid % kCacheBlock == 0) dst_scale_s[tid / kCacheBlock] = at_scale;
-        }
-        if (!IN_PLACE && a.same_pool && to_id >= 0 && p < len && a.from.page == a.to.page &&
-            to_id == seq_page(a.from, b, to_entry, a.err)) {
-          raise_error(a.err, ERRBIT_INDEX);  // (in place, unsaid: the order of reads and writes would be open)
-          dst = -1;
-        }
+  auto find_token = [&](int round) {
+    const int p = place(round);
+    return p >= start && p < end ? __ldg(idx + (p - start)) : 0;
+  };
+  struct Pages {
+    int64_t from, to;
+  };
+  auto find_pages = [&](int round, int t) {
+    const int p = place(round);
+    Pages g{-1, -1};
+    if (p < end) {
+      const int entry = a.to_page.div(p);
+      g.to = seq_page(a.to, b, entry, a.err);
+      if (p >= start) {
+        if (t < 0 || t >= len || (IN_PLACE && t < p))
+          raise_error(a.err, ERRBIT_INDEX);
+        else
+          g.from = seq_page(a.from, b, a.from_page.div(t), a.err);
       }
-      if (tid % kCacheBlock == 0) dst_s[tid / kCacheBlock] = dst;
-      src_s[tid] = src;
-      scale_s[tid] = scale;
-      old_s[tid] = old;
+      if (!IN_PLACE && a.same_pool && g.to >= 0 && p < len && g.to == seq_page(a.from, b, entry, a.err)) {
+        raise_error(a.err, ERRBIT_INDEX);  // (in place, unsaid: the order of reads and writes would be open)
+        g.to = -1;
+      }
     }
-    __syncthreads();
+    return g;
+  };
+  struct Found {
+    int64_t src, dst, at_scale;
+    float scale;
+  };
+  auto find_scale = [&](int round, int t, const Pages& g) {
+    const int p = place(round);
+    Found f{-1, -1, 0, 0.f};
+    if (g.to >= 0) {  // (p < end)
+      const int in = p - a.to_page.div(p) * a.to.page;
+      f.dst = g.to * a.to.page_stride + ((int64_t)h * a.to.page + in) * D;
+      f.at_scale = (g.to * a.to.n_kv + h) * to_blocks + in / kCacheBlock;
+      if (p < start) {
+        f.src = f.dst;
+        f.scale = to_scale[f.at_scale];
+      }
+    }
+    if (g.from >= 0) {
+      const int in = t - a.from_page.div(t) * a.from.page;
+      f.src = g.from * a.from.page_stride + ((int64_t)h * a.from.page + in) * D;
+      f.scale = from_scale[(g.from * a.from.n_kv + h) * from_blocks + in / kCacheBlock];
+    }
+    return f;
+  };
+  auto put = [&](int round, const Found& f) {
+    if (tid >= S::kTokens) return;
+    KeepTile<D>& tile = tile_s[round & 1];
+    if (tid % kCacheBlock == 0) {
+      tile.dst[tid / kCacheBlock] = f.dst;
+      tile.dst_scale[tid / kCacheBlock] = f.at_scale;
+    }
+    tile.src[tid] = f.src;
+    tile.scale[tid] = f.scale;
+    tile.old[tid] = place(round) < start;
+  };
+  int t1 = find_token(0), t2 = find_token(1), t3 = find_token(2);
+  Pages g1 = find_pages(0, t1);
+  Pages g2 = find_pages(1, t2);
+  put(0, find_scale(0, t1, g1));
+  t1 = t2;
+  t2 = t3;
+  g1 = g2;  // (t1, g1: the next round's; t2: the one's after that)
+  for (int round = 0; round < rounds; ++round) {
+    __syncthreads();  // this round's places are there, and the ones before have been read
+    const KeepTile<D>& tile = tile_s[round & 1];
     uint4 codes[S::kTimes];
 #pragma unroll
     for (int u = 0; u < S::kTimes; ++u) {
       const int i = u * S::kSlots + slot;
-      const int64_t src = src_s[i];
+      const int64_t src = tile.src[i];
       codes[u] = make_uint4(0, 0, 0, 0);
-      if (src >= 0) codes[u] = *reinterpret_cast<const uint4*>((old_s[i] ? to : from) + src + 16 * col);
+      if (src >= 0) codes[u] = *reinterpret_cast<const uint4*>((tile.old[i] ? to : from) + src + 16 * col);
     }
+    const Found next = find_scale(round + 1, t1, g1);
+    g2 = find_pages(round + 2, t2);
+    t3 = find_token(round + 3);
     if (IN_PLACE && a.tiles > 1)
       asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     else if (IN_PLACE)
       __syncthreads();
+    const int p0 = place0(round);
 #pragma unroll
     for (int u = 0; u < S::kTimes; ++u) {
       const int i = u * S::kSlots + slot, block = i / kCacheBlock;
-      if (p0 + i >= end || dst_s[block] < 0) continue;
+      if (p0 + i >= end || tile.dst[block] < 0) continue;
       float s = 0.f;
-      const float4* all = reinterpret_cast<const float4*>(scale_s + block * kCacheBlock);
+      const float4* all = reinterpret_cast<const float4*>(tile.scale + block * kCacheBlock);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float4 x = all[e];
         s = fmaxf(s, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
       }
-      const float mine = scale_s[i];
+      const float mine = tile.scale[i];
       uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
       if (mine != s || !(s > 0.f)) {
         const float ratio = s > 0.f ? __fdiv_rn(mine, s) : 0.f;
@@ -148,13 +190,17 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
           float v[4];
           decode4<FMT>(w[e], v);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = src_s[i] >= 0 && ratio > 0.f ? __fmul_rn(v[k], ratio) : 0.f;
+          for (int k = 0; k < 4; ++k) v[k] = ratio > 0.f ? __fmul_rn(v[k], ratio) : 0.f;  // (a token that is none has scale 0)
           w[e] = encode4<FMT, false>(v);
         }
       }
-      *reinterpret_cast<uint4*>(to + dst_s[block] + (i % kCacheBlock) * D + 16 * col) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (i % kCacheBlock == 0 && col == 0) to_scale[dst_scale_s[block]] = s;
+      *reinterpret_cast<uint4*>(to + tile.dst[block] + (i % kCacheBlock) * D + 16 * col) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (i % kCacheBlock == 0 && col == 0) to_scale[tile.dst_scale[block]] = s;
     }
+    put(round + 1, next);
+    t1 = t2;
+    t2 = t3;
+    g1 = g2;
   }
 }
 
@@ -165,7 +211,8 @@ crvq_status launch_keep(KeepArgs& a, bool in_place, cudaStream_t stream) {
   const int64_t units = (int64_t)a.from.n_seq * a.from.n_kv * 2;
   int size = 1;
   while (in_place && size < 8 && size < tiles) size *= 2;
-  a.tiles = in_place ? size : (int)tiles;
+  // into other pages: two waves of CTAs, so that each has tiles to look up while one is on its way
+  a.tiles = in_place ? size : (int)min(tiles, ceil_div((int64_t)6 * sm_count(), units));
   if (units * a.tiles >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many tokens in one call");
   const dim3 grid((unsigned)(units * a.tiles)), threads(kKeepThreads);
   if (!in_place) {

@@ -8,7 +8,8 @@
 // do not depend on timing.
 //   A row is the work of a cluster of 1, 2, 4 or 8 CTAs, each of which holds an equal run of neighbouring tokens in shared
 // memory (it is read from global memory once) and every warp of it an equal run of those: counts over a warp's 32 tokens
-// are ballots. Histograms and counts are joined through the cluster's shared memory: each CTA adds up a slice of the bins.
+// are ballots. Histograms and counts are joined by adding them to every CTA's shared memory: one barrier a digit, and nothing is
+// read across CTAs.
 #include "cache.cuh"
 #include "kernels.h"
 
@@ -18,7 +19,7 @@ namespace {
 
 constexpr int kBins = 2048, kBinRows = kBins / 32;
 constexpr int kMaxWarps = 32;
-constexpr int kStageMax = 48 * 1024;  // weights that a CTA holds in shared memory (more are read again)
+constexpr int kStageMax = 44 * 1024;  // weights that a CTA holds in shared memory (more are read again)
 
 struct SelectArgs {
   const float* w;
@@ -32,32 +33,54 @@ struct SelectArgs {
   unsigned* err;
 };
 
-// Unsigned keys in the order of the weights; -0 is 0, and NaN is above infinity.
+// Unsigned keys in the order of the weights; -0 is 0, and NaN is above infinity. kAlways is above all of them: the first and the
+// most recent tokens are then selected as any others are. 0 is below all: the places behind the last token.
+constexpr uint32_t kAlways = 0xffffffffu, kNan = 0xfffffffeu;
 __device__ __forceinline__ uint32_t order_key(float x) {
-  if (x != x) return 0xffffffffu;
   const uint32_t u = __float_as_uint(x + 0.f);  // (-0 + 0 = 0)
-  return u >> 31 ? ~u : u | 0x80000000u;
+  return x != x ? kNan : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-__device__ __forceinline__ uint32_t load_remote_u32(const uint32_t* p, int rank) {
-  uint32_t at, v;
+// The place of *p in the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t remote(const uint32_t* p, int rank) {
+  uint32_t at;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  return v;
+  return at;
+}
+__device__ __forceinline__ void add_remote(uint32_t at, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+__device__ __forceinline__ void store_remote(uint32_t at, uint32_t v) {
+  asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
 }
 
 struct SelectShared {
-  uint32_t hist[3][kBins];
-  uint32_t rows[3][kBinRows];        // sums of 32 bins
+  uint32_t hist[3][kBins];           // the row's, once every CTA of the cluster has added its own
+  uint32_t mine[kBins];              // this CTA's part of the present one, where the cluster has others
+  uint32_t rows[kBinRows];           // sums of 32 bins
   uint32_t bin, above;               // the threshold's bin, and the keys above it
-  uint32_t total[2];                 // tokens of this CTA that stay for certain; equal to the threshold
+  uint32_t sure[8], equal[8];        // tokens of every CTA that stay for certain; equal to the threshold
   uint32_t warp_sure[kMaxWarps], warp_equal[kMaxWarps];
 };
 
-__global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_constant__ SelectArgs a) {
+// One more key in a bin of the lanes that are `in`. Lanes in the same bin wait for one another; where all are (a row of equal
+// weights) one adds for them.
+__device__ __forceinline__ void count_key(uint32_t* hist, uint32_t bin, bool in) {
+  const unsigned who = __ballot_sync(0xffffffffu, in);
+  if (who == 0) return;
+  const int first = __ffs(who) - 1;
+  const uint32_t b0 = __shfl_sync(0xffffffffu, bin, first);
+  if (__all_sync(0xffffffffu, !in || bin == b0)) {
+    if ((int)(threadIdx.x & 31) == first) atomicAdd(hist + b0, (uint32_t)__popc(who));
+  } else if (in) {
+    atomicAdd(hist + bin, 1u);
+  }
+}
+
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_constant__ SelectArgs a) {
   extern __shared__ __align__(16) char sm[];
   SelectShared& s = *reinterpret_cast<SelectShared*>(sm);
-  float* held = reinterpret_cast<float*>(sm + sizeof(SelectShared));
+  uint32_t* keys = reinterpret_cast<uint32_t*>(sm + sizeof(SelectShared));
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int size = 1 << a.log_cluster, rank = blockIdx.x & (size - 1), row = blockIdx.x >> a.log_cluster;
@@ -68,16 +91,15 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
     else
       asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  for (int i = tid; i < 3 * kBins; i += blockDim.x) (&s.hist[0][0])[i] = 0;
+  for (int i = tid; i < (size > 1 ? 4 : 3) * kBins; i += blockDim.x) (&s.hist[0][0])[i] = 0;
   int len = __ldg(a.lens + b);
   if (len < 0 || len > a.width) {
     raise_error(a.err, ERRBIT_INDEX);
     len = 0;
   }
   const int count = min(len, a.keep);
-  const bool all = len <= a.keep;
-  // tokens [lo, hi) are those between the first and the most recent ones
-  const int lo = all ? len : a.first, hi = all ? len : len - a.recent;
+  const bool find = len > a.keep;  // (else all stay)
+  const int lo = a.first, hi = len - a.recent;  // tokens [lo, hi) are those between the first and the most recent ones
   const float* w = a.w + b * a.w_seq + h * a.w_head;
   // this CTA's tokens, this warp's
   const int per_cta = (int)(((int64_t)len + 32 * size - 1) / (32 * size)) * 32;
@@ -87,8 +109,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
   const bool staged = per_cta <= a.staged;
   __syncthreads();
 
-  uint32_t need = all ? 0u : (uint32_t)(a.keep - a.first - a.recent), threshold = 0xffffffffu;
-  const bool find = need > 0;
+  auto key_of = [&](int t, float x) { return t < lo || t >= hi || !find ? kAlways : order_key(x); };
   constexpr int kBatch = 8;
   for (int t0 = begin; t0 < end; t0 += 32 * kBatch) {
     float x[kBatch];
@@ -100,9 +121,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int t = t0 + 32 * i + lane;
-      if (t >= end) continue;
-      if (staged) held[t - c_begin] = x[i];
-      if (find && t >= lo && t < hi) atomicAdd(&s.hist[0][order_key(x[i]) >> 21], 1u);
+      if (t0 + 32 * i >= end) break;
+      const uint32_t key = t < end ? key_of(t, x[i]) : 0u;
+      if (staged) keys[t - c_begin] = key;
+      if (find) count_key(size > 1 ? s.mine : s.hist[0], key >> 21, t < end);
     }
   }
   // places behind the last token that stays
@@ -114,37 +136,40 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
   for (int t = count + rank * (int)blockDim.x + tid; t < a.keep; t += size * (int)blockDim.x) idx[t] = -1;
   if (h == 0 && rank == 0 && tid == 0) a.count[b] = count;
 
-  auto at = [&](int t) { return staged ? held[t - c_begin] : __ldg(w + t); };
+  // the keys of 32 tokens, a lane each
+  auto at = [&](int t) { return staged ? keys[t - c_begin] : t < end ? key_of(t, __ldg(w + t)) : 0u; };
+  uint32_t need = (uint32_t)a.keep, threshold = kAlways - 1;  // (all stay for certain)
   if (find) {
     uint32_t prefix = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, digits = pass == 2 ? 10 : 11;
       if (pass > 0)
-        for (int t = max(begin, lo) / 32 * 32 + lane; t < min(end, hi); t += 32) {
-          if (t < begin || t < lo) continue;
-          const uint32_t key = order_key(at(t));
-          if (key >> (shift + digits) == prefix) atomicAdd(&s.hist[pass][key >> shift & (kBins - 1) & ((1 << digits) - 1)], 1u);
+        for (int t0 = begin; t0 < end; t0 += 32) {
+          const uint32_t key = at(t0 + lane);
+          count_key(size > 1 ? s.mine : s.hist[pass], key >> shift & ((1u << digits) - 1u), key >> (shift + digits) == prefix);
         }
-      sync_all();
-      // sums of this CTA's slice of the bins
-      const int rows = kBinRows >> a.log_cluster;
-      for (int r = rank * rows + warp; r < (rank + 1) * rows; r += warps) {
-        uint32_t v = s.hist[pass][32 * r + lane];
-        if (size > 1) {
-          v = 0;
-          for (int c = 0; c < size; ++c) v += load_remote_u32(&s.hist[pass][32 * r + lane], c);
-          s.hist[pass][32 * r + lane] = v;
+      if (size > 1) {  // to everyone
+        if (pass == 0) sync_all();  // (whose counts are zeros by then)
+        else __syncthreads();
+        for (int i = tid; i < kBins; i += blockDim.x) {
+          const uint32_t v = s.mine[i];
+          if (v) {
+            s.mine[i] = 0;
+            for (int c = 0; c < size; ++c) add_remote(remote(&s.hist[pass][i], c), v);
+          }
         }
-        v = __reduce_add_sync(0xffffffffu, v);
-        if (lane == 0) s.rows[pass][r] = v;
       }
       sync_all();
+      for (int r = warp; r < kBinRows; r += warps) {
+        const uint32_t v = __reduce_add_sync(0xffffffffu, s.hist[pass][32 * r + lane]);
+        if (lane == 0) s.rows[r] = v;
+      }
+      __syncthreads();
       if (warp == 0) {
         // from the top: lane i holds rows 63 - 2 i and 62 - 2 i
         const int r1 = kBinRows - 1 - 2 * lane, r0 = r1 - 1;
-        const uint32_t v1 = size > 1 ? load_remote_u32(&s.rows[pass][r1], r1 / rows) : s.rows[pass][r1];
-        const uint32_t v0 = size > 1 ? load_remote_u32(&s.rows[pass][r0], r0 / rows) : s.rows[pass][r0];
+        const uint32_t v1 = s.rows[r1], v0 = s.rows[r0];
         uint32_t sum = v1 + v0;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -156,8 +181,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
         const bool second = above + v1 < need;
         const int r = __shfl_sync(0xffffffffu, second ? r0 : r1, hit);
         above = __shfl_sync(0xffffffffu, second ? above + v1 : above, hit);
-        const uint32_t* bins = &s.hist[pass][32 * r + 31 - lane];
-        const uint32_t v = size > 1 ? load_remote_u32(bins, r / rows) : *bins;
+        const uint32_t v = s.hist[pass][32 * r + 31 - lane];
         sum = v;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -177,24 +201,16 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
     threshold = prefix;
   }
 
+  if (size > 1 && !find) sync_all();  // (every CTA is there)
   // this warp's tokens that stay for certain, and those at the threshold
   uint32_t sure = 0, equal = 0;
-  auto look = [&](int t, bool* is_sure, bool* is_equal) {
-    *is_sure = *is_equal = false;
-    if (t >= end) return 0.f;
-    const float x = at(t);
-    const uint32_t key = order_key(x);
-    const bool between = t >= lo && t < hi;
-    *is_sure = !between || (find && key > threshold);
-    *is_equal = between && find && key == threshold;
-    return x;
-  };
   for (int t0 = begin; t0 < end; t0 += 32) {
-    bool is_sure, is_equal;
-    look(t0 + lane, &is_sure, &is_equal);
-    sure += __popc(__ballot_sync(0xffffffffu, is_sure));
-    equal += __popc(__ballot_sync(0xffffffffu, is_equal));
+    const uint32_t key = at(t0 + lane);
+    sure += key > threshold;
+    equal += key == threshold;
   }
+  sure = __reduce_add_sync(0xffffffffu, sure);
+  equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) {
     s.warp_sure[warp] = sure;
     s.warp_equal[warp] = equal;
@@ -215,34 +231,37 @@ __global__ void __launch_bounds__(32 * kMaxWarps) select_kernel(const __grid_con
       s.warp_sure[lane] = vs - ms;
       s.warp_equal[lane] = ve - me;
     }
-    if (lane == 31) {
-      s.total[0] = vs;
-      s.total[1] = ve;
+    vs = __shfl_sync(0xffffffffu, vs, 31);
+    ve = __shfl_sync(0xffffffffu, ve, 31);
+    if (size > 1 && lane < size) {  // to everyone; the last word between the CTAs
+      store_remote(remote(&s.sure[rank], lane), vs);
+      store_remote(remote(&s.equal[rank], lane), ve);
     }
   }
   sync_all();
   sure = s.warp_sure[warp];
   equal = s.warp_equal[warp];
   for (int c = 0; c < rank; ++c) {
-    sure += load_remote_u32(&s.total[0], c);
-    equal += load_remote_u32(&s.total[1], c);
+    sure += s.sure[c];
+    equal += s.equal[c];
   }
   float* out = a.w_out ? a.w_out + b * a.out_seq + h * a.out_head : nullptr;
+  const unsigned before = (1u << lane) - 1u;
   for (int t0 = begin; t0 < end; t0 += 32) {
     const int t = t0 + lane;
-    bool is_sure, is_equal;
-    const float x = look(t, &is_sure, &is_equal);
-    const unsigned ms = __ballot_sync(0xffffffffu, is_sure), me = __ballot_sync(0xffffffffu, is_equal), before = (1u << lane) - 1u;
+    const uint32_t key = at(t);
+    const bool is_sure = key > threshold, is_equal = key == threshold;
+    const unsigned ms = __ballot_sync(0xffffffffu, is_sure), me = __ballot_sync(0xffffffffu, is_equal);
+    if ((ms | me) == 0) continue;
     const uint32_t my_equal = equal + __popc(me & before);
     const uint32_t place = sure + __popc(ms & before) + min(my_equal, need);
     if ((is_sure || (is_equal && my_equal < need)) && place < (uint32_t)count) {
       idx[place] = t;
-      if (out) out[place] = x;
+      if (out) out[place] = __ldg(w + t);
     }
     sure += __popc(ms);
     equal += __popc(me);
   }
-  if (size > 1) sync_all();  // (no CTA leaves while its memory is read)
 }
 
 crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t n_seq, int32_t n_kv, int32_t keep,
