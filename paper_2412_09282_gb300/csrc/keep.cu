@@ -44,10 +44,10 @@ struct KeepShape {
 template <int D>
 struct KeepTile {
   static constexpr int kTokens = KeepShape<D>::kTokens;
-  int64_t src[kTokens];                   // of a token's codes (-1: none)
+  const uint8_t* src[kTokens];            // a token's codes, or null
   int64_t dst[kTokens / kCacheBlock], dst_scale[kTokens / kCacheBlock];
-  float scale[kTokens];
-  bool old[kTokens];                      // it lies in the destination already
+  float ratio[kTokens];                   // its scale / its new block's
+  float scale[kTokens / kCacheBlock];
 };
 
 // Looking a token up takes three loads one after another (its place, its page, its scale), so a tile's begin three rounds ahead:
@@ -111,38 +111,42 @@ __global__ void __launch_bounds__(kKeepThreads, 3) keep_kernel(const __grid_cons
     return g;
   };
   struct Found {
-    int64_t src, dst, at_scale;
+    const uint8_t* src;
+    int64_t dst, at_scale;
     float scale;
   };
   auto find_scale = [&](int round, int t, const Pages& g) {
     const int p = place(round);
-    Found f{-1, -1, 0, 0.f};
+    Found f{nullptr, -1, 0, 0.f};
     if (g.to >= 0) {  // (p < end)
       const int in = p - a.to_page.div(p) * a.to.page;
       f.dst = g.to * a.to.page_stride + ((int64_t)h * a.to.page + in) * D;
       f.at_scale = (g.to * a.to.n_kv + h) * to_blocks + in / kCacheBlock;
       if (p < start) {
-        f.src = f.dst;
+        f.src = to + f.dst;
         f.scale = to_scale[f.at_scale];
       }
     }
     if (g.from >= 0) {
       const int in = t - a.from_page.div(t) * a.from.page;
-      f.src = g.from * a.from.page_stride + ((int64_t)h * a.from.page + in) * D;
+      f.src = from + g.from * a.from.page_stride + ((int64_t)h * a.from.page + in) * D;
       f.scale = from_scale[(g.from * a.from.n_kv + h) * from_blocks + in / kCacheBlock];
     }
     return f;
   };
   auto put = [&](int round, const Found& f) {
-    if (tid >= S::kTokens) return;
+    if (tid >= S::kTokens) return;  // (whole warps)
     KeepTile<D>& tile = tile_s[round & 1];
+    float s = f.scale;  // of a block, 16 lanes
+#pragma unroll
+    for (int d = kCacheBlock / 2; d > 0; d >>= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, d));
     if (tid % kCacheBlock == 0) {
       tile.dst[tid / kCacheBlock] = f.dst;
       tile.dst_scale[tid / kCacheBlock] = f.at_scale;
+      tile.scale[tid / kCacheBlock] = s;
     }
     tile.src[tid] = f.src;
-    tile.scale[tid] = f.scale;
-    tile.old[tid] = place(round) < start;
+    tile.ratio[tid] = s > 0.f ? __fdiv_rn(f.scale, s) : 0.f;
   };
   int t1 = find_token(0), t2 = find_token(1), t3 = find_token(2);
   Pages g1 = find_pages(0, t1);
@@ -158,9 +162,9 @@ __global__ void __launch_bounds__(kKeepThreads, 3) keep_kernel(const __grid_cons
 #pragma unroll
     for (int u = 0; u < S::kTimes; ++u) {
       const int i = u * S::kSlots + slot;
-      const int64_t src = tile.src[i];
+      const uint8_t* src = tile.src[i];
       codes[u] = make_uint4(0, 0, 0, 0);
-      if (src >= 0) codes[u] = *reinterpret_cast<const uint4*>((tile.old[i] ? to : from) + src + 16 * col);
+      if (src) codes[u] = *reinterpret_cast<const uint4*>(src + 16 * col);
     }
     const Found next = find_scale(round + 1, t1, g1);
     g2 = find_pages(round + 2, t2);
@@ -174,28 +178,28 @@ __global__ void __launch_bounds__(kKeepThreads, 3) keep_kernel(const __grid_cons
     for (int u = 0; u < S::kTimes; ++u) {
       const int i = u * S::kSlots + slot, block = i / kCacheBlock;
       if (p0 + i >= end || tile.dst[block] < 0) continue;
-      float s = 0.f;
-      const float4* all = reinterpret_cast<const float4*>(tile.scale + block * kCacheBlock);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 x = all[e];
-        s = fmaxf(s, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
-      }
-      const float mine = tile.scale[i];
+      const float ratio = tile.ratio[i];  // (at most 1; 0 for a token that is none)
       uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
-      if (mine != s || !(s > 0.f)) {
-        const float ratio = s > 0.f ? __fdiv_rn(mine, s) : 0.f;
+      if (ratio == 0.f) {
+        w[0] = w[1] = w[2] = w[3] = 0;
+      } else if (ratio != 1.f) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v[4];
-          decode4<FMT>(w[e], v);
+          if constexpr (FMT == CRVQ_KV_INT8) {  // 2^23 + code + 128, less 2^23 + 128: exact, without conversions
+            const uint32_t x = w[e] ^ 0x80808080u;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = ratio > 0.f ? __fmul_rn(v[k], ratio) : 0.f;  // (a token that is none has scale 0)
-          w[e] = encode4<FMT, false>(v);
+            for (int k = 0; k < 4; ++k) v[k] = __fsub_rn(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + k)), 8388736.f);
+          } else {
+            decode4<FMT>(w[e], v);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = __fmul_rn(v[k], ratio);
+          w[e] = encode4<FMT, true>(v);
         }
       }
       *reinterpret_cast<uint4*>(to + tile.dst[block] + (i % kCacheBlock) * D + 16 * col) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (i % kCacheBlock == 0 && col == 0) to_scale[tile.dst_scale[block]] = s;
+      if (i % kCacheBlock == 0 && col == 0) to_scale[tile.dst_scale[block]] = tile.scale[block];
     }
     put(round + 1, next);
     t1 = t2;

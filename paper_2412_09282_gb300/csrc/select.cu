@@ -1,14 +1,15 @@
 // Which tokens of every (sequence, kv head) stay when a cache is cut down to a budget: the first, the most recent, and of
 // those between them the ones with the largest weights, ties to the lowest place; their places and weights in order.
 //
-// A row's k-th largest weight is found digit by digit (11, 11 and 10 bits, from the top) over keys whose unsigned order
-// is the weights': a histogram of the keys that agree so far, and the bin in which the count from the top passes k. The row
+// A row's k-th largest weight is found digit by digit (11, 7, 7 and 7 bits, from the top) over keys whose unsigned order
+// is the weights': a histogram of the keys that agree so far, and the bin in which the count from the top passes k. (The
+// first digit splits a row's few powers of two. After it every bin would be in use; adding 2048 of them to the other CTAs'
+// takes as long as one more digit.) The row
 // is then gone through once more: a token stays when its key is above the threshold, or equal to it and among the first
 // that are still needed; its new place is the number of such tokens before it. All counts are whole numbers, so results
 // do not depend on timing.
 //   A row is the work of a cluster of 1, 2, 4 or 8 CTAs, each of which holds an equal run of neighbouring tokens in shared
-// memory (it is read from global memory once) and every warp of it an equal run of those: counts over a warp's 32 tokens
-// are ballots. Histograms and counts are joined by adding them to every CTA's shared memory: one barrier a digit, and nothing is
+// memory (it is read from global memory once) and every warp of it an equal run of those, 128 tokens at a time. Histograms and counts are joined by adding them to every CTA's shared memory: one barrier a digit, and nothing is
 // read across CTAs.
 #include "cache.cuh"
 #include "kernels.h"
@@ -17,8 +18,10 @@ namespace crvq {
 
 namespace {
 
-constexpr int kBins = 2048, kBinRows = kBins / 32;
+constexpr int kBins = 2048, kBinRows = kBins / 32;  // of the first digit
+constexpr int kFew = 128;                           // of the others
 constexpr int kMaxWarps = 32;
+constexpr int kStep = 128;  // tokens of a warp at a time, a lane's four neighbours
 constexpr int kStageMax = 44 * 1024;  // weights that a CTA holds in shared memory (more are read again)
 
 struct SelectArgs {
@@ -30,6 +33,7 @@ struct SelectArgs {
   int32_t* count;
   int n_kv, keep, first, recent;
   int log_cluster, staged;  // weights of a CTA in shared memory
+  bool vec;                 // rows of 16-byte groups of weights
   unsigned* err;
 };
 
@@ -40,6 +44,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);  // (-0 + 0 = 0)
   return x != x ? kNan : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+
+__device__ __forceinline__ float weight_of(uint32_t key) { return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key); }
 
 // The place of *p in the shared memory of the cluster's CTA `rank`.
 __device__ __forceinline__ uint32_t remote(const uint32_t* p, int rank) {
@@ -54,27 +60,29 @@ __device__ __forceinline__ void store_remote(uint32_t at, uint32_t v) {
   asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
 }
 
-struct SelectShared {
-  uint32_t hist[3][kBins];           // the row's, once every CTA of the cluster has added its own
-  uint32_t mine[kBins];              // this CTA's part of the present one, where the cluster has others
+struct alignas(16) SelectShared {
+  // the row's counts, once every CTA of the cluster has added its own, and this CTA's (where there are others)
+  uint32_t hist[kBins], few[3][kFew];
+  uint32_t mine[kBins], mine_few[3][kFew];
   uint32_t rows[kBinRows];           // sums of 32 bins
-  uint32_t bin, above;               // the threshold's bin, and the keys above it
   uint32_t sure[8], equal[8];        // tokens of every CTA that stay for certain; equal to the threshold
   uint32_t warp_sure[kMaxWarps], warp_equal[kMaxWarps];
 };
 
-// One more key in a bin of the lanes that are `in`. Lanes in the same bin wait for one another; where all are (a row of equal
-// weights) one adds for them.
-__device__ __forceinline__ void count_key(uint32_t* hist, uint32_t bin, bool in) {
-  const unsigned who = __ballot_sync(0xffffffffu, in);
-  if (who == 0) return;
-  const int first = __ffs(who) - 1;
-  const uint32_t b0 = __shfl_sync(0xffffffffu, bin, first);
-  if (__all_sync(0xffffffffu, !in || bin == b0)) {
-    if ((int)(threadIdx.x & 31) == first) atomicAdd(hist + b0, (uint32_t)__popc(who));
-  } else if (in) {
-    atomicAdd(hist + bin, 1u);
+// Counts a lane's four keys in their bins, those that are `in`. Lanes in the same bin wait for one another; where all keys are (a
+// row of equal weights) one lane adds for them.
+__device__ __forceinline__ void count_keys(uint32_t* hist, const uint32_t bin[4], const bool in[4]) {
+  const uint32_t b0 = __shfl_sync(0xffffffffu, bin[0], 0);
+  bool same = true;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) same = same && in[e] && bin[e] == b0;
+  if (__all_sync(0xffffffffu, same)) {
+    if ((threadIdx.x & 31) == 0) atomicAdd(hist + b0, 128u);
+    return;
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (in[e]) atomicAdd(hist + bin[e], 1u);
 }
 
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_constant__ SelectArgs a) {
@@ -85,13 +93,21 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int size = 1 << a.log_cluster, rank = blockIdx.x & (size - 1), row = blockIdx.x >> a.log_cluster;
   const int b = row / a.n_kv, h = row - b * a.n_kv;
+  auto scan = [&](uint32_t v) {  // sums of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
+    }
+    return v;
+  };
   auto sync_all = [&]() {
     if (size == 1)
       __syncthreads();
     else
       asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  for (int i = tid; i < (size > 1 ? 4 : 3) * kBins; i += blockDim.x) (&s.hist[0][0])[i] = 0;
+  for (int i = tid; i < (size > 1 ? 2 : 1) * (kBins + 3 * kFew); i += blockDim.x) s.hist[i] = 0;
   int len = __ldg(a.lens + b);
   if (len < 0 || len > a.width) {
     raise_error(a.err, ERRBIT_INDEX);
@@ -102,101 +118,141 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   const int lo = a.first, hi = len - a.recent;  // tokens [lo, hi) are those between the first and the most recent ones
   const float* w = a.w + b * a.w_seq + h * a.w_head;
   // this CTA's tokens, this warp's
-  const int per_cta = (int)(((int64_t)len + 32 * size - 1) / (32 * size)) * 32;
+  const int per_cta = (int)(((int64_t)len + kStep * size - 1) / (kStep * size)) * kStep;
   const int c_begin = (int)min((int64_t)len, (int64_t)rank * per_cta), c_end = min(len, c_begin + per_cta);
-  const int per_warp = (c_end - c_begin + 32 * warps - 1) / (32 * warps) * 32;
+  const int per_warp = (c_end - c_begin + kStep * warps - 1) / (kStep * warps) * kStep;
   const int begin = min(c_end, c_begin + warp * per_warp), end = min(c_end, begin + per_warp);
   const bool staged = per_cta <= a.staged;
   __syncthreads();
 
-  auto key_of = [&](int t, float x) { return t < lo || t >= hi || !find ? kAlways : order_key(x); };
-  constexpr int kBatch = 8;
-  for (int t0 = begin; t0 < end; t0 += 32 * kBatch) {
-    float x[kBatch];
+  // keys of the tokens t .. t + 3, 0 behind the last
+  auto load_keys = [&](int t, uint32_t key[4]) {
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.vec && t + 3 < end) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(w + t));
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int t = t0 + 32 * i + lane;
-      x[i] = t < end ? __ldg(w + t) : 0.f;
+      for (int e = 0; e < 4; ++e)
+        if (t + e < end) x[e] = __ldg(w + t + e);
     }
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int t = t0 + 32 * i + lane;
-      if (t0 + 32 * i >= end) break;
-      const uint32_t key = t < end ? key_of(t, x[i]) : 0u;
-      if (staged) keys[t - c_begin] = key;
-      if (find) count_key(size > 1 ? s.mine : s.hist[0], key >> 21, t < end);
+    for (int e = 0; e < 4; ++e) {
+      key[e] = t + e < lo || t + e >= hi || !find ? kAlways : order_key(x[e]);
+      if (t + e >= end) key[e] = 0;
     }
+  };
+  auto at = [&](int t, uint32_t key[4]) {
+    if (staged) {
+      const uint4 v = *reinterpret_cast<const uint4*>(keys + (t - c_begin));
+      key[0] = v.x; key[1] = v.y; key[2] = v.z; key[3] = v.w;
+    } else {
+      load_keys(t, key);
+    }
+  };
+#pragma unroll 4
+  for (int t0 = begin; t0 < end; t0 += kStep) {
+    const int t = t0 + 4 * lane;
+    uint32_t key[4], bin[4];
+    bool in[4];
+    load_keys(t, key);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bin[e] = key[e] >> 21;
+      in[e] = key[e] != 0;
+    }
+    if (staged) *reinterpret_cast<uint4*>(keys + (t - c_begin)) = make_uint4(key[0], key[1], key[2], key[3]);
+    if (find) count_keys(size > 1 ? s.mine : s.hist, bin, in);
   }
   // places behind the last token that stays
   if (a.w_out) {
     float* out = a.w_out + b * a.out_seq + h * a.out_head;
-    for (int64_t t = count + rank * (int)blockDim.x + tid; t < a.out_width; t += size * (int)blockDim.x) out[t] = 0.f;
+    int64_t t = count + rank * (int)blockDim.x + tid;
+    if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0) {  // (up to three before the first group of 16 bytes, and behind the last)
+      const int64_t a0 = (count + 3) / 4, a1 = a.out_width / 4;
+      for (int64_t g = a0 + rank * (int)blockDim.x + tid; g < a1; g += size * (int)blockDim.x)
+        reinterpret_cast<float4*>(out)[g] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (rank == 0 && tid < 4 && count + tid < min(4 * a0, a.out_width)) out[count + tid] = 0.f;
+      t = max(4 * a0, 4 * a1) + (rank == 0 ? tid : a.out_width);
+    }
+    for (; t < a.out_width; t += size * (int)blockDim.x) out[t] = 0.f;
   }
   int32_t* idx = a.idx + (int64_t)row * a.keep;
   for (int t = count + rank * (int)blockDim.x + tid; t < a.keep; t += size * (int)blockDim.x) idx[t] = -1;
   if (h == 0 && rank == 0 && tid == 0) a.count[b] = count;
 
-  // the keys of 32 tokens, a lane each
-  auto at = [&](int t) { return staged ? keys[t - c_begin] : t < end ? key_of(t, __ldg(w + t)) : 0u; };
   uint32_t need = (uint32_t)a.keep, threshold = kAlways - 1;  // (all stay for certain)
   if (find) {
-    uint32_t prefix = 0;
+    if (size > 1) {  // to everyone
+      sync_all();    // (whose counts are zeros by then)
+      for (int i = tid; i < kBins; i += blockDim.x) {
+        const uint32_t v = s.mine[i];
+        if (v)
+          for (int c = 0; c < size; ++c) add_remote(remote(&s.hist[i], c), v);
+      }
+    }
+    sync_all();
+    for (int r = warp; r < kBinRows; r += warps) {
+      const uint32_t v = __reduce_add_sync(0xffffffffu, s.hist[32 * r + lane]);
+      if (lane == 0) s.rows[r] = v;
+    }
+    __syncthreads();
+    // every warp finds the bin: first the row of 32, from the top (lane i holds rows 63 - 2 i and 62 - 2 i)
+    uint32_t prefix;
+    {
+      const int r1 = kBinRows - 1 - 2 * lane, r0 = r1 - 1;
+      const uint32_t v1 = s.rows[r1], v0 = s.rows[r0], sum = scan(v1 + v0);
+      const int hit = __ffs(__ballot_sync(0xffffffffu, sum >= need)) - 1;
+      const uint32_t above = sum - v1 - v0;
+      const bool second = above + v1 < need;
+      const int r = __shfl_sync(0xffffffffu, second ? r0 : r1, hit);
+      need -= __shfl_sync(0xffffffffu, second ? above + v1 : above, hit);
+      const uint32_t v = s.hist[32 * r + 31 - lane], in_row = scan(v);
+      const int at_lane = __ffs(__ballot_sync(0xffffffffu, in_row >= need)) - 1;
+      prefix = 32 * r + 31 - at_lane;
+      need -= __shfl_sync(0xffffffffu, in_row - v, at_lane);
+    }
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, digits = pass == 2 ? 10 : 11;
-      if (pass > 0)
-        for (int t0 = begin; t0 < end; t0 += 32) {
-          const uint32_t key = at(t0 + lane);
-          count_key(size > 1 ? s.mine : s.hist[pass], key >> shift & ((1u << digits) - 1u), key >> (shift + digits) == prefix);
+      const int shift = 14 - 7 * pass;
+      uint32_t* few = size > 1 ? s.mine_few[pass] : s.few[pass];
+      for (int t0 = begin; t0 < end; t0 += kStep) {
+        uint32_t key[4], bin[4];
+        bool in[4];
+        at(t0 + 4 * lane, key);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          in[e] = key[e] >> (shift + 7) == prefix;
+          bin[e] = key[e] >> shift & (kFew - 1);
         }
-      if (size > 1) {  // to everyone
-        if (pass == 0) sync_all();  // (whose counts are zeros by then)
-        else __syncthreads();
-        for (int i = tid; i < kBins; i += blockDim.x) {
-          const uint32_t v = s.mine[i];
-          if (v) {
-            s.mine[i] = 0;
-            for (int c = 0; c < size; ++c) add_remote(remote(&s.hist[pass][i], c), v);
-          }
+        if (__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) count_keys(few, bin, in);
+      }
+      if (size > 1) {
+        __syncthreads();
+        for (int i = tid; i < kFew * size; i += blockDim.x) {
+          const uint32_t v = few[i % kFew];
+          if (v) add_remote(remote(&s.few[pass][i % kFew], i / kFew), v);
         }
       }
       sync_all();
-      for (int r = warp; r < kBinRows; r += warps) {
-        const uint32_t v = __reduce_add_sync(0xffffffffu, s.hist[pass][32 * r + lane]);
-        if (lane == 0) s.rows[r] = v;
-      }
-      __syncthreads();
-      if (warp == 0) {
-        // from the top: lane i holds rows 63 - 2 i and 62 - 2 i
-        const int r1 = kBinRows - 1 - 2 * lane, r0 = r1 - 1;
-        const uint32_t v1 = s.rows[r1], v0 = s.rows[r0];
-        uint32_t sum = v1 + v0;
+      // lane i holds bins 127 - 4 i .. 124 - 4 i
+      const uint4 v = *reinterpret_cast<const uint4*>(&s.few[pass][kFew - 4 - 4 * lane]);
+      const uint32_t mine = v.x + v.y + v.z + v.w, sum = scan(mine);
+      const int hit = __ffs(__ballot_sync(0xffffffffu, sum >= need)) - 1;
+      uint32_t above = sum - mine;
+      uint32_t bin = kFew - 1 - 4 * lane;
+      const uint32_t from_top[3] = {v.w, v.z, v.y};
+      bool done = false;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const uint32_t o = __shfl_up_sync(0xffffffffu, sum, d);
-          if (lane >= d) sum += o;
-        }
-        const int hit = __ffs(__ballot_sync(0xffffffffu, sum >= need)) - 1;
-        uint32_t above = sum - v1 - v0;
-        const bool second = above + v1 < need;
-        const int r = __shfl_sync(0xffffffffu, second ? r0 : r1, hit);
-        above = __shfl_sync(0xffffffffu, second ? above + v1 : above, hit);
-        const uint32_t v = s.hist[pass][32 * r + 31 - lane];
-        sum = v;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const uint32_t o = __shfl_up_sync(0xffffffffu, sum, d);
-          if (lane >= d) sum += o;
-        }
-        const int in_row = __ffs(__ballot_sync(0xffffffffu, above + sum >= need)) - 1;
-        if (lane == in_row) {
-          s.bin = 32 * r + 31 - lane;
-          s.above = above + sum - v;
+      for (int e = 0; e < 3; ++e) {
+        done = done || above + from_top[e] >= need;
+        if (!done) {
+          above += from_top[e];
+          --bin;
         }
       }
-      __syncthreads();
-      prefix = prefix << digits | s.bin;
-      need -= s.above;
+      prefix = prefix << 7 | __shfl_sync(0xffffffffu, bin, hit);
+      need -= __shfl_sync(0xffffffffu, above, hit);
     }
     threshold = prefix;
   }
@@ -204,10 +260,14 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   if (size > 1 && !find) sync_all();  // (every CTA is there)
   // this warp's tokens that stay for certain, and those at the threshold
   uint32_t sure = 0, equal = 0;
-  for (int t0 = begin; t0 < end; t0 += 32) {
-    const uint32_t key = at(t0 + lane);
-    sure += key > threshold;
-    equal += key == threshold;
+  for (int t0 = begin; t0 < end; t0 += kStep) {
+    uint32_t key[4];
+    at(t0 + 4 * lane, key);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sure += key[e] > threshold;
+      equal += key[e] == threshold;
+    }
   }
   sure = __reduce_add_sync(0xffffffffu, sure);
   equal = __reduce_add_sync(0xffffffffu, equal);
@@ -217,16 +277,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   }
   __syncthreads();
   if (warp == 0) {
-    uint32_t vs = lane < warps ? s.warp_sure[lane] : 0u, ve = lane < warps ? s.warp_equal[lane] : 0u;
-    const uint32_t ms = vs, me = ve;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint32_t os = __shfl_up_sync(0xffffffffu, vs, d), oe = __shfl_up_sync(0xffffffffu, ve, d);
-      if (lane >= d) {
-        vs += os;
-        ve += oe;
-      }
-    }
+    const uint32_t ms = lane < warps ? s.warp_sure[lane] : 0u, me = lane < warps ? s.warp_equal[lane] : 0u;
+    uint32_t vs = scan(ms), ve = scan(me);
     if (lane < warps) {
       s.warp_sure[lane] = vs - ms;
       s.warp_equal[lane] = ve - me;
@@ -246,21 +298,29 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
     equal += s.equal[c];
   }
   float* out = a.w_out ? a.w_out + b * a.out_seq + h * a.out_head : nullptr;
-  const unsigned before = (1u << lane) - 1u;
-  for (int t0 = begin; t0 < end; t0 += 32) {
-    const int t = t0 + lane;
-    const uint32_t key = at(t);
-    const bool is_sure = key > threshold, is_equal = key == threshold;
-    const unsigned ms = __ballot_sync(0xffffffffu, is_sure), me = __ballot_sync(0xffffffffu, is_equal);
-    if ((ms | me) == 0) continue;
-    const uint32_t my_equal = equal + __popc(me & before);
-    const uint32_t place = sure + __popc(ms & before) + min(my_equal, need);
-    if ((is_sure || (is_equal && my_equal < need)) && place < (uint32_t)count) {
-      idx[place] = t;
-      if (out) out[place] = __ldg(w + t);
+  for (int t0 = begin; t0 < end; t0 += kStep) {
+    const int t = t0 + 4 * lane;
+    uint32_t key[4], n = 0;  // (sure ones in the low half, equal ones in the high half)
+    at(t, key);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) n += (key[e] > threshold ? 1u : 0u) + (key[e] == threshold ? 1u << 16 : 0u);
+    if (!__any_sync(0xffffffffu, n != 0)) continue;
+    uint32_t sum = scan(n);
+    uint32_t my_sure = sure + ((sum - n) & 0xffffu), my_equal = equal + ((sum - n) >> 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool is_sure = key[e] > threshold, is_equal = key[e] == threshold;
+      const uint32_t place = my_sure + min(my_equal, need);
+      if ((is_sure || (is_equal && my_equal < need)) && place < (uint32_t)count) {
+        idx[place] = t + e;
+        if (out) out[place] = key[e] < kNan ? weight_of(key[e]) : __ldg(w + t + e);
+      }
+      my_sure += is_sure;
+      my_equal += is_equal;
     }
-    sure += __popc(ms);
-    equal += __popc(me);
+    sum = __shfl_sync(0xffffffffu, sum, 31);
+    sure += sum & 0xffffu;
+    equal += sum >> 16;
   }
 }
 
@@ -291,6 +351,7 @@ crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t 
   a.w_seq = weights->ld_seq;
   a.w_head = weights->ld_head;
   a.width = weights->width;
+  a.vec = ((uintptr_t)a.w & 15u) == 0 && (n_seq == 1 || a.w_seq % 4 == 0) && (n_kv == 1 || a.w_head % 4 == 0);
   a.lens = lens;
   a.idx = idx;
   a.count = count;
@@ -306,7 +367,7 @@ crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t 
     ++a.log_cluster;
   }
   if (units * size >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many sequences and heads in one call");
-  const int64_t per_cta = ceil_div(a.width, 32 * size) * 32;
+  const int64_t per_cta = ceil_div(a.width, kStep * size) * kStep;
   const int threads = 32 * (int)min((int64_t)kMaxWarps, max((int64_t)4, ceil_div(per_cta, 128)));
   a.staged = (int)min(per_cta, (int64_t)kStageMax);
   const size_t smem = sizeof(SelectShared) + (size_t)a.staged * sizeof(float);
