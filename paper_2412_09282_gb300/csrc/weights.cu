@@ -10,6 +10,7 @@
 // channels), turns their codes into operands once and goes over all columns with them; up to `chunk` columns' queries lie
 // in shared memory as fp16 relative to a power of two each (two operands from fp32). Blocks are copied ahead into a ring
 // per warp, four steps deep: only keys are read, half of what attention reads.
+#include "attend_mma.cuh"
 #include "weights.cuh"
 
 namespace crvq {
@@ -267,6 +268,9 @@ crvq_status launch(WeightArgs& w, cudaStream_t stream) {
   return CRVQ_OK;
 }
 
+// Columns per sequence, on average, from which tokens are the rows of tcgen05 tiles (weights_tc.cu).
+constexpr int64_t kManyColumns = 64;
+
 template <int D>
 crvq_status pick(WeightArgs& w, int format, cudaStream_t stream) {
   const bool split = w.a.q.type == CRVQ_F32;
@@ -303,6 +307,8 @@ crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_t
   w.decay = decay;
   w.scale = scale;
   const int D = cache->head_dim;
+  if (D != 256 && w.a.q.type != CRVQ_F32 && n_tok * w.a.group >= kManyColumns * (int64_t)w.a.c.n_seq)
+    return launch_weights_many(w, D, cache->format, stream);
   if (D == 64) return pick<64>(w, cache->format, stream);
   if (D == 128) return pick<128>(w, cache->format, stream);
   return pick<256>(w, cache->format, stream);

@@ -1,7 +1,7 @@
 // How much attention cached tokens get (see crvq_cache_weights in crvq.h): arguments and what its kernels share.
 #pragma once
 
-#include "attend_mma.cuh"
+#include "attend.cuh"
 
 namespace crvq {
 
@@ -16,6 +16,9 @@ struct WeightArgs {
   float scale;          // (a's is in log2: there the difference of score and lse would be rounded at their size)
   int chunk;            // columns at a time
 };
+
+// Many columns per sequence (weights_tc.cu): 16-bit queries, 64 or 128 channels.
+crvq_status launch_weights_many(WeightArgs& w, int D, int format, cudaStream_t stream);
 
 namespace {
 

@@ -1,0 +1,355 @@
+// Accumulated attention weights for many queries per sequence (see weights.cu for the formula), on tcgen05.
+//
+// S^T (128 tokens x up to 256 columns) = K Q^T: tokens are the lanes of tensor memory, so a thread has one token's scores, and
+// its sum over the columns is its own: no maxima, no shuffles. All columns' queries (512 at a time, as fp16 relative to a power
+// of two each) lie in shared memory while the tiles of a (sequence, kv head) pass.
+// Two groups of four warps take every other tile, each with its own half of tensor memory and its own issuing warp; four warps
+// turn codes into fp16 operands (exact). While one group's exponentials run, the other's products do.
+// Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; every token is one thread's.
+#include "attend_tc.cuh"
+#include "weights.cuh"
+
+namespace crvq {
+
+namespace {
+
+constexpr int kMostCols = 512, kHalfCols = 256;
+constexpr int kWtThreads = 14 * 32;
+
+template <int D>
+struct WtShape {
+  static constexpr int kQ = kMostCols * D * 2;
+  static constexpr int kSide = kKeys * D * 2;
+  static constexpr size_t kSmem = kQ + 2 * kSide + kMostCols * 16;
+};
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_constant__ WeightArgs w) {
+  using S = WtShape<D>;
+  const AttendArgs& a = w.a;
+  extern __shared__ __align__(128) char sm[];
+  __shared__ __align__(8) uint64_t k_full[2], k_empty[2], s_full[2], s_empty[2], q_full, q_read, all_done[2];
+  __shared__ float sk_s[2][8];
+  __shared__ int live_s[2][8];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int dead_s;
+  volatile int* dead = &dead_s;
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const Line<D, kAllColumns> line(a);
+  const int shares = (int)min((int64_t)a.shares, line.total);
+  int64_t at = 0, at_end = 0;
+  if ((int)blockIdx.x < shares) {
+    at = share_begin(line.total, blockIdx.x, shares);
+    at_end = share_begin(line.total, blockIdx.x + 1, shares);
+  }
+  char* q_sm = sm;
+  char* k_sm = sm + S::kQ;
+  float* f_s = reinterpret_cast<float*>(k_sm + 2 * S::kSide);  // [kMostCols] factors of the scores, -lse, first, last + 1 key seen
+  float* l_s = f_s + kMostCols;
+  int* kb_s = reinterpret_cast<int*>(l_s + kMostCols);
+  int* ke_s = kb_s + kMostCols;
+  if (warp == 12) tc::tmem_alloc(&tmem_slot, 2 * kHalfCols);
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(tc::smem_u32(&k_full[i]), 128);
+      tc::mbar_init(tc::smem_u32(&k_empty[i]), 1 + 4);  // the products, and the group's warps (scales)
+      tc::mbar_init(tc::smem_u32(&s_full[i]), 1);
+      tc::mbar_init(tc::smem_u32(&s_empty[i]), 128);
+      tc::mbar_init(tc::smem_u32(&all_done[i]), 1);
+    }
+    tc::mbar_init(tc::smem_u32(&q_full), 256);
+    tc::mbar_init(tc::smem_u32(&q_read), 256);
+    dead_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  Unit u;
+  int n_tiles = 0;      // of the part
+  int64_t cols = 0;
+  auto next_part = [&]() {
+    while (at < at_end) {
+      u = line.locate(a, at);
+      const int64_t tile0 = u.begin + kStart, unit_end = tile0 + u.s.tiles;
+      const int t_end = (int)max((int64_t)0, min(unit_end, at_end) - tile0);
+      at = min(unit_end, at_end);
+      n_tiles = t_end - u.tile;
+      cols = (int64_t)u.s.n * a.group;
+      if (n_tiles > 0) return true;
+    }
+    return false;
+  };
+  bool ok = true;
+  uint32_t tile_no = 0, q_no = 0;  // tiles, and fillings of Q's memory, of this share
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && wait_for(bar, parity, dead, a.err);
+    ok = __all_sync(0xffffffffu, ok);
+    return ok;
+  };
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ exponentials: thread = token of every other tile
+    const int X = warp >> 2, row = tid & (kKeys - 1);
+    const uint32_t s_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + X * kHalfCols;
+    uint32_t s_no = 0;
+    while (ok && next_part()) {
+      const int len = u.s.len, held = len - u.s.n;
+      float* out = w.out + u.b * w.out_seq + u.h * w.out_head;
+      const float* before = w.before ? w.before + u.b * w.before_seq + u.h * w.before_head : nullptr;
+      for (int64_t c0 = 0; c0 < cols && ok; c0 += kMostCols, ++q_no) {
+        const int n_cols = (int)min((int64_t)kMostCols, cols - c0), n_pad = (n_cols + 31) / 32 * 32;
+        // every thread has read what lay there before; products that read it have ended (their scores have been read)
+        if (q_no > 0 && !wait(&q_read, (q_no - 1) & 1)) break;
+        for (int col = tid; col < n_pad; col += 256) {
+          const bool valid = col < n_cols;
+          const int64_t c = c0 + col;
+          const int j = valid ? (int)(c / a.group) : 0, h = u.h * a.group + (valid ? (int)(c % a.group) : 0);
+          const float lse = valid ? __ldg(w.lse + (u.s.first + j) * a.q.heads + h) : INFINITY;
+          const bool none = isinf(lse);  // (such a query has no weights)
+          const int64_t src = (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head;
+          const uint16_t* row_q = static_cast<const uint16_t*>(a.q.data) + src;
+          uint4 raw[D / 8];
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            if (none) {
+              raw[e] = make_uint4(0, 0, 0, 0);
+            } else if (a.vec_q) {
+              raw[e] = __ldg(reinterpret_cast<const uint4*>(row_q) + e);
+            } else {
+              uint32_t x[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = row_q[8 * e + 2 * i] | (uint32_t)row_q[8 * e + 2 * i + 1] << 16;
+              raw[e] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+          }
+          uint32_t top2 = 0;
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            top2 = __vmaxu2(top2, __vmaxu2(raw[e].x & 0x7fff7fffu, raw[e].y & 0x7fff7fffu));
+            top2 = __vmaxu2(top2, __vmaxu2(raw[e].z & 0x7fff7fffu, raw[e].w & 0x7fff7fffu));
+          }
+          const uint32_t top16 = max(top2 & 0xffffu, top2 >> 16);
+          const float top = a.q.type == CRVQ_BF16 ? __uint_as_float(top16 << 16) : __half2float(__ushort_as_half((uint16_t)top16));
+          const uint32_t ex = __float_as_uint(top) >> 23;
+          const bool plain = ex == 0 || ex == 255;
+          const float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
+          const float back = plain ? 1.f : __uint_as_float(ex << 23);
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            const uint32_t x[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float2 v;
+              if (a.q.type == CRVQ_BF16)
+                v = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
+              else
+                v = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
+              o[i] = half2_bits(v.x * inv, v.y * inv);
+            }
+            *reinterpret_cast<uint4*>(q_sm + piece<D>(col, e)) = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+          const int pos = held + j;
+          f_s[col] = none ? 0.f : back * w.scale;
+          l_s[col] = none ? -INFINITY : -lse;
+          kb_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+          ke_s[col] = a.causal ? min(len, pos + 1) : len;
+        }
+        tc::fence_async_smem();
+        tc::mbar_arrive(tc::smem_u32(&q_full));
+        if (!wait(&q_full, q_no & 1)) break;
+        // keys that every column sees (places do not fall from column to column)
+        const int every_b = kb_s[n_cols - 1], every_e = ke_s[0];
+        for (int i = 0; i < n_tiles && ok; ++i, ++tile_no) {
+          if ((int)(tile_no & 1) != X) continue;
+          const int tok = (u.s.lo + u.tile + i) * kKeys, t = tok + row;
+          if (!wait(&k_full[X], (tile_no >> 1) & 1)) break;
+          const float sk = sk_s[X][row >> 4];
+          const bool live = live_s[X][row >> 4] != 0;
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(tc::smem_u32(&k_empty[X]));
+          const bool writes = t < len && t < w.width;
+          float base = 0.f;
+          if (writes) {
+            if (c0 > 0)
+              base = out[t];
+            else if (before)
+              base = w.decay * before[t];
+          }
+          const bool whole = tok >= every_b && tok + kKeys <= every_e;
+          const uint64_t sk2 = pair(sk, sk), log2e = pair(kLog2e, kLog2e);
+          uint64_t sum[4] = {0, 0, 0, 0};
+          for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
+            if (!wait(&s_full[X], s_no & 1)) break;
+            tc::tc_fence_after();
+            const int n = min(kHalfCols, n_pad - h0);
+#pragma unroll 1
+            for (int ch = 0; ch < n; ch += 32) {
+              float v[32];
+              tc::tmem_ld32(s_at + ch, v);
+              const float* f = f_s + h0 + ch;
+              const float* l = l_s + h0 + ch;
+              if (whole) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                  const float4 f4 = four(f + e), l4 = four(l + e);
+                  float x[4];
+                  halves(mul2(fma2(pair(v[e], v[e + 1]), mul2(pair(f4.x, f4.y), sk2), pair(l4.x, l4.y)), log2e), x[0], x[1]);
+                  halves(mul2(fma2(pair(v[e + 2], v[e + 3]), mul2(pair(f4.z, f4.w), sk2), pair(l4.z, l4.w)), log2e), x[2], x[3]);
+                  sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(pow2(x[0]), pow2(x[1])));
+                  sum[(e / 2 + 1) & 3] = add2(sum[(e / 2 + 1) & 3], pair(pow2(x[2]), pow2(x[3])));
+                }
+              } else {
+                const int* kb = kb_s + h0 + ch;
+                const int* ke = ke_s + h0 + ch;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  const float x = pow2(fmaf(v[e], f[e] * sk, l[e]) * kLog2e), y = pow2(fmaf(v[e + 1], f[e + 1] * sk, l[e + 1]) * kLog2e);
+                  sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(t >= kb[e] && t < ke[e] ? x : 0.f, t >= kb[e + 1] && t < ke[e + 1] ? y : 0.f));
+                }
+              }
+            }
+            tc::tc_fence_before();
+            tc::mbar_arrive(tc::smem_u32(&s_empty[X]));
+          }
+          float x, y;
+          halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), x, y);
+          if (writes && ok) out[t] = base + (live ? x + y : 0.f);
+        }
+        tc::mbar_arrive(tc::smem_u32(&q_read));
+      }
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------ codes to operands: 32 tokens per warp
+    const int cw = warp - 8;
+    constexpr int UH = D / 64;
+    uint4 kr[4][UH];
+    int64_t place[2], place_n[2];
+    float sk[2], sk_n[2];
+    while (ok && next_part()) {
+      const int len = u.s.len, tok0 = (u.s.lo + u.tile) * kKeys + 32 * cw;
+      const int some_b = a.window > 0 ? max(0, len - u.s.n - a.window + 1) : 0;
+      auto look_up = [&](int i) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int tok = tok0 + i * kKeys + 16 * b;
+          place_n[b] = -1;
+          sk_n[b] = 0.f;
+          if (i < n_tiles && tok < len && tok + kCacheBlock > some_b) {
+            const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
+            if (page >= 0) {
+              const int in = tok % a.c.page;
+              place_n[b] = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
+              sk_n[b] = __ldg(a.c.ks + (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock);
+            }
+          }
+        }
+      };
+      // lane: rows (lane & 7) of each 8, 16-byte units (lane >> 3) of each 4
+      auto load = [&](int i) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < UH; ++e)
+            kr[g][e] = i < n_tiles && place_n[g >> 1] >= 0
+                           ? __ldg(reinterpret_cast<const uint4*>(a.c.K + place_n[g >> 1] + (8 * (g & 1) + (lane & 7)) * D + (4 * e + (lane >> 3)) * 16))
+                           : make_uint4(0, 0, 0, 0);
+      };
+      for (int64_t c0 = 0; c0 < cols && ok; c0 += kMostCols) {
+        look_up(0);
+        for (int i = -1; i < n_tiles; ++i) {  // tile i's operands are written, tile i + 1's codes loaded
+          const int buf = tile_no & 1;
+          if (i >= 0) {
+            if (!wait(&k_empty[buf], ((tile_no >> 1) & 1) ^ 1)) break;
+            if (lane < 2) {
+              sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
+              live_s[buf][2 * cw + lane] = (lane ? place[1] : place[0]) >= 0;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+              for (int e = 0; e < UH; ++e)
+                store_codes<FMT>(k_sm + buf * S::kSide + piece<D>(32 * cw + 8 * g + (lane & 7), 2 * (4 * e + (lane >> 3))), kr[g][e]);
+            tc::fence_async_smem();
+            __syncwarp();
+            tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
+            ++tile_no;
+          }
+          load(i + 1);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            place[b] = place_n[b];
+            sk[b] = sk_n[b];
+          }
+          look_up(i + 2);
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ products of a group's tiles (one lane issues)
+    const int X = warp - 12;
+    const uint64_t q_desc = tc::smem_desc(tc::smem_u32(q_sm), 128, D * 16);
+    const uint64_t k_desc = tc::smem_desc(tc::smem_u32(k_sm + X * S::kSide), 128, D * 16);
+    uint32_t s_no = 0;
+    while (ok && next_part()) {
+      for (int64_t c0 = 0; c0 < cols && ok; c0 += kMostCols, ++q_no) {
+        const int n_cols = (int)min((int64_t)kMostCols, cols - c0), n_pad = (n_cols + 31) / 32 * 32;
+        if (!wait(&q_full, q_no & 1)) break;
+        for (int i = 0; i < n_tiles && ok; ++i, ++tile_no) {
+          if ((int)(tile_no & 1) != X) continue;
+          if (!wait(&k_full[X], (tile_no >> 1) & 1)) break;
+          for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
+            if (!wait(&s_empty[X], (s_no & 1) ^ 1)) break;
+            tc::tc_fence_after();
+            const uint32_t idesc = idesc_f16(kKeys, min(kHalfCols, n_pad - h0), false);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+              mma_ss(tmem + X * kHalfCols, k_desc + ks * 16, q_desc + (h0 * D * 2 + ks * 256) / 16, idesc, ks > 0);
+            commit(&s_full[X]);
+          }
+          commit(&k_empty[X]);
+        }
+      }
+    }
+    __syncwarp();
+    commit(&all_done[X]);  // whatever was issued has ended before tensor memory is freed
+    tc::mbar_wait(tc::smem_u32(&all_done[X]), 0, a.err);
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  if (warp == 12) tc::tmem_dealloc(tmem, 2 * kHalfCols);
+  unseen_places<D>(w);
+}
+
+template <int D, int FMT>
+crvq_status launch_wt(WeightArgs& w, cudaStream_t stream) {
+  using S = WtShape<D>;
+  auto kernel = weights_tc_kernel<D, FMT>;
+  CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
+  w.a.shares = sm_count();
+  ProfScope ps("cache_weights", stream, (double)w.a.rows.n_tok * w.a.q.heads * D);
+  CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)w.a.shares), dim3(kWtThreads), S::kSmem, stream, w));
+  CRVQ_LAUNCHED();
+  return CRVQ_OK;
+}
+
+}  // namespace
+
+crvq_status launch_weights_many(WeightArgs& w, int D, int format, cudaStream_t stream) {
+  if (D == 64) return format == CRVQ_KV_INT8 ? launch_wt<64, CRVQ_KV_INT8>(w, stream) : launch_wt<64, CRVQ_KV_E4M3>(w, stream);
+  return format == CRVQ_KV_INT8 ? launch_wt<128, CRVQ_KV_INT8>(w, stream) : launch_wt<128, CRVQ_KV_E4M3>(w, stream);
+}
+
+}  // namespace crvq
