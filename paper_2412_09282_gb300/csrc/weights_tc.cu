@@ -1,10 +1,11 @@
 // Accumulated attention weights for many queries per sequence (see weights.cu for the formula), on tcgen05.
 //
 // S^T (128 tokens x up to 256 columns) = K Q^T: tokens are the lanes of tensor memory, so a thread has one token's scores, and
-// its sum over the columns is its own: no maxima, no shuffles. All columns' queries (512 at a time, as fp16 relative to a power
-// of two each) lie in shared memory while the tiles of a (sequence, kv head) pass.
+// its sum over the columns is its own: no maxima, no shuffles. All columns' queries (512 at a time, as they are) lie in shared
+// memory while the tiles of a (sequence, kv head) pass. Codes become operands of the queries' type, exactly: no query needs
+// a factor.
 // Two groups of four warps take every other tile, each with its own half of tensor memory and its own issuing warp; four warps
-// turn codes into fp16 operands (exact). While one group's exponentials run, the other's products do.
+// turn codes into operands. While one group's exponentials run, the other's products do.
 // Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; every token is one thread's.
 #include "attend_tc.cuh"
 #include "weights.cuh"
@@ -20,7 +21,7 @@ template <int D>
 struct WtShape {
   static constexpr int kQ = kMostCols * D * 2;
   static constexpr int kSide = kKeys * D * 2;
-  static constexpr size_t kSmem = kQ + 2 * kSide + kMostCols * 16;
+  static constexpr size_t kSmem = kQ + 2 * kSide + kMostCols * 12;
 };
 
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
@@ -29,7 +30,42 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 
-template <int D, int FMT>
+// Codes 0, 1 (half 0) or 2, 3 (half 1) of a word as bf16: exact, both formats have 8 significant bits at most.
+template <int FMT, int HALF>
+__device__ __forceinline__ uint32_t codes2_bf16(uint32_t w) {
+  if constexpr (FMT == CRVQ_KV_INT8) {
+    // c = (128 + (u & 127)) - (u & 128 ? 128 : 256) for u = c + 128
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t x = __byte_perm(u & 0x7f7f7f7fu, 0x43434343u, HALF ? 0x4342 : 0x4140);
+    const uint32_t y = __byte_perm((u & 0x80808080u) ^ 0x80808080u, 0x43434343u, HALF ? 0x4342 : 0x4140);
+    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const uint32_t h = codes2<FMT, HALF>(w);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    return __byte_perm(__float_as_uint(f.x), __float_as_uint(f.y), 0x7632);
+  }
+}
+
+// Sixteen codes of a token as the queries' type, to two neighbouring pieces.
+template <int FMT, bool BF16>
+__device__ __forceinline__ void store_codes(char* dst, const uint4& u) {
+  if constexpr (!BF16) {
+    store_codes<FMT>(dst, u);
+  } else {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t h[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[2 * i] = codes2_bf16<FMT, 0>(w[i]);
+      h[2 * i + 1] = codes2_bf16<FMT, 1>(w[i]);
+    }
+    *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
+  }
+}
+
+template <int D, int FMT, bool BF16>
 __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_constant__ WeightArgs w) {
   using S = WtShape<D>;
   const AttendArgs& a = w.a;
@@ -51,8 +87,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   }
   char* q_sm = sm;
   char* k_sm = sm + S::kQ;
-  float* f_s = reinterpret_cast<float*>(k_sm + 2 * S::kSide);  // [kMostCols] factors of the scores, -lse, first, last + 1 key seen
-  float* l_s = f_s + kMostCols;
+  float* l_s = reinterpret_cast<float*>(k_sm + 2 * S::kSide);  // [kMostCols] -lse, first and last + 1 key seen
   int* kb_s = reinterpret_cast<int*>(l_s + kMostCols);
   int* ke_s = kb_s + kMostCols;
   if (warp == 12) tc::tmem_alloc(&tmem_slot, 2 * kHalfCols);
@@ -110,61 +145,50 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
         const int n_cols = (int)min((int64_t)kMostCols, cols - c0), n_pad = (n_cols + 31) / 32 * 32;
         // every thread has read what lay there before; products that read it have ended (their scores have been read)
         if (q_no > 0 && !wait(&q_read, (q_no - 1) & 1)) break;
-        for (int col = tid; col < n_pad; col += 256) {
-          const bool valid = col < n_cols;
-          const int64_t c = c0 + col;
-          const int j = valid ? (int)(c / a.group) : 0, h = u.h * a.group + (valid ? (int)(c % a.group) : 0);
-          const float lse = valid ? __ldg(w.lse + (u.s.first + j) * a.q.heads + h) : INFINITY;
-          const bool none = isinf(lse);  // (such a query has no weights)
-          const int64_t src = (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head;
-          const uint16_t* row_q = static_cast<const uint16_t*>(a.q.data) + src;
-          uint4 raw[D / 8];
+        // a warp takes 8 columns at a time; lane: column (lane & 7), 16-byte pieces (lane >> 3) of each 4. All lse first.
+        constexpr int kTimes = kMostCols / 64;
+        float lse[kTimes];
+        auto query = [&](int col, int* h) {  // (a padding column: any)
+          const uint32_t c = (uint32_t)c0 + (col < n_cols ? col : 0), j = c / (uint32_t)a.group;
+          *h = u.h * a.group + (int)(c - j * (uint32_t)a.group);
+          return (int)j;
+        };
 #pragma unroll
-          for (int e = 0; e < D / 8; ++e) {
-            if (none) {
-              raw[e] = make_uint4(0, 0, 0, 0);
-            } else if (a.vec_q) {
-              raw[e] = __ldg(reinterpret_cast<const uint4*>(row_q) + e);
+        for (int k = 0; k < kTimes; ++k) {
+          const int col = 64 * k + 8 * warp + (lane & 7);
+          int h;
+          const int j = query(col, &h);
+          lse[k] = col < n_cols ? __ldg(w.lse + (u.s.first + j) * a.q.heads + h) : INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < kTimes; ++k) {
+          const int col = 64 * k + 8 * warp + (lane & 7);
+          if (col >= n_pad) break;
+          int h;
+          const int j = query(col, &h);
+          const bool none = isinf(lse[k]);  // (such a query has no weights)
+          const uint16_t* row_q = static_cast<const uint16_t*>(a.q.data) + (u.s.first + j) * a.q.ld_tok + h * a.q.ld_head;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            const int e = 4 * i + (lane >> 3);
+            char* dst = q_sm + piece<D>(col, e);
+            if (a.vec_q) {
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(row_q + 8 * e), "r"(none ? 0 : 16) : "memory");
             } else {
               uint32_t x[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) x[i] = row_q[8 * e + 2 * i] | (uint32_t)row_q[8 * e + 2 * i + 1] << 16;
-              raw[e] = make_uint4(x[0], x[1], x[2], x[3]);
+              for (int y = 0; y < 4; ++y) x[y] = none ? 0u : row_q[8 * e + 2 * y] | (uint32_t)row_q[8 * e + 2 * y + 1] << 16;
+              *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
             }
           }
-          uint32_t top2 = 0;
-#pragma unroll
-          for (int e = 0; e < D / 8; ++e) {
-            top2 = __vmaxu2(top2, __vmaxu2(raw[e].x & 0x7fff7fffu, raw[e].y & 0x7fff7fffu));
-            top2 = __vmaxu2(top2, __vmaxu2(raw[e].z & 0x7fff7fffu, raw[e].w & 0x7fff7fffu));
+          if (lane < 8) {
+            const int pos = held + j;
+            l_s[col] = none ? -INFINITY : -lse[k];
+            kb_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+            ke_s[col] = a.causal ? min(len, pos + 1) : len;
           }
-          const uint32_t top16 = max(top2 & 0xffffu, top2 >> 16);
-          const float top = a.q.type == CRVQ_BF16 ? __uint_as_float(top16 << 16) : __half2float(__ushort_as_half((uint16_t)top16));
-          const uint32_t ex = __float_as_uint(top) >> 23;
-          const bool plain = ex == 0 || ex == 255;
-          const float inv = plain ? 1.f : __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
-          const float back = plain ? 1.f : __uint_as_float(ex << 23);
-#pragma unroll
-          for (int e = 0; e < D / 8; ++e) {
-            const uint32_t x[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float2 v;
-              if (a.q.type == CRVQ_BF16)
-                v = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
-              else
-                v = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
-              o[i] = half2_bits(v.x * inv, v.y * inv);
-            }
-            *reinterpret_cast<uint4*>(q_sm + piece<D>(col, e)) = make_uint4(o[0], o[1], o[2], o[3]);
-          }
-          const int pos = held + j;
-          f_s[col] = none ? 0.f : back * w.scale;
-          l_s[col] = none ? -INFINITY : -lse;
-          kb_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-          ke_s[col] = a.causal ? min(len, pos + 1) : len;
         }
+        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         tc::fence_async_smem();
         tc::mbar_arrive(tc::smem_u32(&q_full));
         if (!wait(&q_full, q_no & 1)) break;
@@ -187,7 +211,8 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
               base = w.decay * before[t];
           }
           const bool whole = tok >= every_b && tok + kKeys <= every_e;
-          const uint64_t sk2 = pair(sk, sk), log2e = pair(kLog2e, kLog2e);
+          const float g = w.scale * sk;
+          const uint64_t g2 = pair(g, g), log2e = pair(kLog2e, kLog2e);
           uint64_t sum[4] = {0, 0, 0, 0};
           for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
             if (!wait(&s_full[X], s_no & 1)) break;
@@ -197,15 +222,14 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
             for (int ch = 0; ch < n; ch += 32) {
               float v[32];
               tc::tmem_ld32(s_at + ch, v);
-              const float* f = f_s + h0 + ch;
               const float* l = l_s + h0 + ch;
               if (whole) {
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                  const float4 f4 = four(f + e), l4 = four(l + e);
+                  const float4 l4 = four(l + e);
                   float x[4];
-                  halves(mul2(fma2(pair(v[e], v[e + 1]), mul2(pair(f4.x, f4.y), sk2), pair(l4.x, l4.y)), log2e), x[0], x[1]);
-                  halves(mul2(fma2(pair(v[e + 2], v[e + 3]), mul2(pair(f4.z, f4.w), sk2), pair(l4.z, l4.w)), log2e), x[2], x[3]);
+                  halves(mul2(fma2(pair(v[e], v[e + 1]), g2, pair(l4.x, l4.y)), log2e), x[0], x[1]);
+                  halves(mul2(fma2(pair(v[e + 2], v[e + 3]), g2, pair(l4.z, l4.w)), log2e), x[2], x[3]);
                   sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(pow2(x[0]), pow2(x[1])));
                   sum[(e / 2 + 1) & 3] = add2(sum[(e / 2 + 1) & 3], pair(pow2(x[2]), pow2(x[3])));
                 }
@@ -214,7 +238,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
                 const int* ke = ke_s + h0 + ch;
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
-                  const float x = pow2(fmaf(v[e], f[e] * sk, l[e]) * kLog2e), y = pow2(fmaf(v[e + 1], f[e + 1] * sk, l[e + 1]) * kLog2e);
+                  const float x = pow2(fmaf(v[e], g, l[e]) * kLog2e), y = pow2(fmaf(v[e + 1], g, l[e + 1]) * kLog2e);
                   sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(t >= kb[e] && t < ke[e] ? x : 0.f, t >= kb[e + 1] && t < ke[e + 1] ? y : 0.f));
                 }
               }
@@ -233,65 +257,72 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
     // ------------------------------------------------------------------ codes to operands: 32 tokens per warp
     const int cw = warp - 8;
     constexpr int UH = D / 64;
-    uint4 kr[4][UH];
-    int64_t place[2], place_n[2];
-    float sk[2], sk_n[2];
+    // codes of two tiles on their way, and places and scales of the one after them
+    uint4 kr[2][4][UH];
+    int64_t place[3][2];
+    float sk[3][2];
     while (ok && next_part()) {
       const int len = u.s.len, tok0 = (u.s.lo + u.tile) * kKeys + 32 * cw;
       const int some_b = a.window > 0 ? max(0, len - u.s.n - a.window + 1) : 0;
-      auto look_up = [&](int i) {
+      auto look_up = [&](int i, int64_t (&p)[2], float (&scale)[2]) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const int tok = tok0 + i * kKeys + 16 * b;
-          place_n[b] = -1;
-          sk_n[b] = 0.f;
+          p[b] = -1;
+          scale[b] = 0.f;
           if (i < n_tiles && tok < len && tok + kCacheBlock > some_b) {
             const int64_t page = seq_page(a.c, u.b, tok / a.c.page, a.err);
             if (page >= 0) {
               const int in = tok % a.c.page;
-              place_n[b] = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
-              sk_n[b] = __ldg(a.c.ks + (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock);
+              p[b] = page * a.c.page_stride + ((int64_t)u.h * a.c.page + in) * D;
+              scale[b] = __ldg(a.c.ks + (page * a.c.n_kv + u.h) * (a.c.page / kCacheBlock) + in / kCacheBlock);
             }
           }
         }
       };
       // lane: rows (lane & 7) of each 8, 16-byte units (lane >> 3) of each 4
-      auto load = [&](int i) {
+      auto load = [&](const int64_t (&p)[2], uint4 (&x)[4][UH]) {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
           for (int e = 0; e < UH; ++e)
-            kr[g][e] = i < n_tiles && place_n[g >> 1] >= 0
-                           ? __ldg(reinterpret_cast<const uint4*>(a.c.K + place_n[g >> 1] + (8 * (g & 1) + (lane & 7)) * D + (4 * e + (lane >> 3)) * 16))
-                           : make_uint4(0, 0, 0, 0);
+            x[g][e] = p[g >> 1] >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.c.K + p[g >> 1] + (8 * (g & 1) + (lane & 7)) * D + (4 * e + (lane >> 3)) * 16))
+                                     : make_uint4(0, 0, 0, 0);
+      };
+      auto store = [&](const int64_t (&p)[2], const float (&scale)[2], const uint4 (&x)[4][UH]) {
+        const int buf = tile_no & 1;
+        if (!wait(&k_empty[buf], ((tile_no >> 1) & 1) ^ 1)) return;
+        if (lane < 2) {
+          sk_s[buf][2 * cw + lane] = lane ? scale[1] : scale[0];
+          live_s[buf][2 * cw + lane] = (lane ? p[1] : p[0]) >= 0;
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < UH; ++e)
+            store_codes<FMT, BF16>(k_sm + buf * S::kSide + piece<D>(32 * cw + 8 * g + (lane & 7), 2 * (4 * e + (lane >> 3))), x[g][e]);
+        tc::fence_async_smem();
+        __syncwarp();
+        tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
+        ++tile_no;
       };
       for (int64_t c0 = 0; c0 < cols && ok; c0 += kMostCols) {
-        look_up(0);
-        for (int i = -1; i < n_tiles; ++i) {  // tile i's operands are written, tile i + 1's codes loaded
-          const int buf = tile_no & 1;
-          if (i >= 0) {
-            if (!wait(&k_empty[buf], ((tile_no >> 1) & 1) ^ 1)) break;
-            if (lane < 2) {
-              sk_s[buf][2 * cw + lane] = lane ? sk[1] : sk[0];
-              live_s[buf][2 * cw + lane] = (lane ? place[1] : place[0]) >= 0;
+        look_up(0, place[0], sk[0]);
+        look_up(1, place[1], sk[1]);
+        load(place[0], kr[0]);
+        load(place[1], kr[1]);
+        for (int i = 0; i < n_tiles && ok; i += 2) {
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            look_up(i + z + 2, place[2], sk[2]);
+            if (i + z < n_tiles && ok) store(place[z], sk[z], kr[z]);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              place[z][b] = place[2][b];
+              sk[z][b] = sk[2][b];
             }
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-              for (int e = 0; e < UH; ++e)
-                store_codes<FMT>(k_sm + buf * S::kSide + piece<D>(32 * cw + 8 * g + (lane & 7), 2 * (4 * e + (lane >> 3))), kr[g][e]);
-            tc::fence_async_smem();
-            __syncwarp();
-            tc::mbar_arrive(tc::smem_u32(&k_full[buf]));
-            ++tile_no;
+            load(place[z], kr[z]);
           }
-          load(i + 1);
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            place[b] = place_n[b];
-            sk[b] = sk_n[b];
-          }
-          look_up(i + 2);
         }
       }
     }
@@ -311,7 +342,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
           for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
             if (!wait(&s_empty[X], (s_no & 1) ^ 1)) break;
             tc::tc_fence_after();
-            const uint32_t idesc = idesc_f16(kKeys, min(kHalfCols, n_pad - h0), false);
+            const uint32_t idesc = idesc_f16(kKeys, min(kHalfCols, n_pad - h0), false) | (BF16 ? 1u << 7 | 1u << 10 : 0u);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
               mma_ss(tmem + X * kHalfCols, k_desc + ks * 16, q_desc + (h0 * D * 2 + ks * 256) / 16, idesc, ks > 0);
@@ -333,10 +364,10 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   unseen_places<D>(w);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool BF16>
 crvq_status launch_wt(WeightArgs& w, cudaStream_t stream) {
   using S = WtShape<D>;
-  auto kernel = weights_tc_kernel<D, FMT>;
+  auto kernel = weights_tc_kernel<D, FMT, BF16>;
   CRVQ_TRY(smem_limit((const void*)kernel, S::kSmem));
   w.a.shares = sm_count();
   ProfScope ps("cache_weights", stream, (double)w.a.rows.n_tok * w.a.q.heads * D);
@@ -348,8 +379,13 @@ crvq_status launch_wt(WeightArgs& w, cudaStream_t stream) {
 }  // namespace
 
 crvq_status launch_weights_many(WeightArgs& w, int D, int format, cudaStream_t stream) {
-  if (D == 64) return format == CRVQ_KV_INT8 ? launch_wt<64, CRVQ_KV_INT8>(w, stream) : launch_wt<64, CRVQ_KV_E4M3>(w, stream);
-  return format == CRVQ_KV_INT8 ? launch_wt<128, CRVQ_KV_INT8>(w, stream) : launch_wt<128, CRVQ_KV_E4M3>(w, stream);
+  const bool int8 = format == CRVQ_KV_INT8;
+  if (w.a.q.type == CRVQ_BF16) {
+    if (D == 64) return int8 ? launch_wt<64, CRVQ_KV_INT8, true>(w, stream) : launch_wt<64, CRVQ_KV_E4M3, true>(w, stream);
+    return int8 ? launch_wt<128, CRVQ_KV_INT8, true>(w, stream) : launch_wt<128, CRVQ_KV_E4M3, true>(w, stream);
+  }
+  if (D == 64) return int8 ? launch_wt<64, CRVQ_KV_INT8, false>(w, stream) : launch_wt<64, CRVQ_KV_E4M3, false>(w, stream);
+  return int8 ? launch_wt<128, CRVQ_KV_INT8, false>(w, stream) : launch_wt<128, CRVQ_KV_E4M3, false>(w, stream);
 }
 
 }  // namespace crvq
