@@ -161,7 +161,7 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
           if (c0 > 0)
             base = out[t_mine];
           else if (before)
-            base = w.decay * __ldg(before + t_mine);
+            base = w.decay * before[t_mine];
         }
         asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
         __syncwarp();
