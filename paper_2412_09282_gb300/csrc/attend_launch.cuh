@@ -62,9 +62,20 @@ crvq_status pick_format(AttendArgs& a, int format, cudaStream_t stream) {
   return split ? pick_columns<D, CRVQ_KV_E4M3, true, TREE>(a, stream) : pick_columns<D, CRVQ_KV_E4M3, false, TREE>(a, stream);
 }
 
+// Trees with that many columns over short sequences: units of 16 columns, at two CTAs each or more, up to this many tiles of
+// 128 tokens in all. This form against tiles of 128 rows, us, for (sequences x kv heads, columns, tokens): (1 x 1, 512,
+// 4000) 25, 52; (1 x 8, 64, 4000) 25, 37; (1 x 8, 128, 1000) 21, 32; (1 x 8, 256, 2000) 35, 44; (4 x 8, 64, 1000) 25, 36;
+// (4 x 8, 64, 2000) 35, 38; (1 x 8, 256, 4000) 67, 50; (4 x 8, 128, 1000) 52, 38; (1 x 8, 512, 1000) 52, 42. (Attention
+// without trees keeps its rule, and with it its results.)
+constexpr int64_t kFewTiles = 2048;
+inline bool few_tiles(const AttendArgs& a) {
+  const int64_t units = most_units<16>(a), tiles = ceil_div((int64_t)a.c.max_pages * a.c.page, 128);
+  return 2 * units <= 3 * (int64_t)sm_count() && units * tiles <= kFewTiles;
+}
+
 template <bool TREE>
 crvq_status launch_form(AttendArgs& a, int D, int format, cudaStream_t stream) {
-  if (D != 256 && a.q.type != CRVQ_F32 && a.rows.n_tok * a.group >= kManyColumns * (int64_t)a.c.n_seq)
+  if (D != 256 && a.q.type != CRVQ_F32 && a.rows.n_tok * a.group >= kManyColumns * (int64_t)a.c.n_seq && !(TREE && few_tiles(a)))
     return TREE ? launch_tree_many(a, D, format, stream) : launch_attend_many(a, D, format, stream);
   if (D == 64) return pick_format<64, TREE>(a, format, stream);
   if (D == 128) return pick_format<128, TREE>(a, format, stream);
