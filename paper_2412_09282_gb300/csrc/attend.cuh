@@ -228,7 +228,8 @@ __device__ __forceinline__ uint32_t range32(int t0, int kb, int ke) {
 
 // Trees of drafted tokens. The last n tokens of a sequence are the drafted ones, token `held` the first of them. A query
 // sees the cached tokens from kb on and those drafted ones that its row of bits names: tokens t0 + i as bits.
-__device__ __forceinline__ uint32_t tree32(const AttendArgs& a, int64_t row, int t0, int kb, int held, int len) {
+// (Out of line: few tiles need it, and inline its registers are every tile's.)
+__device__ __noinline__ uint32_t tree32(const AttendArgs& a, int64_t row, int t0, int kb, int held, int len) {
   uint32_t seen = range32(t0, kb, min(held, len));
   if (t0 + 32 <= held || t0 >= len) return seen;
   const int first = t0 - held, w = first >> 5;  // (before the first drafted token: words of zeros)

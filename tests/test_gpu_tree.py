@@ -41,7 +41,7 @@ def _queries(seed, n, heads, d, dtype, size=1.0):
     return torch.from_numpy(x).to(U.TORCH[dtype]).float().numpy()
 
 
-def _check(host, gpu, q, counts, mask, dtype, ragged=True, positions=None, window=0, gap=0):
+def _check(host, gpu, q, counts, mask, dtype, ragged=True, positions=None, window=0, gap=0, least=0.0):
     import paper_2412_09282_gb300 as P
     d = q.shape[2]
     scale = 1.0 / math.sqrt(d)
@@ -53,7 +53,8 @@ def _check(host, gpu, q, counts, mask, dtype, ragged=True, positions=None, windo
     n = int(max(host["lens"]))
     per = 2.0 ** -23 + (2.0 ** -21 / (d + 16) if dtype == "f32" else 0.0)
     rel = 2 * U.WEIGHT_ROUND[dtype] + 2.0 ** -21 * n / 16 + 4 * per * shake[..., None] + 2.0 ** -19
-    bound = U.OUT_ROUND[dtype] * np.abs(ref) + rel * mass + (2.0 ** -25 if dtype == "f16" else 1e-30)
+    bound = U.OUT_ROUND[dtype] * np.abs(ref) + rel * mass + n * least * mass.max(-1, keepdims=True) + \
+        (2.0 ** -25 if dtype == "f16" else 1e-30)
     got = U.exactly(out).astype(np.float64)
     empty = ~np.isfinite(lse_ref)
     assert np.all(np.abs(got - ref) <= bound), float((np.abs(got - ref) / bound).max())
@@ -300,3 +301,49 @@ def test_a_captured_step_replays_with_new_trees_and_lengths():
             ref = step()
             P.crvq_sync()
             assert torch.equal(out, ref) and (ref != 0).any()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,page,n_kv,group,n", [(128, 64, 20, 1, 20), (64, 16, 24, 2, 12), (128, 48, 16, 4, 9), (64, 32, 32, 1, 40)])
+def test_some_tens_of_queries_over_many_heads(fmt, dtype, d, page, n_kv, group, n):
+    """Long and short sequences beside each other, trees that are all there is, none, and windows; not all full units.
+    Weights below fp16's normal numbers are off by 2^-25 beside a largest one of 2^5 at least, so n of them by n 2^-30 of the
+    largest's weight, whose token has at least half of its block's largest code in some channel: n 2^-29 of the row's
+    largest sum of p |V|. It shows in a channel where that token's code is 0, as one of 20 x 128 x 84 here has."""
+    lens, counts = [1400, 17, 333, n, 700, 128], [n, 9, max(1, n - 5), n, 0, n]
+    host, gpu = U.make(40, lens, page, n_kv, d, fmt, page_gap=1)
+    q = _queries(41, sum(counts), n_kv * group, d, dtype, 2.0)
+    mask, pos = C.tree_mask(_parents(42, counts), counts, -(-max(counts) // 32), 0, lens)
+    _check(host, gpu, q, counts, mask, dtype, gap=5, least=2.0 ** -29)
+    mask, pos = C.tree_mask(_parents(42, counts), counts, -(-max(counts) // 32), 300, lens)
+    _check(host, gpu, q, counts, mask, dtype, positions=pos, window=300, least=2.0 ** -29)
+
+
+def test_growing_maxima_and_scales_far_apart_with_some_tens_of_queries():
+    """Key scales that grow along the sequence (references move many times), value scales far apart (as far as fp16 outputs
+    hold them, and 2^80), zeros among them, and not finite queries beside finite ones. What weights below fp16's normal
+    numbers are off by, 2^-25 beside a largest one of 2^5 at least, is n 2^-29 of the row's largest sum of p |V| (see
+    test_gpu_attention_scales.py)."""
+    import paper_2412_09282_gb300 as P
+    for fmt, dtype, low, high in (("int8", "f16", -12, 8), ("e4m3", "bf16", -40, 40)):
+        host, _ = U.make(43, [2000, 900], 16, 16, 128, fmt)
+        rng = np.random.default_rng(44)
+        for b, n in enumerate((125, 57)):
+            order = host["pages"][b, :n]
+            host["k_scale"][order, :, 0] *= np.exp(np.linspace(-2.0, 1.5, n)).astype(np.float32)[:, None]
+            host["v_scale"][order, :, 0] *= np.exp2(rng.uniform(low, high, (n, 16))).astype(np.float32)
+            host["v_scale"][order[20], :, 0] = 0.0
+        gpu = U.on_gpu(host, fmt)
+        q = _queries(45, 40, 16, 128, dtype, 1.0)
+        mask, _ = C.tree_mask(_parents(46, [20, 20]), [20, 20], 1)
+        _check(host, gpu, q, [20, 20], mask, dtype, least=2.0 ** -29)
+        ref = U.exactly(P.crvq_cache_tree_attention(gpu, U.heads(q, dtype), _bits(mask), q_off=U.offsets([20, 20])))
+        q[7, 1, 3], q[30, 0, 5] = np.nan, np.inf
+        out = U.exactly(P.crvq_cache_tree_attention(gpu, U.heads(q, dtype), _bits(mask), q_off=U.offsets([20, 20])))
+        again = U.exactly(P.crvq_cache_tree_attention(gpu, U.heads(q, dtype), _bits(mask), q_off=U.offsets([20, 20])))
+        P.crvq_sync()
+        same = np.ones((40, 16), bool)
+        same[7, 1] = same[30, 0] = False
+        assert np.array_equal(out[same], ref[same]) and np.isnan(out[~same]).all()
+        assert np.array_equal(out, again, equal_nan=True)
