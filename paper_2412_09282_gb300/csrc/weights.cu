@@ -29,7 +29,8 @@ struct WShape {
   }
 };
 
-template <int D, int FMT, bool SPLIT>
+// ONE: sequences of up to 8 columns each: their queries stay in registers, and codes are used as they are converted.
+template <int D, int FMT, bool SPLIT, bool ONE>
 __global__ void __launch_bounds__(kThreads, D == 256 ? 2 : 3)
 weights_kernel(const __grid_constant__ WeightArgs w) {
   using S = WShape<D>;
@@ -143,6 +144,18 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
       // keys that every column sees (places do not fall from column to column)
       const int every_b = __float_as_int(col_s[n_cols - 1].z), every_e = __float_as_int(col_s[0].w);
 
+      uint4 q_one[ONE && SPLIT ? 2 : 1][ONE ? D / 64 : 1][2];
+      if constexpr (ONE) {
+#pragma unroll
+        for (int z = 0; z < (SPLIT ? 2 : 1); ++z)
+#pragma unroll
+          for (int j = 0; j < D / 64; ++j) {
+            const uint4* p = reinterpret_cast<const uint4*>(q_s + ((size_t)z * w.chunk + gid) * S::kQRow + 64 * j + 16 * tig);
+            q_one[z][j][0] = p[0];
+            q_one[z][j][1] = p[1];
+          }
+      }
+
       for (int i = 0; i < n_tiles; ++i) {
         const bool old = (i * NB >> 5) != batch;
         const int tok = (u.s.lo + u.tile + i) * kTile<D> + warp * NB * kCacheBlock;
@@ -166,31 +179,42 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
         asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
         __syncwarp();
         const char* keys = mine + (i % S::kStages) * S::kStage;
-        uint32_t k[NB][D / 16][4];
+        // 16 consecutive codes of rows gid and gid + 8 of a block: four steps of the product
+        auto codes = [&](int b, int j, uint4* k0, uint4* k1) {
+          const char* p = keys + b * Tile<D>::kBytes + (j >> 1) * 128;
+          *k0 = *reinterpret_cast<const uint4*>(p + (key_at ^ (j & 1) * 64));
+          *k1 = *reinterpret_cast<const uint4*>(p + 8 * D + (key_at ^ (j & 1) * 64));
+        };
+        auto operand = [&](const uint4& k0, const uint4& k1, int e, uint32_t (&f)[4]) {
+          const uint32_t x = word(k0, e), y = word(k1, e);
+          f[0] = codes2<FMT, 0>(x);
+          f[1] = codes2<FMT, 0>(y);
+          f[2] = codes2<FMT, 1>(x);
+          f[3] = codes2<FMT, 1>(y);
+        };
+        auto next_copies = [&]() {
+          __syncwarp();  // every lane has read what these copies overwrite
+          look_up(i + S::kStages - 1);
+          start(i + S::kStages - 1);
+        };
+        uint32_t k[ONE ? 1 : NB][ONE ? 1 : D / 16][4];
+        if constexpr (!ONE) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int j = 0; j < D / 64; ++j) {
-            const char* p = keys + b * Tile<D>::kBytes + (j >> 1) * 128;
-            const uint4 k0 = *reinterpret_cast<const uint4*>(p + (key_at ^ (j & 1) * 64));
-            const uint4 k1 = *reinterpret_cast<const uint4*>(p + 8 * D + (key_at ^ (j & 1) * 64));
+            for (int j = 0; j < D / 64; ++j) {
+              uint4 k0, k1;
+              codes(b, j, &k0, &k1);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t x = word(k0, e), y = word(k1, e);
-              k[b][4 * j + e][0] = codes2<FMT, 0>(x);
-              k[b][4 * j + e][1] = codes2<FMT, 0>(y);
-              k[b][4 * j + e][2] = codes2<FMT, 1>(x);
-              k[b][4 * j + e][3] = codes2<FMT, 1>(y);
+              for (int e = 0; e < 4; ++e) operand(k0, k1, e, k[b][4 * j + e]);
             }
-          }
-        __syncwarp();  // every lane has read what these copies overwrite
-        look_up(i + S::kStages - 1);
-        start(i + S::kStages - 1);
+          next_copies();
+        }
         const bool whole = tok >= every_b && tok + NB * kCacheBlock <= every_e;
         float sum[NB][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b) sum[b][0] = sum[b][1] = 0.f;
-        for (int g = 0; g < groups; ++g) {
+        for (int g = 0; g < (ONE ? 1 : groups); ++g) {
           // 64 channels' products at a time, second operands' apart, are added up in fp32: a tensor core's sums are cut off
           // towards zero where they are long or a small product meets a large sum (16 of both kinds in a chain: weights
           // 1e-6 too small on average; so, 2e-7)
@@ -199,17 +223,32 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
           for (int j = 0; j < D / 64; ++j)
 #pragma unroll
             for (int z = SPLIT ? 1 : 0; z >= 0; --z) {
-              const uint4* p = reinterpret_cast<const uint4*>(q_s + ((size_t)z * w.chunk + 8 * g + gid) * S::kQRow + 64 * j + 16 * tig);
-              const uint4 x = p[0], y = p[1];
+              uint4 x, y;
+              if constexpr (ONE) {
+                x = q_one[z][j][0];
+                y = q_one[z][j][1];
+              } else {
+                const uint4* p = reinterpret_cast<const uint4*>(q_s + ((size_t)z * w.chunk + 8 * g + gid) * S::kQRow + 64 * j + 16 * tig);
+                x = p[0];
+                y = p[1];
+              }
               float part[NB][4];
 #pragma unroll
-              for (int b = 0; b < NB; ++b) part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
+              for (int b = 0; b < NB; ++b) {
+                part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
+                uint4 k0, k1;
+                if constexpr (ONE) codes(b, j, &k0, &k1);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-                  mma_f16(part[b], k[b][4 * j + e][0], k[b][4 * j + e][1], k[b][4 * j + e][2], k[b][4 * j + e][3],
-                          e < 2 ? word(x, 2 * e) : word(y, 2 * e - 4), e < 2 ? word(x, 2 * e + 1) : word(y, 2 * e - 3));
+                for (int e = 0; e < 4; ++e) {
+                  uint32_t f[4];
+                  if constexpr (ONE)
+                    operand(k0, k1, e, f);
+                  else
+                    f[0] = k[b][4 * j + e][0], f[1] = k[b][4 * j + e][1], f[2] = k[b][4 * j + e][2], f[3] = k[b][4 * j + e][3];
+                  mma_f16(part[b], f[0], f[1], f[2], f[3], e < 2 ? word(x, 2 * e) : word(y, 2 * e - 4),
+                          e < 2 ? word(x, 2 * e + 1) : word(y, 2 * e - 3));
+                }
+              }
 #pragma unroll
               for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -232,6 +271,7 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
             }
           }
         }
+        if constexpr (ONE) next_copies();
         float v = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -250,22 +290,28 @@ weights_kernel(const __grid_constant__ WeightArgs w) {
   unseen_places<D>(w);
 }
 
-template <int D, int FMT, bool SPLIT>
-crvq_status launch(WeightArgs& w, cudaStream_t stream) {
+template <int D, int FMT, bool SPLIT, bool ONE>
+crvq_status launch(WeightArgs& w, int64_t cols, cudaStream_t stream) {
   using S = WShape<D>;
-  auto kernel = weights_kernel<D, FMT, SPLIT>;
-  const AttendArgs& a = w.a;
-  // columns of a sequence, by the average where the rows' offsets are on the device
-  const int64_t cols = a.rows.off ? 2 * ceil_div(a.rows.n_tok * a.group, a.c.n_seq) : (int64_t)a.rows.per * a.group;
+  auto kernel = weights_kernel<D, FMT, SPLIT, ONE>;
   w.chunk = (int)min((int64_t)S::kMost, ceil_div(max(cols, (int64_t)1), 8) * 8);
   const size_t smem = S::smem(w.chunk, SPLIT);
   CRVQ_TRY(smem_limit((const void*)kernel, smem));
   const int per_sm = max(1, min(D == 256 ? 2 : 3, (int)(233472 / (smem + 1024))));
   w.a.shares = sm_count() * per_sm;
-  ProfScope ps("cache_weights", stream, (double)a.rows.n_tok * a.q.heads * D);
+  ProfScope ps("cache_weights", stream, (double)w.a.rows.n_tok * w.a.q.heads * D);
   CRVQ_CUDA(launch_pdl(kernel, dim3((unsigned)w.a.shares), dim3(kThreads), smem, stream, w));
   CRVQ_LAUNCHED();
   return CRVQ_OK;
+}
+
+template <int D, int FMT, bool SPLIT>
+crvq_status pick_columns(WeightArgs& w, cudaStream_t stream) {
+  // columns of a sequence, by the average where the rows' offsets are on the device (a chunk then, several where there are more)
+  const AttendArgs& a = w.a;
+  const int64_t cols = a.rows.off ? 2 * ceil_div(a.rows.n_tok * a.group, a.c.n_seq) : (int64_t)a.rows.per * a.group;
+  if (a.rows.n_tok * a.group <= 8 * (int64_t)a.c.n_seq) return launch<D, FMT, SPLIT, true>(w, min(cols, (int64_t)8), stream);
+  return launch<D, FMT, SPLIT, false>(w, cols, stream);
 }
 
 // Columns per sequence, on average, from which tokens are the rows of tcgen05 tiles (weights_tc.cu).
@@ -275,8 +321,8 @@ template <int D>
 crvq_status pick(WeightArgs& w, int format, cudaStream_t stream) {
   const bool split = w.a.q.type == CRVQ_F32;
   if (format == CRVQ_KV_INT8)
-    return split ? launch<D, CRVQ_KV_INT8, true>(w, stream) : launch<D, CRVQ_KV_INT8, false>(w, stream);
-  return split ? launch<D, CRVQ_KV_E4M3, true>(w, stream) : launch<D, CRVQ_KV_E4M3, false>(w, stream);
+    return split ? pick_columns<D, CRVQ_KV_INT8, true>(w, stream) : pick_columns<D, CRVQ_KV_INT8, false>(w, stream);
+  return split ? pick_columns<D, CRVQ_KV_E4M3, true>(w, stream) : pick_columns<D, CRVQ_KV_E4M3, false>(w, stream);
 }
 
 crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_tok, const int32_t* q_off, float scale,
