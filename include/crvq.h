@@ -617,7 +617,7 @@ typedef struct crvq_token_sums {
  * that crvq_cache_attention returned for the same queries, scale, causal and window. Tokens 0 .. lens[b] of every sequence
  * get their sums (without queries: decay * before), the places behind them 0.
  *   lse     [n_tok x q->heads] fp32; a query with an infinite lse (one that sees nothing) adds nothing.
- *   before  or NULL: zeros. The same memory as out, or none that it shares. Finite decay.
+ *   before  or NULL: zeros. The same memory as out (with the same strides), or memory apart from it. Finite decay.
  * Both have the same width; tokens at or behind it have no sum and are reported as CRVQ_ERR_DEVICE by crvq_sync.
  * Scores and sums are fp32 (products as in crvq_cache_attention), every sum in one fixed order.
  */
@@ -635,7 +635,7 @@ crvq_status crvq_cache_weights(const crvq_kv_cache* cache, const crvq_heads* q, 
  *   idx     [n_seq x n_kv x keep] int32: the places that stay, in order; -1 behind the last.
  *   count   [n_seq] int32: min(lens[b], keep), the tokens that stay.
  *   weights_out  or NULL: the weights of those tokens, in their order, and 0 behind them; at least min(keep,
- *                weights->width) wide. Shares no memory with weights.
+ *                weights->width) wide. Memory apart from weights'.
  */
 crvq_status crvq_cache_select(const crvq_token_sums* weights, const int32_t* lens, int32_t n_seq, int32_t n_kv,
                               int32_t keep, int32_t first, int32_t recent, int32_t* idx, int32_t* count,

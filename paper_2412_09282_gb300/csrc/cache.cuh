@@ -59,6 +59,7 @@ crvq_status make_heads(const crvq_heads* h, const char* name, int head_dim, int6
 crvq_status make_rows(const int32_t* off, int64_t n_tok, int n_seq, RowsView* out);
 // (weights.cu)
 crvq_status check_sums(const crvq_token_sums* s, const char* name, int n_seq, int n_kv);
+bool sums_overlap(const crvq_token_sums* x, const crvq_token_sums* y, int n_seq, int n_kv);  // from the first to the last element
 
 inline size_t type_bytes(int type) { return type == CRVQ_F32 ? 4 : 2; }
 

@@ -330,6 +330,7 @@ crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t 
   SelectArgs a{};
   CRVQ_CHECK_ARG(n_seq >= 1 && n_kv >= 1, "need n_seq, n_kv >= 1");
   CRVQ_TRY(check_sums(weights, "weights", n_seq, n_kv));
+  CRVQ_CHECK_ARG(weights->width < ((int64_t)1 << 31) - (1 << 16), "weights: width must be below 2^31 - 2^16");
   CRVQ_CHECK_ARG(keep >= 1, "keep must be >= 1");
   CRVQ_CHECK_ARG(first >= 0 && recent >= 0 && (int64_t)first + recent <= keep, "first and recent must be >= 0 and fit in keep");
   CRVQ_CHECK_ARG(lens && idx && count, "lens, idx and count must not be NULL");
@@ -338,10 +339,7 @@ crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t 
   if (weights_out) {
     CRVQ_TRY(check_sums(weights_out, "weights_out", n_seq, n_kv));
     CRVQ_CHECK_ARG(weights_out->width >= min((int64_t)keep, weights->width), "weights_out is too narrow for keep weights a row");
-    auto end = [&](const crvq_token_sums* s) {
-      return s->data + (n_seq > 1 ? (n_seq - 1) * s->ld_seq : 0) + (n_kv > 1 ? (n_kv - 1) * s->ld_head : 0) + s->width;
-    };
-    CRVQ_CHECK_ARG(end(weights_out) <= weights->data || end(weights) <= weights_out->data, "weights_out and weights share memory");
+    CRVQ_CHECK_ARG(!sums_overlap(weights, weights_out, n_seq, n_kv), "weights_out and weights share memory");
     a.w_out = weights_out->data;
     a.out_seq = weights_out->ld_seq;
     a.out_head = weights_out->ld_head;

@@ -338,8 +338,8 @@ crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_t
   if (before) {
     CRVQ_TRY(check_sums(before, "before", w.a.c.n_seq, w.a.c.n_kv));
     CRVQ_CHECK_ARG(before->width == out->width, "before and out differ in width");
-    CRVQ_CHECK_ARG(before->data != out->data || (before->ld_seq == out->ld_seq && before->ld_head == out->ld_head),
-                   "before and out share memory with different strides");
+    const bool same = before->data == out->data && before->ld_seq == out->ld_seq && before->ld_head == out->ld_head;
+    CRVQ_CHECK_ARG(same || !sums_overlap(before, out, w.a.c.n_seq, w.a.c.n_kv), "before and out share memory, but are not the same");
     w.before = before->data;
     w.before_seq = before->ld_seq;
     w.before_head = before->ld_head;
@@ -361,6 +361,13 @@ crvq_status weights(const crvq_kv_cache* cache, const crvq_heads* q, int64_t n_t
 }
 
 }  // namespace
+
+bool sums_overlap(const crvq_token_sums* x, const crvq_token_sums* y, int n_seq, int n_kv) {
+  auto end = [&](const crvq_token_sums* s) {
+    return s->data + (n_seq > 1 ? (n_seq - 1) * s->ld_seq : 0) + (n_kv > 1 ? (n_kv - 1) * s->ld_head : 0) + s->width;
+  };
+  return x->data < end(y) && y->data < end(x);
+}
 
 crvq_status check_sums(const crvq_token_sums* s, const char* name, int n_seq, int n_kv) {
   CRVQ_CHECK_ARG(s != nullptr && s->data != nullptr, "%s is NULL", name);
