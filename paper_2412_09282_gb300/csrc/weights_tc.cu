@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
       tc::mbar_init(tc::smem_u32(&all_done[i]), 1);
     }
     tc::mbar_init(tc::smem_u32(&q_full), 256);
-    tc::mbar_init(tc::smem_u32(&q_read), 256);
+    tc::mbar_init(tc::smem_u32(&q_read), 256 + 2);  // (and the issuing warps, one of which may have no tile: neither falls a filling behind)
     dead_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -350,6 +350,8 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
           }
           commit(&k_empty[X]);
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&q_read));
       }
     }
     __syncwarp();
