@@ -4,13 +4,16 @@
 // A row's k-th largest weight is found digit by digit (11, 7, 7 and 7 bits, from the top) over keys whose unsigned order
 // is the weights': a histogram of the keys that agree so far, and the bin in which the count from the top passes k. (The
 // first digit splits a row's few powers of two. After it every bin would be in use; adding 2048 of them to the other CTAs'
-// takes as long as one more digit.) The row
-// is then gone through once more: a token stays when its key is above the threshold, or equal to it and among the first
-// that are still needed; its new place is the number of such tokens before it. All counts are whole numbers, so results
-// do not depend on timing.
+// takes as long as one more digit.) Every warp lists its keys in the first digit's bin, a few in a hundred, and goes by its
+// list from there on. The row is then gone through once more: a token stays when its key is above the threshold, or equal to
+// it and among the first that are still needed; its new place is the number of such tokens before it. All counts are
+// whole numbers, so results do not depend on timing.
 //   A row is the work of a cluster of 1, 2, 4 or 8 CTAs, each of which holds an equal run of neighbouring tokens in shared
-// memory (it is read from global memory once) and every warp of it an equal run of those, 128 tokens at a time. Histograms and counts are joined by adding them to every CTA's shared memory: one barrier a digit, and nothing is
-// read across CTAs.
+// memory (it is read from global memory once) and every warp of it an equal run of those, 128 tokens at a time. Histograms
+// and counts are joined by adding them to every CTA's shared memory: one barrier a digit, and nothing is read across CTAs.
+//   What bounds it: 32 rows of 131072 tokens take 22 us, of which reading and writing are 5. A CTA's 40000 cycles are, by
+// clocks read in the kernel, 15% loading, 15% the first histogram, 15% the lists, 35% joining and searching four digits (six
+// barriers of the cluster), 20% the last pass: instructions of 32 warps, and barriers.
 #include "cache.cuh"
 #include "kernels.h"
 
@@ -21,8 +24,9 @@ namespace {
 constexpr int kBins = 2048, kBinRows = kBins / 32;  // of the first digit
 constexpr int kFew = 128;                           // of the others
 constexpr int kMaxWarps = 32;
-constexpr int kStep = 128;  // tokens of a warp at a time, a lane's four neighbours
+constexpr int kLogStep = 7, kStep = 1 << kLogStep;  // tokens of a warp at a time, a lane's four neighbours
 constexpr int kStageMax = 44 * 1024;  // weights that a CTA holds in shared memory (more are read again)
+constexpr int kCandidates = 128;      // of a warp, in shared memory (a warp with more goes through all its tokens)
 
 struct SelectArgs {
   const float* w;
@@ -73,12 +77,14 @@ struct alignas(16) SelectShared {
 // row of equal weights) one lane adds for them.
 __device__ __forceinline__ void count_keys(uint32_t* hist, const uint32_t bin[4], const bool in[4]) {
   const uint32_t b0 = __shfl_sync(0xffffffffu, bin[0], 0);
-  bool same = true;
+  if (__all_sync(0xffffffffu, in[0] && bin[0] == b0)) {
+    bool same = true;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) same = same && in[e] && bin[e] == b0;
-  if (__all_sync(0xffffffffu, same)) {
-    if ((threadIdx.x & 31) == 0) atomicAdd(hist + b0, 128u);
-    return;
+    for (int e = 1; e < 4; ++e) same = same && in[e] && bin[e] == b0;
+    if (__all_sync(0xffffffffu, same)) {
+      if ((threadIdx.x & 31) == 0) atomicAdd(hist + b0, 128u);
+      return;
+    }
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -88,9 +94,10 @@ __device__ __forceinline__ void count_keys(uint32_t* hist, const uint32_t bin[4]
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_constant__ SelectArgs a) {
   extern __shared__ __align__(16) char sm[];
   SelectShared& s = *reinterpret_cast<SelectShared*>(sm);
-  uint32_t* keys = reinterpret_cast<uint32_t*>(sm + sizeof(SelectShared));
-  pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  uint32_t* cand = reinterpret_cast<uint32_t*>(sm + sizeof(SelectShared)) + warp * kCandidates;
+  uint32_t* keys = reinterpret_cast<uint32_t*>(sm + sizeof(SelectShared)) + warps * kCandidates;
+  pdl_wait();
   const int size = 1 << a.log_cluster, rank = blockIdx.x & (size - 1), row = blockIdx.x >> a.log_cluster;
   const int b = row / a.n_kv, h = row - b * a.n_kv;
   auto scan = [&](uint32_t v) {  // sums of the lanes up to this one
@@ -107,7 +114,6 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
     else
       asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  for (int i = tid; i < (size > 1 ? 2 : 1) * (kBins + 3 * kFew); i += blockDim.x) s.hist[i] = 0;
   int len = __ldg(a.lens + b);
   if (len < 0 || len > a.width) {
     raise_error(a.err, ERRBIT_INDEX);
@@ -118,17 +124,34 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   const int lo = a.first, hi = len - a.recent;  // tokens [lo, hi) are those between the first and the most recent ones
   const float* w = a.w + b * a.w_seq + h * a.w_head;
   // this CTA's tokens, this warp's
-  const int per_cta = (int)(((int64_t)len + kStep * size - 1) / (kStep * size)) * kStep;
+  const int per_cta = (int)(((uint32_t)len + (uint32_t)(kStep * size) - 1) >> (kLogStep + a.log_cluster)) * kStep;
   const int c_begin = (int)min((int64_t)len, (int64_t)rank * per_cta), c_end = min(len, c_begin + per_cta);
   const int per_warp = (c_end - c_begin + kStep * warps - 1) / (kStep * warps) * kStep;
   const int begin = min(c_end, c_begin + warp * per_warp), end = min(c_end, begin + per_warp);
   const bool staged = per_cta <= a.staged;
-  __syncthreads();
+  // all of a warp's weights on their way at once
+  if (staged) {
+    for (int t = begin + 4 * lane; t < end; t += kStep) {
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(keys + (t - c_begin));
+      if (a.vec && t + 3 < end) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(w + t) : "memory");
+      } else {
+        for (int e = 0; e < 4 && t + e < end; ++e)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 4 * e), "l"(w + t + e) : "memory");
+      }
+    }
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  for (int i = tid; i < (size > 1 ? 2 : 1) * (kBins + 3 * kFew); i += blockDim.x) s.hist[i] = 0;
 
-  // keys of the tokens t .. t + 3, 0 behind the last
-  auto load_keys = [&](int t, uint32_t key[4]) {
+  // keys of a warp's tokens t0 .. t0 + 127, four of a lane; 0 behind the last
+  auto load_keys = [&](int t0, uint32_t key[4]) {
+    const int t = t0 + 4 * lane;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (a.vec && t + 3 < end) {
+    if (staged) {  // (each lane reads what it copied; behind `end` anything)
+      const float4 v = *reinterpret_cast<const float4*>(keys + (t - c_begin));
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else if (a.vec && t + 3 < end) {
       const float4 v = __ldg(reinterpret_cast<const float4*>(w + t));
       x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
     } else {
@@ -137,33 +160,22 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
         if (t + e < end) x[e] = __ldg(w + t + e);
     }
 #pragma unroll
+    for (int e = 0; e < 4; ++e) key[e] = order_key(x[e]);
+    if (find && t0 >= lo && t0 + kStep <= min(hi, end)) return;
+#pragma unroll
     for (int e = 0; e < 4; ++e) {
-      key[e] = t + e < lo || t + e >= hi || !find ? kAlways : order_key(x[e]);
+      if (t + e < lo || t + e >= hi || !find) key[e] = kAlways;
       if (t + e >= end) key[e] = 0;
     }
   };
-  auto at = [&](int t, uint32_t key[4]) {
+  auto at = [&](int t0, uint32_t key[4]) {
     if (staged) {
-      const uint4 v = *reinterpret_cast<const uint4*>(keys + (t - c_begin));
+      const uint4 v = *reinterpret_cast<const uint4*>(keys + (t0 + 4 * lane - c_begin));
       key[0] = v.x; key[1] = v.y; key[2] = v.z; key[3] = v.w;
     } else {
-      load_keys(t, key);
+      load_keys(t0, key);
     }
   };
-#pragma unroll 4
-  for (int t0 = begin; t0 < end; t0 += kStep) {
-    const int t = t0 + 4 * lane;
-    uint32_t key[4], bin[4];
-    bool in[4];
-    load_keys(t, key);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bin[e] = key[e] >> 21;
-      in[e] = key[e] != 0;
-    }
-    if (staged) *reinterpret_cast<uint4*>(keys + (t - c_begin)) = make_uint4(key[0], key[1], key[2], key[3]);
-    if (find) count_keys(size > 1 ? s.mine : s.hist, bin, in);
-  }
   // places behind the last token that stays
   if (a.w_out) {
     float* out = a.w_out + b * a.out_seq + h * a.out_head;
@@ -181,7 +193,25 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   for (int t = count + rank * (int)blockDim.x + tid; t < a.keep; t += size * (int)blockDim.x) idx[t] = -1;
   if (h == 0 && rank == 0 && tid == 0) a.count[b] = count;
 
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();  // (counts are zeros)
+  for (int t0 = begin; t0 < end; t0 += kStep) {
+    uint32_t key[4], bin[4];
+    bool in[4];
+    load_keys(t0, key);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bin[e] = key[e] >> 21;
+      in[e] = key[e] != 0;
+    }
+    if (staged) *reinterpret_cast<uint4*>(keys + (t0 + 4 * lane - c_begin)) = make_uint4(key[0], key[1], key[2], key[3]);
+    if (find) count_keys(size > 1 ? s.mine : s.hist, bin, in);
+  }
+
   uint32_t need = (uint32_t)a.keep, threshold = kAlways - 1;  // (all stay for certain)
+  uint32_t sure = 0, equal = 0;  // this warp's tokens that stay for certain, and those at the threshold (of a lane, at first)
+  bool listed = false;           // all of this warp's tokens in the first digit's bin are in its list
+  const uint32_t below = (1u << lane) - 1;
   if (find) {
     if (size > 1) {  // to everyone
       sync_all();    // (whose counts are zeros by then)
@@ -212,17 +242,37 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
       prefix = 32 * r + 31 - at_lane;
       need -= __shfl_sync(0xffffffffu, in_row - v, at_lane);
     }
+    // the other digits go by the tokens in that bin alone, a few in a hundred: their keys, in any order
+    int n_cand = 0;
+    for (int t0 = begin; t0 < end; t0 += kStep) {
+      uint32_t key[4];
+      at(t0, key);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t digit = key[e] >> 21;
+        sure += digit > prefix;
+        const uint32_t all = __ballot_sync(0xffffffffu, digit == prefix && key[e] != 0);
+        const int place = n_cand + __popc(all & below);
+        if ((all >> lane & 1) && place < kCandidates) cand[place] = key[e];
+        n_cand += __popc(all);
+      }
+    }
+    listed = n_cand <= kCandidates;
+    __syncwarp();
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = 14 - 7 * pass;
       uint32_t* few = size > 1 ? s.mine_few[pass] : s.few[pass];
-      for (int t0 = begin; t0 < end; t0 += kStep) {
+      if (listed)
+        for (int i = lane; i < n_cand; i += 32)
+          if (cand[i] >> (shift + 7) == prefix) atomicAdd(few + (cand[i] >> shift & (kFew - 1)), 1u);
+      for (int t0 = listed ? end : begin; t0 < end; t0 += kStep) {
         uint32_t key[4], bin[4];
         bool in[4];
-        at(t0 + 4 * lane, key);
+        at(t0, key);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          in[e] = key[e] >> (shift + 7) == prefix;
+          in[e] = key[e] >> (shift + 7) == prefix && key[e] != 0;
           bin[e] = key[e] >> shift & (kFew - 1);
         }
         if (__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) count_keys(few, bin, in);
@@ -255,14 +305,17 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
       need -= __shfl_sync(0xffffffffu, above, hit);
     }
     threshold = prefix;
+    for (int i = lane; listed && i < n_cand; i += 32) {
+      sure += cand[i] > threshold;
+      equal += cand[i] == threshold;
+    }
   }
 
   if (size > 1 && !find) sync_all();  // (every CTA is there)
-  // this warp's tokens that stay for certain, and those at the threshold
-  uint32_t sure = 0, equal = 0;
-  for (int t0 = begin; t0 < end; t0 += kStep) {
+  if (!listed) sure = 0;
+  for (int t0 = listed ? end : begin; t0 < end; t0 += kStep) {
     uint32_t key[4];
-    at(t0 + 4 * lane, key);
+    at(t0, key);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       sure += key[e] > threshold;
@@ -298,29 +351,42 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
     equal += s.equal[c];
   }
   float* out = a.w_out ? a.w_out + b * a.out_seq + h * a.out_head : nullptr;
+  uint32_t staying = sure + min(equal, need);  // before the warp's next tokens
   for (int t0 = begin; t0 < end; t0 += kStep) {
     const int t = t0 + 4 * lane;
-    uint32_t key[4], n = 0;  // (sure ones in the low half, equal ones in the high half)
-    at(t, key);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) n += (key[e] > threshold ? 1u : 0u) + (key[e] == threshold ? 1u << 16 : 0u);
-    if (!__any_sync(0xffffffffu, n != 0)) continue;
-    uint32_t sum = scan(n);
-    uint32_t my_sure = sure + ((sum - n) & 0xffffu), my_equal = equal + ((sum - n) >> 16);
+    uint32_t key[4], flags = 0, equals = 0;  // a bit per token of this lane
+    at(t0, key);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool is_sure = key[e] > threshold, is_equal = key[e] == threshold;
-      const uint32_t place = my_sure + min(my_equal, need);
-      if ((is_sure || (is_equal && my_equal < need)) && place < (uint32_t)count) {
-        idx[place] = t + e;
-        if (out) out[place] = key[e] < kNan ? weight_of(key[e]) : __ldg(w + t + e);
-      }
-      my_sure += is_sure;
-      my_equal += is_equal;
+      flags |= key[e] > threshold ? 1u << e : 0u;
+      equals |= key[e] == threshold ? 1u << e : 0u;
     }
-    sum = __shfl_sync(0xffffffffu, sum, 31);
-    sure += sum & 0xffffu;
-    equal += sum >> 16;
+    if (__any_sync(0xffffffffu, equals != 0)) {  // the first of them stay, too
+      uint32_t mine = equal;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t all = __ballot_sync(0xffffffffu, equals >> e & 1);
+        mine += __popc(all & below);
+        equal += __popc(all);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (equals >> e & 1 && mine++ < need) flags |= 1u << e;
+    }
+    uint32_t place = staying;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t all = __ballot_sync(0xffffffffu, flags >> e & 1);
+      place += __popc(all & below);
+      staying += __popc(all);
+    }
+    for (; flags; flags &= flags - 1, ++place) {  // (few tokens stay: most lanes have none or one)
+      const int e = __ffs(flags) - 1;
+      const uint32_t k = e < 2 ? (e ? key[1] : key[0]) : (e == 2 ? key[2] : key[3]);
+      if (place >= (uint32_t)count) break;
+      idx[place] = t + e;
+      if (out) out[place] = k < kNan ? weight_of(k) : __ldg(w + t + e);
+    }
   }
 }
 
@@ -359,16 +425,23 @@ crvq_status select(const crvq_token_sums* weights, const int32_t* lens, int32_t 
   a.recent = recent;
   CRVQ_TRY(device_error_word(&a.err));
   const int64_t units = (int64_t)n_seq * n_kv;
+  // CTAs of a row: as many as hold it in shared memory; twice as many while each is left an SM of its own and 2048 tokens
+  // (1, 2, 4, 8 CTAs, us: 32 rows of 131072 tokens 79, 46, 22, 33; 8 such rows 79, 46, 23, 16; 64 of 16384 14, 13, 17, 19;
+  // 512 of 16384 46, 66, 108, 118; 8 of 8192 10.2, 11.0, 9.1, 9.6; 8 of 4096 8.3, 8.8, 8.9, 11.0)
   int size = 1;
-  while (size < 8 && a.width > (int64_t)4096 * size) {
+  while (size < 8 && (a.width > (int64_t)kStageMax * size ||
+                      (units * size * 2 <= sm_count() && a.width > 4096 && a.width > (int64_t)2048 * size))) {
     size *= 2;
     ++a.log_cluster;
   }
   if (units * size >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many sequences and heads in one call");
   const int64_t per_cta = ceil_div(a.width, kStep * size) * kStep;
-  const int threads = 32 * (int)min((int64_t)kMaxWarps, max((int64_t)4, ceil_div(per_cta, 128)));
+  // 128 tokens a warp, or 512 where SMs have several CTAs, one after another: every warp searches the digits' counts (128, 256,
+  // 512, 1024 tokens a warp, us: 2048 rows of 4096 tokens 81, 52, 41, 42; 512 of 4096 25, 17, 14, 15; 8 of 1001 6.1, 7.5)
+  const int steps = units * size > sm_count() ? 4 : 1;
+  const int threads = 32 * (int)min((int64_t)kMaxWarps, max((int64_t)4, ceil_div(per_cta, kStep * steps)));
   a.staged = (int)min(per_cta, (int64_t)kStageMax);
-  const size_t smem = sizeof(SelectShared) + (size_t)a.staged * sizeof(float);
+  const size_t smem = sizeof(SelectShared) + (size_t)(threads * (kCandidates / 32) + a.staged) * sizeof(float);
   CRVQ_TRY(smem_limit((const void*)select_kernel, smem));
   ProfScope ps("cache_select", stream, (double)units * a.width);
   cudaLaunchAttribute attr[2];

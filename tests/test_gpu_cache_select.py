@@ -159,3 +159,20 @@ def test_a_captured_call_replays_with_new_weights_and_lengths():
         P.crvq_sync()
         ref, rc, _ = C.select(x, n, 700, 4, 9)
         assert np.array_equal(idx.cpu().numpy(), ref) and np.array_equal(count.cpu().numpy(), rc)
+
+
+@pytest.mark.parametrize("rows,width", [((1, 1), 3000), ((3, 70), 3001), ((2, 2), 30000), ((40, 4), 9001), ((1, 1), 400000)])
+def test_weights_that_share_their_first_digits(rows, width):
+    """Keys that agree in 11, 18 and 25 bits, more of them than a warp lists, beside rows where few do; of every number of
+    tokens a warp takes (rows of SMs to themselves, and several on one)."""
+    rng = np.random.default_rng(140)
+    w = np.empty(rows + (width,), np.float32)
+    flat = w.reshape(-1, width)
+    for r in range(flat.shape[0]):
+        near = [0.2, 2.0 ** -10, 2.0 ** -17, 2.0 ** -22, 0.0, 8.0][r % 6]
+        flat[r] = (1 + near * rng.random(width)).astype(np.float32)
+        if r % 4 == 3:
+            flat[r, rng.integers(0, width, width // 3)] *= np.float32(0.01)
+    lens = [width - 17 * b for b in range(rows[0])]
+    for keep, first, recent in ((1000, 0, 0), (1500, 3, 200)):
+        _check(w, lens, keep, first, recent)
