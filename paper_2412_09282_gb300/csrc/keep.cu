@@ -50,6 +50,21 @@ struct KeepTile {
   float scale[kTokens / kCacheBlock];
 };
 
+// (x - 8388736) * ratio + 12582912 of two numbers, each operation rounded, as bits.
+__device__ __forceinline__ void scale2(uint32_t x, uint32_t y, float ratio, uint32_t& rx, uint32_t& ry) {
+  asm("{\n.reg .b64 v, f, c;\n"
+      "mov.b64 v, {%2, %3};\n"
+      "mov.b64 f, {%4, %4};\n"
+      "mov.b64 c, {%5, %5};\n"
+      "add.rn.f32x2 v, v, c;\n"
+      "mul.rn.f32x2 v, v, f;\n"
+      "mov.b64 c, {%6, %6};\n"
+      "add.rn.f32x2 v, v, c;\n"
+      "mov.b64 {%0, %1}, v;\n}"
+      : "=r"(rx), "=r"(ry)
+      : "r"(x), "r"(y), "f"(ratio), "f"(-8388736.f), "f"(12582912.f));
+}
+
 // Looking a token up takes three loads one after another (its place, its page, its scale), so a tile's begin three rounds ahead:
 // in every round one step of three tiles is on its way beside the present tile's codes.
 template <int D, int FMT, bool IN_PLACE>
@@ -185,17 +200,21 @@ __global__ void __launch_bounds__(kKeepThreads, 3) keep_kernel(const __grid_cons
       } else if (ratio != 1.f) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v[4];
-          if constexpr (FMT == CRVQ_KV_INT8) {  // 2^23 + code + 128, less 2^23 + 128: exact, without conversions
+          if constexpr (FMT == CRVQ_KV_INT8) {
+            // 2^23 + code + 128, less 2^23 + 128: exact, without conversions; adding 1.5 * 2^23 rounds to an integer
             const uint32_t x = w[e] ^ 0x80808080u;
+            uint32_t r[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = __fsub_rn(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + k)), 8388736.f);
+            for (int k = 0; k < 4; k += 2)
+              scale2(__byte_perm(x, 0x4b000000u, 0x7440 + k), __byte_perm(x, 0x4b000000u, 0x7441 + k), ratio, r[k], r[k + 1]);
+            w[e] = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
           } else {
+            float v[4];
             decode4<FMT>(w[e], v);
-          }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = __fmul_rn(v[k], ratio);
-          w[e] = encode4<FMT, true>(v);
+            for (int k = 0; k < 4; ++k) v[k] = __fmul_rn(v[k], ratio);
+            w[e] = encode4<FMT, true>(v);
+          }
         }
       }
       *reinterpret_cast<uint4*>(to + tile.dst[block] + (i % kCacheBlock) * D + 16 * col) = make_uint4(w[0], w[1], w[2], w[3]);
