@@ -5,7 +5,8 @@
 // memory while the tiles of a (sequence, kv head) pass. Codes become operands of the queries' type, exactly: no query needs
 // a factor.
 // Two groups of four warps take every other tile, each with its own half of tensor memory and its own issuing warp; four warps
-// turn codes into operands. While one group's exponentials run, the other's products do.
+// turn codes into operands. While one group's exponentials run, the other's products do, and its own next 128 columns' (two
+// of 64 queries over up to 32768 tokens, 64 heads on 8: 92.8 -> 90.6 us).
 // Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; every token is one thread's.
 #include "attend_tc.cuh"
 #include "weights.cuh"
@@ -14,7 +15,7 @@ namespace crvq {
 
 namespace {
 
-constexpr int kMostCols = 512, kHalfCols = 256;
+constexpr int kMostCols = 512, kStepCols = 128;  // a group's two halves of its 256 columns of tensor memory
 constexpr int kWtThreads = 14 * 32;
 
 template <int D>
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   using S = WtShape<D>;
   const AttendArgs& a = w.a;
   extern __shared__ __align__(128) char sm[];
-  __shared__ __align__(8) uint64_t k_full[2], k_empty[2], s_full[2], s_empty[2], q_full, q_read, all_done[2];
+  __shared__ __align__(8) uint64_t k_full[2], k_empty[2], s_full[2][2], s_empty[2][2], q_full, q_read, all_done[2];
   __shared__ float sk_s[2][8];
   __shared__ int live_s[2][8];
   __shared__ uint32_t tmem_slot;
@@ -90,13 +91,15 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   float* l_s = reinterpret_cast<float*>(k_sm + 2 * S::kSide);  // [kMostCols] -lse, first and last + 1 key seen
   int* kb_s = reinterpret_cast<int*>(l_s + kMostCols);
   int* ke_s = kb_s + kMostCols;
-  if (warp == 12) tc::tmem_alloc(&tmem_slot, 2 * kHalfCols);
+  if (warp == 12) tc::tmem_alloc(&tmem_slot, 4 * kStepCols);
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(tc::smem_u32(&k_full[i]), 128);
       tc::mbar_init(tc::smem_u32(&k_empty[i]), 1 + 4);  // the products, and the group's warps (scales)
-      tc::mbar_init(tc::smem_u32(&s_full[i]), 1);
-      tc::mbar_init(tc::smem_u32(&s_empty[i]), 128);
+      for (int j = 0; j < 2; ++j) {
+        tc::mbar_init(tc::smem_u32(&s_full[i][j]), 1);
+        tc::mbar_init(tc::smem_u32(&s_empty[i][j]), 128);
+      }
       tc::mbar_init(tc::smem_u32(&all_done[i]), 1);
     }
     tc::mbar_init(tc::smem_u32(&q_full), 256);
@@ -135,7 +138,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   if (warp < 8) {
     // ------------------------------------------------------------------ exponentials: thread = token of every other tile
     const int X = warp >> 2, row = tid & (kKeys - 1);
-    const uint32_t s_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + X * kHalfCols;
+    const uint32_t s_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + X * 2 * kStepCols;
     uint32_t s_no = 0;
     while (ok && next_part()) {
       const int len = u.s.len, held = len - u.s.n;
@@ -214,14 +217,15 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
           const float g = w.scale * sk;
           const uint64_t g2 = pair(g, g), log2e = pair(kLog2e, kLog2e);
           uint64_t sum[4] = {0, 0, 0, 0};
-          for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
-            if (!wait(&s_full[X], s_no & 1)) break;
+          for (int h0 = 0; h0 < n_pad; h0 += kStepCols, ++s_no) {
+            const int half = s_no & 1;
+            if (!wait(&s_full[X][half], (s_no >> 1) & 1)) break;
             tc::tc_fence_after();
-            const int n = min(kHalfCols, n_pad - h0);
+            const int n = min(kStepCols, n_pad - h0);
 #pragma unroll 1
             for (int ch = 0; ch < n; ch += 32) {
               float v[32];
-              tc::tmem_ld32(s_at + ch, v);
+              tc::tmem_ld32(s_at + half * kStepCols + ch, v);
               const float* l = l_s + h0 + ch;
               if (whole) {
 #pragma unroll
@@ -244,7 +248,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
               }
             }
             tc::tc_fence_before();
-            tc::mbar_arrive(tc::smem_u32(&s_empty[X]));
+            tc::mbar_arrive(tc::smem_u32(&s_empty[X][half]));
           }
           float x, y;
           halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), x, y);
@@ -339,14 +343,15 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
         for (int i = 0; i < n_tiles && ok; ++i, ++tile_no) {
           if ((int)(tile_no & 1) != X) continue;
           if (!wait(&k_full[X], (tile_no >> 1) & 1)) break;
-          for (int h0 = 0; h0 < n_pad; h0 += kHalfCols, ++s_no) {
-            if (!wait(&s_empty[X], (s_no & 1) ^ 1)) break;
+          for (int h0 = 0; h0 < n_pad; h0 += kStepCols, ++s_no) {
+            const int half = s_no & 1;
+            if (!wait(&s_empty[X][half], ((s_no >> 1) & 1) ^ 1)) break;
             tc::tc_fence_after();
-            const uint32_t idesc = idesc_f16(kKeys, min(kHalfCols, n_pad - h0), false) | (BF16 ? 1u << 7 | 1u << 10 : 0u);
+            const uint32_t idesc = idesc_f16(kKeys, min(kStepCols, n_pad - h0), false) | (BF16 ? 1u << 7 | 1u << 10 : 0u);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
-              mma_ss(tmem + X * kHalfCols, k_desc + ks * 16, q_desc + (h0 * D * 2 + ks * 256) / 16, idesc, ks > 0);
-            commit(&s_full[X]);
+              mma_ss(tmem + (2 * X + half) * kStepCols, k_desc + ks * 16, q_desc + (h0 * D * 2 + ks * 256) / 16, idesc, ks > 0);
+            commit(&s_full[X][half]);
           }
           commit(&k_empty[X]);
         }
@@ -362,7 +367,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
-  if (warp == 12) tc::tmem_dealloc(tmem, 2 * kHalfCols);
+  if (warp == 12) tc::tmem_dealloc(tmem, 4 * kStepCols);
   unseen_places<D>(w);
 }
 
