@@ -10,8 +10,8 @@
 // scales are read by all of them before any is written. Tokens only move towards the front there (idx >= place), so what a
 // later round reads lies behind all that earlier ones have written.
 //   What bounds it: loads in flight, and the instructions that turn codes into others (4 per code). 2047 of up to 8192 tokens of 8
-// sequences, 32 heads, e4m3, into other pages: 60 us, 4.5 TB/s. 16384 of up to 65536 of 2, 8 heads, int8, in place: 41 us,
-// 3.3 TB/s, eight rounds of 5 us (43 without the next round's codes on their way).
+// sequences, 32 heads, e4m3, into other pages: 60 us, 4.5 TB/s. 16384 of up to 65536 of 2, 8 heads, int8, in place: 42 us,
+// 3.2 TB/s, eight rounds of 5 us (46 before a round's codes were on their way beside the writes of the one before).
 #include "cache.cuh"
 #include "kernels.h"
 
@@ -53,19 +53,21 @@ struct KeepTile {
   float scale[kTokens / kCacheBlock];
 };
 
-// (x - 8388736) * ratio + 12582912 of two numbers, each operation rounded, as bits.
+// (x - 8388736) * ratio + 12582912 of two numbers, each operation rounded, as bits. (The last one number by number: a product
+// and a sum of two numbers at a time became one operation with one rounding.)
 __device__ __forceinline__ void scale2(uint32_t x, uint32_t y, float ratio, uint32_t& rx, uint32_t& ry) {
+  float vx, vy;
   asm("{\n.reg .b64 v, f, c;\n"
       "mov.b64 v, {%2, %3};\n"
       "mov.b64 f, {%4, %4};\n"
       "mov.b64 c, {%5, %5};\n"
       "add.rn.f32x2 v, v, c;\n"
       "mul.rn.f32x2 v, v, f;\n"
-      "mov.b64 c, {%6, %6};\n"
-      "add.rn.f32x2 v, v, c;\n"
       "mov.b64 {%0, %1}, v;\n}"
-      : "=r"(rx), "=r"(ry)
-      : "r"(x), "r"(y), "f"(ratio), "f"(-8388736.f), "f"(12582912.f));
+      : "=f"(vx), "=f"(vy)
+      : "r"(x), "r"(y), "f"(ratio), "f"(-8388736.f));
+  rx = __float_as_uint(__fadd_rn(vx, 12582912.f));
+  ry = __float_as_uint(__fadd_rn(vy, 12582912.f));
 }
 
 // Looking a token up takes three loads one after another (its place, its page, its scale), so a tile's begin three rounds ahead:

@@ -215,3 +215,38 @@ def test_refusals():
             P.crvq_cache_keep(gpu, *args)
     with pytest.raises(ValueError):
         P.crvq_cache_keep(gpu, idx, count, start=_ints([0]))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_products_that_round_to_ties(in_place):
+    """int8: c (their scale / its scale) is rounded to fp32, and that to a whole number: where the first rounding ends on
+    k + 1/2 and the exact product does not, one rounding of both would give another code."""
+    import paper_2412_09282_gb300 as P
+    pairs = []
+    for c in range(3, 128):
+        for k in range(c):
+            r = np.float32((k + 0.5) / c)
+            exact = float(r) * c                                 # (31 bits: exact in fp64)
+            if np.float32(c) * r == np.float32(k + 0.5) and exact != k + 0.5 and round(exact) != round(k + 0.5):
+                pairs.append((c, r))
+    assert len(pairs) > 1000
+    pairs = pairs[:1500]
+    blocks = 16 * (len(pairs) // 15)                             # of 16 tokens; every 16th has scale 1
+    host, _ = U.make(150, [16 * blocks], 16, 1, 64, "int8")
+    idx = 16 * np.arange(blocks, dtype=np.int32) + np.random.default_rng(151).integers(0, 16, blocks)
+    idx[:16] = 16 * np.arange(16)
+    at = 0
+    for i in range(blocks):
+        pg = host["pages"][0, i]
+        for name, s in (("K", "k_scale"), ("V", "v_scale")):
+            host[s][pg, 0, 0] = 1.0 if i % 16 == 0 else pairs[at][1]
+            if i % 16:
+                host[name][pg, 0, :, 5::16] = pairs[at][0] if name == "K" else -pairs[at][0]
+        at += i % 16 != 0
+    gpu = U.on_gpu(host, "int8")
+    other, to = (host, gpu) if in_place else U.make(152, [blocks], 32, 1, 64, "int8")
+    ref = {k: v.copy() for k, v in other.items()}
+    C.keep(host, idx[None], [blocks], [0], ref, "int8")
+    P.crvq_cache_keep(gpu, _ints(idx[None]), _ints([blocks]), out=to)
+    P.crvq_sync()
+    _equal(ref, to, "int8")
