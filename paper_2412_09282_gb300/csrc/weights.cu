@@ -10,6 +10,9 @@
 // channels), turns their codes into operands once and goes over all columns with them; up to `chunk` columns' queries lie
 // in shared memory as fp16 relative to a power of two each (two operands from fp32). Blocks are copied ahead into a ring
 // per warp, four steps deep: only keys are read, half of what attention reads.
+//   What bounds it: memory. One token of 64 sequences of up to 4096, 32 heads, e4m3: 113 us, 5.4 TB/s. Alone at 46% of the
+// issue slots (373 instructions per warp and 32 tokens); page numbers looked up a step earlier, and warps without a barrier
+// at a unit's start, left it there (113.5, 112).
 #include "attend_mma.cuh"
 #include "weights.cuh"
 
