@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kKeepThreads, IN_PLACE ? 2 : 3) keep_kernel(co
   if (n == 0) return;  // (with its whole cluster)
   const int len = seq_len(a.from, b, a.err);
   const int base = start / kCacheBlock * kCacheBlock, end = start + n;
-  const int n_tiles = (end - base + S::kTokens - 1) / S::kTokens;
+  const int n_tiles = (int)(((uint32_t)(end - base) + S::kTokens - 1) / S::kTokens);
   // (in place, every CTA of a cluster takes part in every round)
   const int rounds = IN_PLACE ? (n_tiles + a.tiles - 1) / a.tiles : max(0, n_tiles - rank + a.tiles - 1) / a.tiles;
   const int32_t* idx = a.idx + b * a.ld_seq + h * a.ld_head;
@@ -101,9 +101,13 @@ __global__ void __launch_bounds__(kKeepThreads, IN_PLACE ? 2 : 3) keep_kernel(co
   float* to_scale = is_key ? a.to.ks : a.to.vs;
   const int from_blocks = (unsigned)a.from.page / kCacheBlock, to_blocks = (unsigned)a.to.page / kCacheBlock;
   const int col = tid % S::kRow, slot = tid / S::kRow;
-  auto place0 = [&](int round) { return base + (rank + round * a.tiles) * S::kTokens; };
+  // (places go up to 2^31 - 16)
+  auto place0 = [&](int round) { return (int)min((int64_t)end, base + (int64_t)(rank + round * a.tiles) * S::kTokens); };
   // the place that this thread looks up for a round; `end` where there is none
-  auto place = [&](int round) { return tid < S::kTokens && round < rounds ? min(place0(round) + tid, end) : end; };
+  auto place = [&](int round) {
+    const int p0 = place0(round);
+    return tid < S::kTokens && round < rounds && tid < end - p0 ? p0 + tid : end;
+  };
 
   auto find_token = [&](int round) {
     const int p = place(round);
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(kKeepThreads, IN_PLACE ? 2 : 3) keep_kernel(co
 #pragma unroll
     for (int u = 0; u < S::kTimes; ++u) {
       const int i = u * S::kSlots + slot, block = i / kCacheBlock;
-      if (p0 + i >= end || tile.dst[block] < 0) continue;
+      if (i >= end - p0 || tile.dst[block] < 0) continue;
       const float ratio = tile.ratio[i];  // (at most 1; 0 for a token that is none)
       uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
       if (ratio == 0.f) {

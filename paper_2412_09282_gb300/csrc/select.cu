@@ -179,9 +179,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
   // places behind the last token that stays
   if (a.w_out) {
     float* out = a.w_out + b * a.out_seq + h * a.out_head;
-    int64_t t = count + rank * (int)blockDim.x + tid;
+    int64_t t = (int64_t)count + rank * (int)blockDim.x + tid;
     if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0) {  // (up to three before the first group of 16 bytes, and behind the last)
-      const int64_t a0 = (count + 3) / 4, a1 = a.out_width / 4;
+      const int64_t a0 = ((int64_t)count + 3) / 4, a1 = a.out_width / 4;
       for (int64_t g = a0 + rank * (int)blockDim.x + tid; g < a1; g += size * (int)blockDim.x)
         reinterpret_cast<float4*>(out)[g] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (rank == 0 && tid < 4 && count + tid < min(4 * a0, a.out_width)) out[count + tid] = 0.f;
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) select_kernel(const __grid_
     for (; t < a.out_width; t += size * (int)blockDim.x) out[t] = 0.f;
   }
   int32_t* idx = a.idx + (int64_t)row * a.keep;
-  for (int t = count + rank * (int)blockDim.x + tid; t < a.keep; t += size * (int)blockDim.x) idx[t] = -1;
+  for (int64_t t = (int64_t)count + rank * (int)blockDim.x + tid; t < a.keep; t += size * (int)blockDim.x) idx[t] = -1;
   if (h == 0 && rank == 0 && tid == 0) a.count[b] = count;
 
   asm volatile("cp.async.wait_group 0;" ::: "memory");

@@ -176,3 +176,14 @@ def test_weights_that_share_their_first_digits(rows, width):
     lens = [width - 17 * b for b in range(rows[0])]
     for keep, first, recent in ((1000, 0, 0), (1500, 3, 200)):
         _check(w, lens, keep, first, recent)
+
+
+def test_room_for_more_tokens_than_there_can_be():
+    """The largest keep: 2^31 - 1 places a row, -1 behind the last token up to the end."""
+    import paper_2412_09282_gb300 as P
+    w = torch.rand((1, 1, 100), device="cuda")
+    keep = 2 ** 31 - 1
+    idx, count = P.crvq_cache_select(w, _ints([77]), keep)
+    P.crvq_sync()
+    assert count.item() == 77 and torch.equal(idx[0, 0, :77], torch.arange(77, dtype=torch.int32, device="cuda"))
+    assert int(idx[0, 0, 77:].max()) == int(idx[0, 0, 77:].min()) == -1
