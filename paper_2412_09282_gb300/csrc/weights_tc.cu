@@ -9,8 +9,9 @@
 // of 64 queries over up to 32768 tokens, 64 heads on 8: 92.8 -> 90.6 us).
 // Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; every token is one thread's.
 //   What bounds it: the chain from tensor memory to registers, exponentials and sums, 32 columns at a time, of two warps per scheduler
-// (690 TFLOP/s of products; the tensor pipe is active 28% of the time). Slower: four groups of 128 columns (128 us), loads in
-// two buffers (112), one power of two for all columns of fp16 operands (113).
+// (690 TFLOP/s of products; the tensor pipe is active 28% of the time). Slower, in us: four groups of 128 columns 128, loads in
+// two buffers 112 (with 168 registers, and two converting warps for that, 97), an eighth of the exponentials by a polynomial 97,
+// one power of two for all columns of fp16 operands 113.
 #include "attend_tc.cuh"
 #include "weights.cuh"
 
