@@ -250,3 +250,18 @@ def test_products_that_round_to_ties(in_place):
     P.crvq_cache_keep(gpu, _ints(idx[None]), _ints([blocks]), out=to)
     P.crvq_sync()
     _equal(ref, to, "int8")
+
+
+@pytest.mark.parametrize("d,fmt,page", [(64, "int8", 48), (128, "e4m3", 16), (256, "int8", 64)])
+def test_in_place_over_several_rounds_from_the_middle_of_a_block(d, fmt, page):
+    """Rounds whose codes are read while the ones before are written: dense selections (few tokens dropped, sources just
+    behind their places), sparse ones, and a sequence that ends earlier."""
+    import paper_2412_09282_gb300 as P
+    lens, start = [9001, 4100, 9000], [1003, 17, 0]
+    for seed, counts in ((160, [7990, 100, 8999]), (161, [2100, 4083, 1])):
+        host, gpu = U.make(seed, lens, page, 2, d, fmt)
+        idx = _choice(seed + 10, lens, start, counts, 2, True)
+        P.crvq_cache_keep(gpu, _ints(idx), _ints(counts), start=_ints(start))
+        P.crvq_sync()
+        C.keep(host, idx, counts, start, host, fmt)
+        _equal(host, gpu, fmt)
