@@ -298,7 +298,10 @@ crvq_status keep(const crvq_kv_cache* cache, const int32_t* idx, int64_t ld_seq,
                  const int32_t* count, const int32_t* start, const crvq_kv_cache* out, cudaStream_t stream) {
   KeepArgs a{};
   CRVQ_TRY(make_cache(cache, &a.from));
-  CRVQ_TRY(make_cache(out, &a.to));
+  if (out == cache)
+    a.to = a.from;
+  else
+    CRVQ_TRY(make_cache(out, &a.to));
   CRVQ_CHECK_ARG(a.from.n_seq == a.to.n_seq && a.from.n_kv == a.to.n_kv && cache->head_dim == out->head_dim &&
                      cache->format == out->format,
                  "cache and out differ in sequences, kv heads, head_dim or format");

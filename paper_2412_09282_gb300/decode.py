@@ -354,7 +354,9 @@ def crvq_cache_select(weights, lens, keep, first=0, recent=0, weights_out=None, 
             raise ValueError("idx_out must be contiguous n_seq x n_kv x keep")
     if count_out is None:
         count_out = _empty((n_seq,), device=weights.device, dtype=torch.int32)
-    count_at = _per_seq(count_out, n_seq, "count_out")
+        count_at = count_out.data_ptr()
+    else:
+        count_at = _per_seq(count_out, n_seq, "count_out")
     st = _L().crvq_cache_select(_addressof(wc), lens_at, n_seq, n_kv, keep, first, recent, idx_out.data_ptr(), count_at,
                                 None if weights_out is None else _addressof(oc),
                                 _raw_stream(weights.get_device()) if stream is None else
