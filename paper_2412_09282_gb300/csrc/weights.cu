@@ -27,9 +27,13 @@ struct WShape {
   static constexpr int kStage = Tile<D>::kBytes * kBlocks<D>;
   static constexpr int kRing = kStage * kStages;
   static constexpr int kHad = kStages * 32;  // floats per warp: what the ring's tokens had
-  static constexpr int kMost = 256;    // columns at a time
-  static size_t smem(int chunk, bool split) {
+  static constexpr size_t smem(int chunk, bool split) {
     return (size_t)kWarps * (kRing + kHad * 4) + (size_t)chunk * (kQRow * 2 * (split ? 2 : 1) + 16);
+  }
+  // columns at a time: 256, or what a CTA's 227 KB hold (152 of 256 channels, two operands each)
+  static constexpr int most(bool split) {
+    const size_t fit = (232448 - smem(0, split)) / (smem(1, split) - smem(0, split)) / 8 * 8;
+    return fit < 256 ? (int)fit : 256;
   }
 };
 
@@ -309,7 +313,7 @@ template <int D, int FMT, bool SPLIT, bool ONE>
 crvq_status launch(WeightArgs& w, int64_t cols, cudaStream_t stream) {
   using S = WShape<D>;
   auto kernel = weights_kernel<D, FMT, SPLIT, ONE>;
-  w.chunk = (int)min((int64_t)S::kMost, ceil_div(max(cols, (int64_t)1), 8) * 8);
+  w.chunk = (int)min((int64_t)S::most(SPLIT), ceil_div(max(cols, (int64_t)1), 8) * 8);
   const size_t smem = S::smem(w.chunk, SPLIT);
   CRVQ_TRY(smem_limit((const void*)kernel, smem));
   const int per_sm = max(1, min(D == 256 ? 2 : 3, (int)(233472 / (smem + 1024))));
