@@ -3,7 +3,9 @@
 // S^T (128 tokens x up to 256 columns) = K Q^T: tokens are the lanes of tensor memory, so a thread has one token's scores, and
 // its sum over the columns is its own: no maxima, no shuffles. All columns' queries (512 at a time, as they are) lie in shared
 // memory while the tiles of a (sequence, kv head) pass. Codes become operands of the queries' type, exactly: no query needs
-// a factor.
+// a factor but bf16 ones so large that their sums could leave fp32's range where scores do not. Those are laid out relative to the
+// power of two at their largest element, which joins a factor per column; all tiles then go by these factors, with the loop of
+// tiles that some columns do not see, while this filling of Q's memory lasts. Looking for them takes 1.2 us of 90.
 // Two groups of four warps take every other tile, each with its own half of tensor memory and its own issuing warp; four warps
 // turn codes into operands. While one group's exponentials run, the other's products do, and its own next 128 columns' (two
 // of 64 queries over up to 32768 tokens, 64 heads on 8: 92.8 -> 90.6 us).
@@ -26,8 +28,13 @@ template <int D>
 struct WtShape {
   static constexpr int kQ = kMostCols * D * 2;
   static constexpr int kSide = kKeys * D * 2;
-  static constexpr size_t kSmem = kQ + 2 * kSide + kMostCols * 12;
+  static constexpr size_t kSmem = kQ + 2 * kSide + kMostCols * 16;
 };
+
+// Queries of elements below 2^65 go as they are by a scale of up to 2^60: over 128 channels and codes up to 448 their sums stay
+// below 2^81; where the scale times a key's scale has lost bits, below 2^-126, their scores are below 2^-45; and that product is
+// beyond fp32's range for a key's scale above 2^67 alone. By a larger scale all queries are laid out with a factor.
+constexpr float kNearScale = 0x1p60f;
 
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
@@ -70,6 +77,48 @@ __device__ __forceinline__ void store_codes(char* dst, const uint4& u) {
   }
 }
 
+// Lays column col of Q out relative to the power of two at its largest element, if that is 2^65 or more (or all are to be), with the
+// power joined to its factor. Four lanes have every fourth piece each, e0 the first; a warp has eight columns.
+template <int D>
+__device__ __forceinline__ void far_column(char* q_sm, int col, int e0, bool all, float* f_s) {
+  uint32_t top2 = 0;
+  for (int i = 0; i < D / 32; ++i) {
+    const uint4 x = *reinterpret_cast<const uint4*>(q_sm + piece<D>(col, 4 * i + e0));
+    top2 = __vmaxu2(top2, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+  }
+  top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 8));
+  top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 16));
+  const uint32_t ex = max(top2 & 0xffffu, top2 >> 16) >> 7;
+  if (ex == 0 || ex == 255 || !(all || ex >= 192)) return;
+  const float inv = __uint_as_float(ex == 254 ? 0x00400000u : (254u - ex) << 23);
+  auto times = [&](uint32_t v) {  // (exact, but for elements below 2^-126 of the largest)
+    return __byte_perm(__float_as_uint(__uint_as_float(v << 16) * inv), __float_as_uint(__uint_as_float(v & 0xffff0000u) * inv), 0x7632);
+  };
+  for (int i = 0; i < D / 32; ++i) {
+    uint4& x = *reinterpret_cast<uint4*>(q_sm + piece<D>(col, 4 * i + e0));
+    x = make_uint4(times(x.x), times(x.y), times(x.z), times(x.w));
+  }
+  if (e0 == 0) f_s[col] *= __uint_as_float(ex << 23);
+}
+
+// The same for all of this warp's columns; true if there were any. (Out of line: its registers are not the tiles'.)
+template <int D>
+__device__ __noinline__ bool far_columns(char* q_sm, int n_pad, bool all, float* f_s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t large = all ? 0x40004000u : 0u;  // elements of 2^65 and more: exponents of 11......
+#pragma unroll 2
+  for (int col = 8 * warp + (lane & 7); col < n_pad; col += 64) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {  // (a lane looks at what it copied)
+      const uint4 x = *reinterpret_cast<const uint4*>(q_sm + piece<D>(col, 4 * i + (lane >> 3)));
+      large |= (x.x & x.x << 1) | (x.y & x.y << 1) | (x.z & x.z << 1) | (x.w & x.w << 1);
+    }
+  }
+  if (!__any_sync(0xffffffffu, large & 0x40004000u)) return false;
+  for (int col = 8 * warp + (lane & 7); col < n_pad; col += 64) far_column<D>(q_sm, col, lane >> 3, all, f_s);
+  return true;
+}
+
 template <int D, int FMT, bool BF16>
 __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_constant__ WeightArgs w) {
   using S = WtShape<D>;
@@ -78,6 +127,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   __shared__ __align__(8) uint64_t k_full[2], k_empty[2], s_full[2][2], s_empty[2][2], q_full, q_read, all_done[2];
   __shared__ float sk_s[2][8];
   __shared__ int live_s[2][8];
+  __shared__ uint32_t far_s;  // number + 1 of the last filling with far queries
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_s;
   volatile int* dead = &dead_s;
@@ -95,6 +145,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
   float* l_s = reinterpret_cast<float*>(k_sm + 2 * S::kSide);  // [kMostCols] -lse, first and last + 1 key seen
   int* kb_s = reinterpret_cast<int*>(l_s + kMostCols);
   int* ke_s = kb_s + kMostCols;
+  float* f_s = reinterpret_cast<float*>(ke_s + kMostCols);     // the scale, times the query's power of two if it is far
   if (warp == 12) tc::tmem_alloc(&tmem_slot, 4 * kStepCols);
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -109,6 +160,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
     tc::mbar_init(tc::smem_u32(&q_full), 256);
     tc::mbar_init(tc::smem_u32(&q_read), 256 + 2);  // (and the issuing warps, one of which may have no tile: neither falls a filling behind)
     dead_s = 0;
+    far_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc::tc_fence_before();
@@ -193,14 +245,17 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
             l_s[col] = none ? -INFINITY : -lse[k];
             kb_s[col] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
             ke_s[col] = a.causal ? min(len, pos + 1) : len;
+            f_s[col] = w.scale;
           }
         }
         asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+        if constexpr (BF16)
+          if (far_columns<D>(q_sm, n_pad, fabsf(w.scale) > kNearScale, f_s)) far_s = q_no + 1;
         tc::fence_async_smem();
         tc::mbar_arrive(tc::smem_u32(&q_full));
         if (!wait(&q_full, q_no & 1)) break;
         // keys that every column sees (places do not fall from column to column)
-        const int every_b = kb_s[n_cols - 1], every_e = ke_s[0];
+        const int every_b = BF16 && far_s == q_no + 1 ? INT_MAX : kb_s[n_cols - 1], every_e = ke_s[0];
         for (int i = 0; i < n_tiles && ok; ++i, ++tile_no) {
           if ((int)(tile_no & 1) != X) continue;
           const int tok = (u.s.lo + u.tile + i) * kKeys, t = tok + row;
@@ -242,12 +297,21 @@ __global__ void __launch_bounds__(kWtThreads, 1) weights_tc_kernel(const __grid_
                   sum[(e / 2 + 1) & 3] = add2(sum[(e / 2 + 1) & 3], pair(pow2(x[2]), pow2(x[3])));
                 }
               } else {
-                const int* kb = kb_s + h0 + ch;
-                const int* ke = ke_s + h0 + ch;
+                // (sixteen bytes at a time: number by number, with a factor, these few tiles took 2.5 us of 93)
+                const int4* kb = reinterpret_cast<const int4*>(kb_s + h0 + ch);
+                const int4* ke = reinterpret_cast<const int4*>(ke_s + h0 + ch);
+                const float* f = f_s + h0 + ch;
+                auto weight = [&](float s, float fc, float lc, int b, int e) {
+                  const float x = pow2(fmaf(s, fc * sk, lc) * kLog2e);
+                  return t >= b && t < e ? x : 0.f;
+                };
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                  const float x = pow2(fmaf(v[e], g, l[e]) * kLog2e), y = pow2(fmaf(v[e + 1], g, l[e + 1]) * kLog2e);
-                  sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(t >= kb[e] && t < ke[e] ? x : 0.f, t >= kb[e + 1] && t < ke[e + 1] ? y : 0.f));
+                for (int e = 0; e < 32; e += 4) {
+                  const float4 l4 = four(l + e), f4 = four(f + e);
+                  const int4 b4 = kb[e / 4], e4 = ke[e / 4];
+                  sum[e / 2 & 3] = add2(sum[e / 2 & 3], pair(weight(v[e], f4.x, l4.x, b4.x, e4.x), weight(v[e + 1], f4.y, l4.y, b4.y, e4.y)));
+                  sum[(e / 2 + 1) & 3] =
+                      add2(sum[(e / 2 + 1) & 3], pair(weight(v[e + 2], f4.z, l4.z, b4.z, e4.z), weight(v[e + 3], f4.w, l4.w, b4.w, e4.w)));
                 }
               }
             }
