@@ -63,10 +63,12 @@ crvq_status pick_format(AttendArgs& a, int format, cudaStream_t stream) {
 }
 
 // Trees with that many columns over short sequences: units of 16 columns, at two CTAs each or more, up to this many tiles of
-// 128 tokens in all. This form against tiles of 128 rows, us, for (sequences x kv heads, columns, tokens): (1 x 1, 512,
-// 4000) 25, 52; (1 x 8, 64, 4000) 25, 37; (1 x 8, 128, 1000) 21, 32; (1 x 8, 256, 2000) 35, 44; (4 x 8, 64, 1000) 25, 36;
-// (4 x 8, 64, 2000) 35, 38; (1 x 8, 256, 4000) 67, 50; (4 x 8, 128, 1000) 52, 38; (1 x 8, 512, 1000) 52, 42. (Attention
-// without trees keeps its rule, and with it its results.)
+// 128 tokens in all; by clusters up to 64 tiles a unit, else by shares of the line. This form against tiles of 128 rows, us, for
+// (sequences x kv heads, columns, tokens): (1 x 1, 512, 4000) 25, 52; (1 x 8, 64, 4000) 25, 37; (1 x 8, 128, 1000) 21, 32; (1 x
+// 8, 256, 2000) 35, 44; (4 x 8, 64, 1000) 25, 36; (4 x 8, 64, 2000) 35, 38; (1 x 8, 256, 4000) 67, 50; (4 x 8, 128, 1000) 52, 38;
+// (1 x 8, 512, 1000) 52, 42; in a graph (32 x 1, 64, 1500) 24, 29. By the line, in a graph: (1 x 1, 64, 20000) 37, 61; (1 x 1, 64,
+// 50000) 44, 64; (1 x 1, 64, 4000 of a table for 50000) 20, 26; (1 x 2, 64, 10000) 30, 43; (1 x 2, 64, 20000) 34, 45; (4 x 1, 64,
+// 12000) 36, 36. (Attention without trees keeps its rule, and with it its results.)
 constexpr int64_t kFewTiles = 2048;
 inline bool few_tiles(const AttendArgs& a) {
   const int64_t units = most_units<16>(a), tiles = ceil_div((int64_t)a.c.max_pages * a.c.page, 128);

@@ -726,7 +726,8 @@ crvq_status launch_tc(AttendArgs& a, cudaStream_t stream) {
 }
 
 // (bf16 outputs' own rounding is 8 times a single piece's error. fp16 outputs with a single piece were 1.4 to 1.5 times as
-// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 414 to 487 us.)
+// far from exact as their rounding; the second one takes two prompts of up to 1024 tokens over 8192 from 414 to 487 us. Trees of 64
+// tokens over two sequences of up to 65536 in bf16, one piece and two: 1.672e-3 and 1.659e-3 from exact, 340 and 371 us.)
 template <int D, bool TREE>
 crvq_status pick_tc(AttendArgs& a, int format, cudaStream_t stream) {
   const bool two = a.q.type == CRVQ_F16;

@@ -262,7 +262,9 @@ crvq_status launch_keep(KeepArgs& a, bool in_place, cudaStream_t stream) {
   const int64_t units = (int64_t)a.from.n_seq * a.from.n_kv * 2;
   int size = 1;
   while (in_place && size < 8 && size < tiles) size *= 2;
-  // into other pages: two waves of CTAs, so that each has tiles to look up while one is on its way
+  // Into other pages: two waves of CTAs, so that each has tiles to look up while one is on its way. One wave, two, four, a CTA per
+  // tile, us, for (sequences x kv heads, tokens of a sequence): (8 x 32, 2047, e4m3) 71, 59, 55, 56; (2 x 8, 16384) 38, 30, 30, 29; (64 x
+  // 32, 300) 74, 74, 74, 83; (16 x 8, 1000) 13.8, 13.0, 13.1, 13.0; (8 x 8, 4000, 64 channels) 18.2, 16.9, 18.8, 17.7.
   a.tiles = in_place ? size : (int)min(tiles, ceil_div((int64_t)6 * sm_count(), units));
   if (units * a.tiles >= (int64_t)1 << 31) return fail(CRVQ_ERR_UNSUPPORTED, "too many tokens in one call");
   const dim3 grid((unsigned)(units * a.tiles)), threads(kKeepThreads);

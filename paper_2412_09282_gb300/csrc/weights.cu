@@ -329,11 +329,18 @@ crvq_status pick_columns(WeightArgs& w, cudaStream_t stream) {
   // columns of a sequence, by the average where the rows' offsets are on the device (a chunk then, several where there are more)
   const AttendArgs& a = w.a;
   const int64_t cols = a.rows.off ? 2 * ceil_div(a.rows.n_tok * a.group, a.c.n_seq) : (int64_t)a.rows.per * a.group;
+  // Up to 8 columns on average: queries in registers. Against shared memory, us, for (sequences of up to this many tokens x kv heads,
+  // columns): (64 of 4096 x 32, 1, e4m3) 112, 117; (64 of 4096 x 32, 1, int8) 117, 124; (16 of 8192 x 8, 8) 18.7, 19.7; (1 of 65536 x
+  // 8, 8) 15.4, 16.2; (8 of 4096 x 32, 7) 20.5, 21.6; (8 of 4096 x 4, 8, fp32) 7.7, 8.0; (1 of 1001 x 8, 8) 5.4, 5.4.
   if (a.rows.n_tok * a.group <= 8 * (int64_t)a.c.n_seq) return launch<D, FMT, SPLIT, true>(w, min(cols, (int64_t)8), stream);
   return launch<D, FMT, SPLIT, false>(w, cols, stream);
 }
 
-// Columns per sequence, on average, from which tokens are the rows of tcgen05 tiles (weights_tc.cu).
+// Columns per sequence, on average, from which tokens are the rows of tcgen05 tiles (weights_tc.cu). This form against that, us,
+// for (sequences of up to this many tokens x kv heads, columns): (64 of 4096 x 32, 32) 256, 541; (64 of 4096 x 32, 64) 527, 555; (16 of
+// 4096 x 8, 48) 32, 43; (16 of 4096 x 8, 64) 39, 44; (1 of 4096 x 8, 32) 9.3, 10.0; (1 of 4096 x 8, 64) 14.0, 10.3; (1 of 4096 x 8,
+// 128) 24.0, 11.1; (1 of 32768 x 8, 64) 30.6, 31.9; (1 of 32768 x 8, 128) 52, 32; (2 of 32768 x 8, 64) 41, 43; (1 of 1000 x 1, 64)
+// 12.3, 7.2.
 constexpr int64_t kManyColumns = 64;
 
 template <int D>

@@ -9,7 +9,8 @@
 // Two groups of four warps take every other tile, each with its own half of tensor memory and its own issuing warp; four warps
 // turn codes into operands. While one group's exponentials run, the other's products do, and its own next 128 columns' (two
 // of 64 queries over up to 32768 tokens, 64 heads on 8: 92.8 -> 90.6 us).
-// Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; every token is one thread's.
+// Work is split like attend_mma.cuh's line: equal shares of all tiles, a CTA per SM; while a filling of Q's memory lasts, every token
+// is one thread's (the next filling's may be the other group's, which has waited for all to be done with the one before).
 //   What bounds it: the chain from tensor memory to registers, exponentials and sums, 32 columns at a time, of two warps per scheduler
 // (690 TFLOP/s of products; the tensor pipe is active 28% of the time). Slower, in us: four groups of 128 columns 128, loads in
 // two buffers 112 (with 168 registers, and two converting warps for that, 97), an eighth of the exponentials by a polynomial 97,
